@@ -616,9 +616,9 @@ def run(state):
     plan, ws = s["kept"].plan, s["kept"].workspace
     stream = torch.cuda.current_stream().cuda_stream
     if op == "write":
-        vb.vatt_write_kv(plan, s["q"], s["k_new"], s["v_new"], s["q"].stride(1), s["k_new"].stride(1), s["v_new"].stride(1),
-                         s["case"]["n_new"], s["first"], s["new"], s["k"], s["v"], s["table"], s["summary"], s["out_q"], s["after"],
-                         stream)
+        strides = [vb.token_stride(s[x]) for x in ("q", "k_new", "v_new")]
+        vb.vatt_write_kv(plan, s["q"], s["k_new"], s["v_new"], *strides, s["case"]["n_new"], s["first"], s["new"], s["k"], s["v"],
+                         s["table"], s["summary"], s["out_q"], s["after"], stream)
         out = dict(q=s["out_q"], summary=s["summary"], after=s["after"])
         if not s["case"]["back"]:
             out.update(k=s["k"], v=s["v"])
