@@ -347,6 +347,119 @@ int vatt_append_kv(vatt_plan* plan, const void* k_new, const void* v_new, void* 
                    const int32_t* block_table, int32_t* seq_lens, void* stream);
 
 /*
+ * The cache from the projections' outputs to the attention that reads it: rotated and, if wanted, quantised rows written as
+ * they come, blocks of tokens chosen by a cheap bound of their scores, attention over the chosen blocks.
+ *
+ * Formats.  VATT_OPT_KV_FORMAT says how a plan's cache holds its rows:
+ *   VATT_KV_BF16   as described above (the default)
+ *   VATT_KV_E4M3   8 bits a value: sign, 4 exponent bits (bias 7), 3 of the mantissa, largest 448
+ *   VATT_KV_E2M1   4 bits a value: 0 .5 1 1.5 2 3 4 6 with a sign; column 2 j of a row in the lower half of byte j
+ * A quantised buffer (K or V) has vatt_kv_cache_bytes(plan) bytes: the codes of all rows in the order of the bf16 layout, then, from
+ * byte vatt_kv_scale_offset(plan) on, one byte per 32 columns of every row, x, which makes the scale 2^(x - 127) (255: the 32 values are
+ * NaN).  In the contiguous layout the scales are [batch, n_kv_heads, n_max rounded up to a multiple of 8, head_dim / 32], in the
+ * paged one [num_blocks, n_kv_heads, page_size, head_dim / 32].  The scale of 32 values is the smallest power of two at which none
+ * is above the format's largest value; values are rounded to the nearest, ties to even; magnitudes above 1.5 * 2^127 count as that.
+ * On a quantised plan vatt_write_kv, vatt_read_kv, vatt_block_summary_fill, vatt_block_decode and vatt_dense_decode work; the others
+ * that take K or V return VATT_E_UNSUPPORTED_SHAPE.
+ *
+ * Blocks.  VATT_OPT_BLOCK_TOKENS = c (a power of two in 16 .. 256, in the paged layout at most page_size; default 16): block j of a
+ * sequence is its tokens j c .. j c + c - 1.  A block's summary is, for every column, the largest and the smallest value that its
+ * tokens' K rows hold in the cache (bf16; exact for every format; NaN where one of them is NaN):
+ *   contiguous: bf16 [batch, n_kv_heads, ceil(n_max / c), 2, head_dim], paged: [num_blocks, n_kv_heads, page_size / c, 2, head_dim],
+ * vatt_block_summary_bytes(plan) bytes, the largest first.  The calls that take summaries or lists of blocks return
+ * VATT_E_UNSUPPORTED_SHAPE for plans with pages of 8 tokens.
+ */
+enum { VATT_OPT_KV_FORMAT = 17, VATT_OPT_BLOCK_TOKENS = 18 };
+enum { VATT_KV_BF16 = 0, VATT_KV_E4M3 = 1, VATT_KV_E2M1 = 2 };
+size_t vatt_kv_cache_bytes(const vatt_plan* plan);        /* bytes of one buffer, K or V, in the plan's format           */
+size_t vatt_kv_scale_offset(const vatt_plan* plan);       /* byte offset of its scales; vatt_kv_cache_bytes without any  */
+size_t vatt_block_summary_bytes(const vatt_plan* plan);   /* 0 where the plan has no blocks                              */
+size_t vatt_block_list_capacity(const vatt_plan* plan);   /* entries of one list of chosen blocks; 0 likewise            */
+
+/*
+ * Rotary positions.  The first rotary_dim columns of a row are rotary_dim / 2 pairs; pair i of the token at position p is turned by the
+ * angle p f_i (in 64 bits) and multiplied by `attention`:
+ *   layout  VATT_ROTARY_HALF: columns i and i + rotary_dim / 2;  VATT_ROTARY_PAIRS: columns 2 i and 2 i + 1
+ *   f_i = theta^(-2 i / rotary_dim), for contexts longer than the trained original_len scaled by
+ *   VATT_ROTARY_LINEAR      f_i / factor
+ *   VATT_ROTARY_WAVELENGTH  f_i (a + (1 - a) / factor), a = (original_len f_i / (2 pi) - low) / (high - low) clamped to [0, 1]
+ *   VATT_ROTARY_YARN        the same with a = 1 - clamp((i - i0) / max(i1 - i0, 0.001)), where with r(t) = rotary_dim
+ *                           ln(original_len / (2 pi t)) / (2 ln theta): i0 = max(floor r(high), 0), i1 = min(ceil r(low), rotary_dim - 1)
+ *   attention  0 means 1, and 0.1 ln(factor) + 1 with VATT_ROTARY_YARN
+ * rotary_dim: a multiple of 16, at most head_dim (VATT_E_UNSUPPORTED_SHAPE otherwise); 0 means head_dim.  theta > 1, factor >= 1;
+ * original_len > 0 and 0 < low < high where they count.  NULL takes the rotation off the plan (the default).  Host only.
+ */
+enum { VATT_ROTARY_HALF = 0, VATT_ROTARY_PAIRS = 1 };
+enum { VATT_ROTARY_NONE = 0, VATT_ROTARY_LINEAR = 1, VATT_ROTARY_WAVELENGTH = 2, VATT_ROTARY_YARN = 3 };
+typedef struct vatt_rotary {
+  int32_t rotary_dim, layout, scaling, original_len;
+  double theta, factor, low, high, attention;
+} vatt_rotary;
+int vatt_plan_set_rotary(vatt_plan* plan, const vatt_rotary* rotary);
+
+/*
+ * Writes n_new tokens per sequence into the cache: token j of sequence b goes to position first[b] + j, its K row (and its q row,
+ * into out_q) rotated to that position if the plan has a rotation, K and V in the plan's format.  Rotated values are computed in 32 bits
+ * and rounded once.  Single tokens, the tokens of a chunk and whole prompts alike; n_new need not be the plan's q_len.
+ *   q            device, bf16, token j of sequence b at q + (b n_new + j) q_stride, its heads [Hq, d] packed; NULL with out_q for none
+ *   k_new, v_new device, bf16, the same with [Hkv, d] and their strides
+ *   *_stride     elements between tokens, multiples of 8, at least heads * d (the rows of a fused projection's output, for instance)
+ *   n_new        1 .. n_max
+ *   first        device, int32 [B]; a sequence with first[b] outside [0, n_max) is left as it is
+ *   new_lens     device, int32 [B] or NULL: only the first new_lens[b] tokens of sequence b count (clamped to [0, n_new]; NULL: all)
+ *   k, v         device, the cache; tokens that would lie at n_max or beyond are dropped, their rows of out_q left as they were
+ *   summary      device or NULL: the summaries of every block that gets a token become those of the sequence as it now is (whatever they
+ *                were: a sequence may be cut back by writing from an earlier position)
+ *   out_q        device, bf16 [B, n_new, Hq, d]; needs a rotation
+ *   out_lens     device, int32 [B] or NULL: the sequences' new lengths, first[b] + tokens written; not the buffer `first`, which
+ *                workgroups of the call still read
+ * No output may overlap an input.  Pointers 16-byte aligned (lengths: 4).  Errors as in vatt_decode.
+ */
+int vatt_write_kv(vatt_plan* plan, const void* q, const void* k_new, const void* v_new, int64_t q_stride, int64_t k_stride,
+                  int64_t v_stride, int n_new, const int32_t* first, const int32_t* new_lens, void* k, void* v,
+                  const int32_t* block_table, void* summary, void* out_q, int32_t* out_lens, void* stream);
+
+/*
+ * Rows first[b] .. first[b] + n_rows - 1 of every sequence, as far as they are below seq_lens[b], back in bf16 (exact):
+ * out_k, out_v device, bf16 [B, Hkv, n_rows, d]; either may be NULL; rows that a sequence does not have are left as they were.
+ *   first        device, int32 [B] or NULL (0); entries below 0 count as 0
+ */
+int vatt_read_kv(vatt_plan* plan, const void* k, const void* v, const int32_t* block_table, const int32_t* seq_lens,
+                 const int32_t* first, int n_rows, void* out_k, void* out_v, void* stream);
+
+/* The summaries of all blocks of sequences that exist already (seq_lens[b] tokens each, clamped to [0, n_max]). */
+int vatt_block_summary_fill(vatt_plan* plan, const void* k, const int32_t* block_table, const int32_t* seq_lens, void* summary,
+                            void* stream);
+
+/*
+ * Chooses blocks for every (query token, KV head) by an upper bound of their scores.  With the sizes of Algorithm 1 for the n tokens
+ * that the query sees (sink, window, k = topk_abs or floor(topk_frac n)): the blocks that hold a token of the sink or of the
+ * window (of the newest token, if the window is empty) are taken, and of the blocks between them the floor(k / c) best, by
+ *   u = max over the query heads of the KV head of sum_c q_c (q_c < 0 ? smallest_c : largest_c)  >=  <q, K[i]> for every token i in it,
+ * as if computed in 64 bits and rounded to 32; ties go to the lower block, NaN is above everything.
+ *   q            device, bf16 [B, Hq, d] (multi-query plans [B, q_len, Hq, d])
+ *   out_blocks   device, int32 [B, Hkv, vatt_block_list_capacity(plan)]: the taken blocks in ascending order; what lies behind the
+ *                last one is left as it was
+ *   out_count    device, int32 [B, Hkv]: how many they are
+ *   topk_idx, topk_cnt  device or both NULL: the tokens of the chosen blocks between sink and window, in the shapes of
+ *                vatt_decode_given_topk, the same for all heads of a group (entries behind the last one left as they were)
+ */
+int vatt_select_blocks(vatt_plan* plan, const void* q, const void* summary, const int32_t* block_table, const int32_t* seq_lens,
+                       void* workspace, size_t workspace_bytes, int32_t* out_blocks, int32_t* out_count, int32_t* topk_idx,
+                       int32_t* topk_cnt, void* stream);
+
+/*
+ * Attention over the tokens of listed blocks, as far as the query sees them; K and V in the plan's format.
+ *   blocks       device, int32 [B, Hkv, vatt_block_list_capacity(plan)] (multi-query plans [B, q_len, Hkv, ..]), in any order; entries
+ *                that are no block of the sequence add nothing, a block listed twice counts twice
+ *   block_count  device, int32 [B, Hkv]; clamped to [0, capacity]
+ * A query whose list holds no token that it sees gets out_o 0 and out_lse -Inf.  Other arguments as in vatt_dense_decode.
+ */
+int vatt_block_decode(vatt_plan* plan, const void* q, const void* k, const void* v, const int32_t* block_table,
+                      const int32_t* seq_lens, const int32_t* blocks, const int32_t* block_count, void* workspace,
+                      size_t workspace_bytes, float* out_o, float* out_lse, void* stream);
+
+/*
  * KV cache in host memory (the paper's efficiency experiment hosts the KV cache on the CPU and finds the time
  * per step proportional to the amount of KV cache read; its implementation notes keep only the small random
  * cache and the top-k method's own structures on the GPU).

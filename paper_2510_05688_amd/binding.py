@@ -39,6 +39,11 @@ VATT_OPT_CACHE_SLOTS = 13
 VATT_OPT_GIVEN_SPLITS = 14
 VATT_OPT_SPARSE_SPLITS = 15
 VATT_OPT_GIVEN_FUSED = 16
+VATT_OPT_KV_FORMAT = 17
+VATT_OPT_BLOCK_TOKENS = 18
+VATT_KV_BF16, VATT_KV_E4M3, VATT_KV_E2M1 = 0, 1, 2
+VATT_ROTARY_HALF, VATT_ROTARY_PAIRS = 0, 1
+VATT_ROTARY_NONE, VATT_ROTARY_LINEAR, VATT_ROTARY_WAVELENGTH, VATT_ROTARY_YARN = 0, 1, 2, 3
 VATT_BOUND_CLT = 0
 VATT_BOUND_HOEFFDING = 1
 VATT_BOUND_HOEFFDING_RANGE = 2
@@ -49,6 +54,8 @@ EXPORTS = [
     "vatt_plan_index_segment", "vatt_decode", "vatt_decode_static", "vatt_static_scratch_bytes", "vatt_decode_given_topk", "vatt_dense_decode", "vatt_score", "vatt_append_kv", "vatt_stream_read", "vatt_row_read",
     "vatt_random_cache_bytes", "vatt_random_cache_slots", "vatt_random_cache_fill", "vatt_append_kv_cached",
     "vatt_decode_given_topk_cached", "vatt_random_cache_read",
+    "vatt_kv_cache_bytes", "vatt_kv_scale_offset", "vatt_block_summary_bytes", "vatt_block_list_capacity", "vatt_plan_set_rotary",
+    "vatt_write_kv", "vatt_read_kv", "vatt_block_summary_fill", "vatt_select_blocks", "vatt_block_decode",
     "vatt_host_kv_device_pointer", "vatt_status_string",
 ]
 
@@ -62,6 +69,14 @@ class vatt_params(ctypes.Structure):
         ("base_abs", ctypes.c_int32), ("base_frac", ctypes.c_float), ("epsilon", ctypes.c_float),
         ("delta", ctypes.c_float), ("target", ctypes.c_int32), ("sm_scale", ctypes.c_float),
         ("budget_cap_frac", ctypes.c_float),
+    ]
+
+
+class vatt_rotary(ctypes.Structure):
+    _fields_ = [
+        ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+        ("original_len", ctypes.c_int32), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+        ("low", ctypes.c_double), ("high", ctypes.c_double), ("attention", ctypes.c_double),
     ]
 
 
@@ -131,6 +146,21 @@ def _load():
     lib.vatt_decode_given_topk_cached.restype = ctypes.c_int
     lib.vatt_random_cache_read.argtypes = [vp] * 5
     lib.vatt_random_cache_read.restype = ctypes.c_int
+    for name in ("vatt_kv_cache_bytes", "vatt_kv_scale_offset", "vatt_block_summary_bytes", "vatt_block_list_capacity"):
+        getattr(lib, name).argtypes = [vp]
+        getattr(lib, name).restype = sz
+    lib.vatt_plan_set_rotary.argtypes = [vp, ctypes.POINTER(vatt_rotary)]
+    lib.vatt_plan_set_rotary.restype = ctypes.c_int
+    lib.vatt_write_kv.argtypes = [vp] * 4 + [i64] * 3 + [ctypes.c_int] + [vp] * 9
+    lib.vatt_write_kv.restype = ctypes.c_int
+    lib.vatt_read_kv.argtypes = [vp] * 6 + [ctypes.c_int] + [vp] * 3
+    lib.vatt_read_kv.restype = ctypes.c_int
+    lib.vatt_block_summary_fill.argtypes = [vp] * 6
+    lib.vatt_block_summary_fill.restype = ctypes.c_int
+    lib.vatt_select_blocks.argtypes = [vp] * 6 + [sz] + [vp] * 5
+    lib.vatt_select_blocks.restype = ctypes.c_int
+    lib.vatt_block_decode.argtypes = [vp] * 9 + [sz] + [vp] * 3
+    lib.vatt_block_decode.restype = ctypes.c_int
     lib.vatt_status_string.argtypes = [ctypes.c_int]
     lib.vatt_status_string.restype = ctypes.c_char_p
     return lib
@@ -313,6 +343,82 @@ def vatt_random_cache_read(plan, rcache, out_tokens, out_counts, stream=None) ->
     rc = _lib.vatt_random_cache_read(plan, _ptr(rcache), _ptr(out_tokens), _ptr(out_counts), _ptr(stream))
     if rc != VATT_OK:
         raise VattError(rc, "vatt_random_cache_read")
+
+
+def vatt_kv_cache_bytes(plan) -> int:
+    return int(_lib.vatt_kv_cache_bytes(plan))
+
+
+def vatt_kv_scale_offset(plan) -> int:
+    return int(_lib.vatt_kv_scale_offset(plan))
+
+
+def vatt_block_summary_bytes(plan) -> int:
+    return int(_lib.vatt_block_summary_bytes(plan))
+
+
+def vatt_block_list_capacity(plan) -> int:
+    return int(_lib.vatt_block_list_capacity(plan))
+
+
+def vatt_plan_set_rotary(plan, rotary) -> None:
+    """`rotary` is a vatt_rotary, a dict of its fields (those left out are 0), or None for no rotation."""
+    if isinstance(rotary, dict):
+        rotary = vatt_rotary(**rotary)
+    rc = _lib.vatt_plan_set_rotary(plan, None if rotary is None else ctypes.byref(rotary))
+    if rc != VATT_OK:
+        raise VattError(rc, "vatt_plan_set_rotary")
+
+
+def token_stride(x) -> int:
+    """Elements between the tokens of a tensor [B, n_new, heads, d].  (torch's strides say nothing in dimensions of size 1.)"""
+    b, n_new, heads, d = x.shape
+    rows = (heads == 1 or x.stride(2) == d) and x.stride(3) == 1 and (b == 1 or n_new == 1 or x.stride(0) == n_new * x.stride(1))
+    if not rows:
+        raise ValueError("heads have to lie one behind the other, sequences n_new tokens apart")
+    if n_new > 1:
+        return x.stride(1)
+    return x.stride(0) if b > 1 else heads * d
+
+
+def vatt_write_kv(plan, q, k_new, v_new, q_stride, k_stride, v_stride, n_new, first, new_lens, k, v, block_table, summary, out_q,
+                  out_lens, stream=None) -> None:
+    """The strides are elements between tokens: see token_stride."""
+    rc = _lib.vatt_write_kv(plan, _ptr(q), _ptr(k_new), _ptr(v_new), q_stride, k_stride, v_stride, n_new, _ptr(first),
+                            _ptr(new_lens), _ptr(k), _ptr(v), _ptr(block_table), _ptr(summary), _ptr(out_q), _ptr(out_lens),
+                            _ptr(stream))
+    if rc != VATT_OK:
+        raise VattError(rc, "vatt_write_kv")
+
+
+def vatt_read_kv(plan, k, v, block_table, seq_lens, first, n_rows, out_k, out_v, stream=None) -> None:
+    rc = _lib.vatt_read_kv(plan, _ptr(k), _ptr(v), _ptr(block_table), _ptr(seq_lens), _ptr(first), n_rows, _ptr(out_k),
+                           _ptr(out_v), _ptr(stream))
+    if rc != VATT_OK:
+        raise VattError(rc, "vatt_read_kv")
+
+
+def vatt_block_summary_fill(plan, k, block_table, seq_lens, summary, stream=None) -> None:
+    rc = _lib.vatt_block_summary_fill(plan, _ptr(k), _ptr(block_table), _ptr(seq_lens), _ptr(summary), _ptr(stream))
+    if rc != VATT_OK:
+        raise VattError(rc, "vatt_block_summary_fill")
+
+
+def vatt_select_blocks(plan, q, summary, block_table, seq_lens, workspace, out_blocks, out_count, topk_idx=None, topk_cnt=None,
+                       stream=None) -> None:
+    rc = _lib.vatt_select_blocks(plan, _ptr(q), _ptr(summary), _ptr(block_table), _ptr(seq_lens), _ptr(workspace),
+                                 _nbytes(workspace), _ptr(out_blocks), _ptr(out_count), _ptr(topk_idx), _ptr(topk_cnt),
+                                 _ptr(stream))
+    if rc != VATT_OK:
+        raise VattError(rc, "vatt_select_blocks")
+
+
+def vatt_block_decode(plan, q, k, v, block_table, seq_lens, blocks, block_count, workspace, out_o, out_lse, stream=None) -> None:
+    rc = _lib.vatt_block_decode(plan, _ptr(q), _ptr(k), _ptr(v), _ptr(block_table), _ptr(seq_lens), _ptr(blocks),
+                                _ptr(block_count), _ptr(workspace), _nbytes(workspace), _ptr(out_o), _ptr(out_lse),
+                                _ptr(stream))
+    if rc != VATT_OK:
+        raise VattError(rc, "vatt_block_decode")
 
 
 def vatt_row_read(src, rows_total: int, rows, count: int, sink, stream=None) -> None:

@@ -104,6 +104,9 @@ int build_plan(Plan& pl, const vatt_params& p, int q_len, int device) {
   pl.score_order = pl.group_major && p.n_max < 65536 && score_bytes(pl) < kScoreBytesLarge ? kScoreOrderKvHead : kScoreOrderBlocks;
   if (q_len != 1) pl.score_order = kScoreOrderTile;
 
+  pl.kv_format = VATT_KV_BF16;
+  pl.block_tokens = p.kv_layout == VATT_LAYOUT_PAGED && p.page_size < 16 ? 0 : 16;
+
   const int n_max = p.n_max;
   pl.n_pad = (int)align_up((size_t)n_max, 256);
   pl.n_sub = (int)align_up((size_t)n_max, 256) / kSubTile;
@@ -257,6 +260,17 @@ void* scratch_of(int device) {
   return g_scratch_ptr[device];
 }
 
+// What every call on the cache's rows checks.
+int check_cache(const vatt_plan* plan, const int32_t* block_table) {
+  if (!plan) return VATT_E_INVALID_ARG;
+  if (plan->pl.device < 0) return VATT_E_NO_DEVICE;
+  if (plan->pl.p.kv_layout == VATT_LAYOUT_PAGED && !block_table) return VATT_E_INVALID_ARG;
+  int cur = -1;
+  if (hipGetDevice(&cur) != hipSuccess) return VATT_E_HIP;
+  if (cur != plan->pl.device) return VATT_E_HIP;
+  return VATT_OK;
+}
+
 int check_common(const vatt_plan* plan, const void* ws, size_t ws_bytes, const int32_t* block_table) {
   if (!plan || !ws) return VATT_E_INVALID_ARG;
   if (plan->pl.device < 0) return VATT_E_NO_DEVICE;
@@ -269,12 +283,30 @@ int check_common(const vatt_plan* plan, const void* ws, size_t ws_bytes, const i
   return VATT_OK;
 }
 
+// Calls that read or write rows of a bf16 cache only.
+bool bf16_cache(const vatt_plan* plan) { return plan->pl.kv_format == VATT_KV_BF16; }
+
 #define VATT_LAUNCH(expr)                    \
   do {                                       \
     if ((expr) != hipSuccess) return VATT_E_HIP; \
   } while (0)
 
 }  // namespace
+
+size_t kv_scale_offset(const Plan& pl) {
+  const size_t heads = pl.p.kv_layout == VATT_LAYOUT_PAGED ? (size_t)pl.p.num_blocks * pl.p.n_kv_heads : (size_t)pl.p.batch * pl.p.n_kv_heads;
+  const size_t bytes = heads * (pl.p.kv_layout == VATT_LAYOUT_PAGED ? pl.p.page_size : pl.p.n_max) * kv_row_bytes(pl);
+  return pl.kv_format == VATT_KV_BF16 ? bytes : align_up(bytes, 256);
+}
+
+// (a window of w >= 1 tokens touches at most w / c + 2 blocks of c)
+int block_list_capacity(const Plan& pl) {
+  const int c = pl.block_tokens;
+  if (c == 0) return 0;
+  const int64_t most = ((int64_t)pl.p.sink + c - 1) / c + pl.p.window / c + 2 + pl.k_max / c;
+  return (int)std::min<int64_t>((pl.p.n_max + c - 1) / c, most);
+}
+
 }  // namespace vatt
 
 using namespace vatt;
@@ -402,6 +434,17 @@ int vatt_plan_set_option(vatt_plan* plan, int option, int value) {
     (option == VATT_OPT_GIVEN_SPLITS ? plan->pl.given_splits : plan->pl.sparse_splits) = value;
     return VATT_OK;
   }
+  if (option == VATT_OPT_KV_FORMAT) {
+    if (value != VATT_KV_BF16 && value != VATT_KV_E4M3 && value != VATT_KV_E2M1) return VATT_E_INVALID_ARG;
+    plan->pl.kv_format = value;
+    return VATT_OK;
+  }
+  if (option == VATT_OPT_BLOCK_TOKENS) {
+    if (value < 16 || value > 256 || ilog2_exact(value) < 0) return VATT_E_INVALID_ARG;
+    if (plan->pl.p.kv_layout == VATT_LAYOUT_PAGED && value > plan->pl.p.page_size) return VATT_E_UNSUPPORTED_SHAPE;
+    plan->pl.block_tokens = value;
+    return VATT_OK;
+  }
   if (option == VATT_OPT_CACHE_SLOTS) {
     if (value < 1 || value > kCacheSlotsMax || (value & 3) != 0) return VATT_E_INVALID_ARG;
     plan->pl.cache_slots = value;
@@ -457,6 +500,7 @@ int vatt_score(vatt_plan* plan, const void* q, const void* k, const int32_t* blo
                void* workspace, size_t workspace_bytes, void* stream) {
   int rc = check_common(plan, workspace, workspace_bytes, block_table);
   if (rc != VATT_OK) return rc;
+  if (!bf16_cache(plan)) return VATT_E_UNSUPPORTED_SHAPE;
   if (!q || !k || !seq_lens || !aligned16(q) || !aligned16(k)) return VATT_E_INVALID_ARG;
   if (plan->pl.q_len > 1)
     VATT_LAUNCH(launch_score_chunk(plan->pl, q, k, block_table, seq_lens, workspace, static_cast<hipStream_t>(stream)));
@@ -486,6 +530,7 @@ int vatt_decode(vatt_plan* plan, const void* q, const void* k, const void* v, co
                 float* out_stats, void* stream) {
   int rc = check_common(plan, workspace, workspace_bytes, block_table);
   if (rc != VATT_OK) return rc;
+  if (!bf16_cache(plan)) return VATT_E_UNSUPPORTED_SHAPE;
   if (!q || !k || !v || !seq_lens || !seq_seeds || !out_o || !out_idx || !out_counts) return VATT_E_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return VATT_E_INVALID_ARG;
   const Plan& pl = plan->pl;
@@ -520,6 +565,7 @@ int vatt_decode_given_topk(vatt_plan* plan, const void* q, const void* k, const 
                            float* out_stats, void* stream) {
   int rc = check_common(plan, workspace, workspace_bytes, block_table);
   if (rc != VATT_OK) return rc;
+  if (!bf16_cache(plan)) return VATT_E_UNSUPPORTED_SHAPE;
   if (!q || !k || !v || !seq_lens || !seq_seeds || !topk_idx || !topk_cnt || !out_o || !out_idx || !out_counts)
     return VATT_E_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return VATT_E_INVALID_ARG;
@@ -538,6 +584,7 @@ int vatt_random_cache_fill(vatt_plan* plan, const void* k, const void* v, const 
                            const int32_t* seq_lens, const uint64_t* cache_seeds, void* rcache, void* stream) {
   if (!plan) return VATT_E_INVALID_ARG;
   if (plan->pl.device < 0) return VATT_E_NO_DEVICE;
+  if (!bf16_cache(plan)) return VATT_E_UNSUPPORTED_SHAPE;
   if (plan->pl.p.kv_layout == VATT_LAYOUT_PAGED && !block_table) return VATT_E_INVALID_ARG;
   if (!k || !v || !seq_lens || !cache_seeds || !rcache) return VATT_E_INVALID_ARG;
   if (!aligned16(k) || !aligned16(v) || (reinterpret_cast<uintptr_t>(rcache) & 255u) != 0) return VATT_E_INVALID_ARG;
@@ -551,6 +598,7 @@ int vatt_append_kv_cached(vatt_plan* plan, const void* k_new, const void* v_new,
                           void* stream) {
   if (!plan) return VATT_E_INVALID_ARG;
   if (plan->pl.device < 0) return VATT_E_NO_DEVICE;
+  if (!bf16_cache(plan)) return VATT_E_UNSUPPORTED_SHAPE;
   if (plan->pl.p.kv_layout == VATT_LAYOUT_PAGED && !block_table) return VATT_E_INVALID_ARG;
   if (!k_new || !v_new || !k || !v || !seq_lens || !cache_seeds || !rcache) return VATT_E_INVALID_ARG;
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k) || !aligned16(v) ||
@@ -569,6 +617,7 @@ int vatt_decode_given_topk_cached(vatt_plan* plan, const void* q, const void* k,
                                   void* stream) {
   int rc = check_common(plan, workspace, workspace_bytes, block_table);
   if (rc != VATT_OK) return rc;
+  if (!bf16_cache(plan)) return VATT_E_UNSUPPORTED_SHAPE;
   if (!q || !k || !v || !seq_lens || !seq_seeds || !topk_idx || !topk_cnt || !rcache || !out_o || !out_idx || !out_counts)
     return VATT_E_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || (reinterpret_cast<uintptr_t>(rcache) & 255u) != 0)
@@ -594,6 +643,11 @@ int vatt_dense_decode(vatt_plan* plan, const void* q, const void* k, const void*
   if (rc != VATT_OK) return rc;
   if (!q || !k || !v || !seq_lens || !out_o) return VATT_E_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return VATT_E_INVALID_ARG;
+  if (!bf16_cache(plan)) {
+    VATT_LAUNCH(launch_attend(plan->pl, q, k, v, block_table, seq_lens, nullptr, nullptr, workspace, out_o, out_lse,
+                              static_cast<hipStream_t>(stream)));
+    return VATT_OK;
+  }
   VATT_LAUNCH(launch_dense(plan->pl, q, k, v, block_table, seq_lens, workspace, out_o, out_lse,
                            static_cast<hipStream_t>(stream)));
   return VATT_OK;
@@ -633,10 +687,142 @@ int vatt_append_kv(vatt_plan* plan, const void* k_new, const void* v_new, void* 
                    const int32_t* block_table, int32_t* seq_lens, void* stream) {
   if (!plan) return VATT_E_INVALID_ARG;
   if (plan->pl.device < 0) return VATT_E_NO_DEVICE;
+  if (!bf16_cache(plan)) return VATT_E_UNSUPPORTED_SHAPE;
   if (plan->pl.p.kv_layout == VATT_LAYOUT_PAGED && !block_table) return VATT_E_INVALID_ARG;
   if (!k_new || !v_new || !k || !v || !seq_lens) return VATT_E_INVALID_ARG;
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k) || !aligned16(v)) return VATT_E_INVALID_ARG;
   VATT_LAUNCH(launch_append(plan->pl, k_new, v_new, k, v, block_table, seq_lens, static_cast<hipStream_t>(stream)));
+  return VATT_OK;
+}
+
+size_t vatt_kv_cache_bytes(const vatt_plan* plan) {
+  if (!plan) return 0;
+  const Plan& pl = plan->pl;
+  if (pl.kv_format == VATT_KV_BF16) return kv_scale_offset(pl);
+  const bool paged = pl.p.kv_layout == VATT_LAYOUT_PAGED;
+  const size_t heads = (size_t)(paged ? pl.p.num_blocks : pl.p.batch) * pl.p.n_kv_heads;
+  return kv_scale_offset(pl) + heads * (paged ? (size_t)pl.p.page_size : align_up(pl.p.n_max, 8)) * (pl.p.head_dim / 32);
+}
+
+size_t vatt_kv_scale_offset(const vatt_plan* plan) { return plan ? kv_scale_offset(plan->pl) : 0; }
+
+size_t vatt_block_summary_bytes(const vatt_plan* plan) {
+  if (!plan || plan->pl.block_tokens == 0) return 0;
+  const Plan& pl = plan->pl;
+  const size_t row = 4 * (size_t)pl.p.head_dim * pl.p.n_kv_heads;
+  if (pl.p.kv_layout == VATT_LAYOUT_PAGED) return (size_t)pl.p.num_blocks * (pl.p.page_size / pl.block_tokens) * row;
+  return (size_t)pl.p.batch * ((pl.p.n_max + pl.block_tokens - 1) / pl.block_tokens) * row;
+}
+
+size_t vatt_block_list_capacity(const vatt_plan* plan) { return plan ? (size_t)block_list_capacity(plan->pl) : 0; }
+
+int vatt_plan_set_rotary(vatt_plan* plan, const vatt_rotary* rotary) {
+  if (!plan) return VATT_E_INVALID_ARG;
+  Plan& pl = plan->pl;
+  if (!rotary) {
+    pl.rotary_dim = 0;
+    return VATT_OK;
+  }
+  const vatt_rotary r = *rotary;
+  const int dim = r.rotary_dim == 0 ? pl.p.head_dim : r.rotary_dim;
+  if (dim < 0) return VATT_E_INVALID_ARG;
+  if (dim % 16 != 0 || dim > pl.p.head_dim) return VATT_E_UNSUPPORTED_SHAPE;
+  if (r.layout != VATT_ROTARY_HALF && r.layout != VATT_ROTARY_PAIRS) return VATT_E_INVALID_ARG;
+  if (r.scaling < VATT_ROTARY_NONE || r.scaling > VATT_ROTARY_YARN) return VATT_E_INVALID_ARG;
+  if (!(r.theta > 1.0) || !std::isfinite(r.theta) || !(r.attention >= 0.0) || !std::isfinite(r.attention)) return VATT_E_INVALID_ARG;
+  if (r.scaling != VATT_ROTARY_NONE && (!(r.factor >= 1.0) || !std::isfinite(r.factor))) return VATT_E_INVALID_ARG;
+  const bool by_turns = r.scaling == VATT_ROTARY_WAVELENGTH || r.scaling == VATT_ROTARY_YARN;
+  if (by_turns && (r.original_len <= 0 || !(r.low > 0.0) || !(r.high > r.low) || !std::isfinite(r.high))) return VATT_E_INVALID_ARG;
+  const double len = (double)r.original_len;
+  double lo = 0.0, hi = 0.0;
+  if (r.scaling == VATT_ROTARY_YARN) {
+    // (the pair that makes t turns within the original length)
+    auto pair = [&](double t) { return dim * std::log(len / (2.0 * M_PI * t)) / (2.0 * std::log(r.theta)); };
+    lo = std::max(std::floor(pair(r.high)), 0.0);
+    hi = std::min(std::ceil(pair(r.low)), dim - 1.0);
+  }
+  for (int i = 0; i < dim / 2; ++i) {
+    const double f = std::pow(r.theta, -2.0 * i / dim);
+    double keep = 1.0;
+    if (r.scaling == VATT_ROTARY_LINEAR) keep = 0.0;
+    if (r.scaling == VATT_ROTARY_WAVELENGTH) keep = std::min(std::max((len * f / (2.0 * M_PI) - r.low) / (r.high - r.low), 0.0), 1.0);
+    if (r.scaling == VATT_ROTARY_YARN) keep = 1.0 - std::min(std::max((i - lo) / std::max(hi - lo, 0.001), 0.0), 1.0);
+    pl.rotary_freq[i] = r.scaling == VATT_ROTARY_NONE ? f : f * keep + f / r.factor * (1.0 - keep);
+  }
+  pl.rotary_dim = dim;
+  pl.rotary_pairs = r.layout == VATT_ROTARY_PAIRS;
+  pl.rotary_attention = r.attention > 0.0 ? r.attention : r.scaling == VATT_ROTARY_YARN ? 0.1 * std::log(r.factor) + 1.0 : 1.0;
+  return VATT_OK;
+}
+
+int vatt_write_kv(vatt_plan* plan, const void* q, const void* k_new, const void* v_new, int64_t q_stride, int64_t k_stride,
+                  int64_t v_stride, int n_new, const int32_t* first, const int32_t* new_lens, void* k, void* v,
+                  const int32_t* block_table, void* summary, void* out_q, int32_t* out_lens, void* stream) {
+  if (!plan) return VATT_E_INVALID_ARG;
+  const Plan& pl = plan->pl;
+  if (!k_new || !v_new || !first || !k || !v) return VATT_E_INVALID_ARG;
+  if (!q != !out_q || (q && (pl.rotary_dim == 0 || q == out_q))) return VATT_E_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k) || !aligned16(v) || !aligned16(summary) || !aligned16(out_q))
+    return VATT_E_INVALID_ARG;
+  if (n_new < 1 || n_new > pl.p.n_max || out_lens == first) return VATT_E_INVALID_ARG;
+  const int64_t q_row = (int64_t)pl.p.n_q_heads * pl.p.head_dim, kv_row = (int64_t)pl.p.n_kv_heads * pl.p.head_dim;
+  if ((q && (q_stride < q_row || q_stride % 8 != 0)) || k_stride < kv_row || k_stride % 8 != 0 || v_stride < kv_row || v_stride % 8 != 0)
+    return VATT_E_INVALID_ARG;
+  if (summary && pl.block_tokens == 0) return VATT_E_UNSUPPORTED_SHAPE;
+  const int rc = check_cache(plan, block_table);
+  if (rc != VATT_OK) return rc;
+  VATT_LAUNCH(launch_write(pl, q, k_new, v_new, q_stride, k_stride, v_stride, n_new, first, new_lens, k, v, block_table, summary, out_q,
+                           out_lens, static_cast<hipStream_t>(stream)));
+  return VATT_OK;
+}
+
+int vatt_read_kv(vatt_plan* plan, const void* k, const void* v, const int32_t* block_table, const int32_t* seq_lens,
+                 const int32_t* first, int n_rows, void* out_k, void* out_v, void* stream) {
+  if (!plan) return VATT_E_INVALID_ARG;
+  if (!seq_lens || (out_k && !k) || (out_v && !v) || (!out_k && !out_v) || n_rows < 1 || n_rows > plan->pl.p.n_max) return VATT_E_INVALID_ARG;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(out_k) || !aligned16(out_v)) return VATT_E_INVALID_ARG;
+  const int rc = check_cache(plan, block_table);
+  if (rc != VATT_OK) return rc;
+  VATT_LAUNCH(launch_read(plan->pl, k, v, block_table, seq_lens, first, n_rows, out_k, out_v, static_cast<hipStream_t>(stream)));
+  return VATT_OK;
+}
+
+int vatt_block_summary_fill(vatt_plan* plan, const void* k, const int32_t* block_table, const int32_t* seq_lens, void* summary,
+                            void* stream) {
+  if (!plan) return VATT_E_INVALID_ARG;
+  if (!k || !seq_lens || !summary || !aligned16(k) || !aligned16(summary)) return VATT_E_INVALID_ARG;
+  if (plan->pl.block_tokens == 0) return VATT_E_UNSUPPORTED_SHAPE;
+  const int rc = check_cache(plan, block_table);
+  if (rc != VATT_OK) return rc;
+  VATT_LAUNCH(launch_block_summary(plan->pl, k, block_table, seq_lens, summary, static_cast<hipStream_t>(stream)));
+  return VATT_OK;
+}
+
+int vatt_select_blocks(vatt_plan* plan, const void* q, const void* summary, const int32_t* block_table, const int32_t* seq_lens,
+                       void* workspace, size_t workspace_bytes, int32_t* out_blocks, int32_t* out_count, int32_t* topk_idx,
+                       int32_t* topk_cnt, void* stream) {
+  if (!plan) return VATT_E_INVALID_ARG;
+  if (!q || !summary || !seq_lens || !out_blocks || !out_count || !topk_idx != !topk_cnt) return VATT_E_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(summary)) return VATT_E_INVALID_ARG;
+  if (plan->pl.block_tokens == 0) return VATT_E_UNSUPPORTED_SHAPE;
+  const int rc = check_common(plan, workspace, workspace_bytes, block_table);
+  if (rc != VATT_OK) return rc;
+  VATT_LAUNCH(launch_select_blocks(plan->pl, q, summary, block_table, seq_lens, workspace, out_blocks, out_count, topk_idx, topk_cnt,
+                                   static_cast<hipStream_t>(stream)));
+  return VATT_OK;
+}
+
+int vatt_block_decode(vatt_plan* plan, const void* q, const void* k, const void* v, const int32_t* block_table,
+                      const int32_t* seq_lens, const int32_t* blocks, const int32_t* block_count, void* workspace,
+                      size_t workspace_bytes, float* out_o, float* out_lse, void* stream) {
+  if (!plan) return VATT_E_INVALID_ARG;
+  if (!q || !k || !v || !seq_lens || !blocks || !block_count || !out_o) return VATT_E_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return VATT_E_INVALID_ARG;
+  if (plan->pl.block_tokens == 0) return VATT_E_UNSUPPORTED_SHAPE;
+  const int rc = check_common(plan, workspace, workspace_bytes, block_table);
+  if (rc != VATT_OK) return rc;
+  VATT_LAUNCH(launch_attend(plan->pl, q, k, v, block_table, seq_lens, blocks, block_count, workspace, out_o, out_lse,
+                            static_cast<hipStream_t>(stream)));
   return VATT_OK;
 }
 

@@ -1,0 +1,556 @@
+// Attention over the tokens of listed blocks, or over all tokens of a quantised cache.
+#include <algorithm>
+
+#include "vatt_format.h"
+
+namespace vatt {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+__device__ __forceinline__ uint32_t lower_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+
+constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / kWave;
+constexpr int kUnit = 32;          // keys that a wave takes at a time
+constexpr int kSlots = 1024;       // groups of 8 tokens that a workgroup looks up at a time
+constexpr int kNowhere = 0x7fffff00;  // token of a group that does not exist: beyond every sequence
+
+struct AttendArgs {
+  const uint16_t* q;
+  const unsigned char* k;
+  const unsigned char* v;
+  int64_t scale_off;
+  const int32_t* seq_lens;
+  const int32_t* blocks;  // nullptr: all tokens
+  const int32_t* block_count;
+  float* part;     // [B * q_len * Hq][splits][d]: sums of the weighted V rows
+  float2* part_ml;  // [B * q_len * Hq][splits]: (max, sum of the weights); max -Inf: no token seen
+  float* out_o;
+  float* out_lse;
+  RowMap M;
+  int Hq, Hkv, q_len, splits, rounds, capacity, block_shift;
+  float sm_scale;
+};
+
+// A list of tokens in groups of 8: how many groups, and the first token of each (kNowhere where there is none).
+struct TokenList {
+  const int32_t* blocks;
+  int count, shift, n;  // n: tokens of the sequence that count
+};
+__device__ __forceinline__ TokenList token_list(const AttendArgs& A, int vb, int kvh, int n) {
+  TokenList L = {nullptr, 0, A.block_shift, n};
+  if (A.blocks) {
+    const int64_t row = (int64_t)vb * A.Hkv + kvh;
+    L.blocks = A.blocks + row * A.capacity;
+    L.count = min(max(A.block_count[row], 0), A.capacity) << (A.block_shift - 3);
+  } else {
+    L.count = (n + 7) / 8;
+  }
+  return L;
+}
+__device__ __forceinline__ int token_of(const TokenList& L, int group) {
+  if (group >= L.count) return kNowhere;
+  if (!L.blocks) return group * 8;
+  const int blk = L.blocks[group >> (L.shift - 3)];
+  if ((uint32_t)blk > (uint32_t)(L.n - 1) >> L.shift) return kNowhere;
+  return (blk << L.shift) + ((group << 3) & ((1 << L.shift) - 1));
+}
+
+// The scale bytes of one row (d / 32 of them).
+template <int D>
+__device__ __forceinline__ uint32_t row_scales(const unsigned char* p) {
+  if constexpr (D == 128) return *reinterpret_cast<const uint32_t*>(p);
+  else return *reinterpret_cast<const uint16_t*>(p);
+}
+
+// Attention with the query vectors of a KV head on the matrix cores, 32 keys of a wave at a time:
+//   S [keys x vectors] = K Q^T   and   O^T [d x vectors] += V^T P^T,   P = exp(S - m),
+// both v_mfma_f32_16x16x32_bf16 (operand lane l: row or column l % 16, eight inner elements; result lane l: column l % 16, rows
+// 4 (l / 16) .. + 3).  The result layout of S is the operand layout of P when lane group g = l / 16 takes keys 4 g + r and 16 + 4 g + r
+// as inner elements r and 4 + r.
+//   * Codes become bf16 in registers, exactly, with their scales.  Which columns of a row are inner elements of which step of the first
+//     product is free as long as K and q agree: every lane loads 16 bytes of its row and takes the 8 to 32 values in them as one to
+//     four steps.
+//   * V is not transposed: a lane loads d / 16 columns of the eight rows of its group and pairs them by rows in registers.
+//   * P goes in as three bf16 terms that add up to the fp32 value, so that the sums keep fp32 accuracy.
+// The running maximum of a column moves only when a score passes it by more than kLazy.
+template <int D, int FMT, bool PAGED, int NQT>
+__global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A) {
+  constexpr int S = D / 32;  // steps over a row of K
+  constexpr int E = D / 16;  // values of a V row per lane = tiles over the head dimension
+  constexpr int ROW = kRowBytes<FMT, D>;
+  constexpr int KB = ROW / 4 < 16 ? ROW / 4 : 16, KL = ROW / 4 / KB;  // K: bytes per load, loads per lane and row
+  constexpr int STEPS = S / KL;                                       // steps that one load holds
+  constexpr int VB = ROW / 16;                                        // V: bytes per lane and row
+  constexpr int VW = VB < 4 ? 1 : VB / 4;
+  constexpr bool QUANT = FMT != VATT_KV_BF16;
+  constexpr float kLazy = 6.0f, kLog2e = 1.44269504088896340736f;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g4 = lane >> 4;
+  const int kvh = blockIdx.x, split = (int)blockIdx.y / A.rounds, round = (int)blockIdx.y - split * A.rounds;
+  const int G = A.Hq / A.Hkv, Q = A.q_len;
+  const bool listed = A.blocks != nullptr;
+  const int seq = listed ? seq_of_pair(blockIdx.z, Q) : blockIdx.z;
+  const int n_seq = min(max(A.seq_lens[seq], 1), A.M.n_max);
+  // listed: the vectors are the heads of one query token; else those of all query tokens
+  const int t0 = listed ? (int)blockIdx.z - seq * Q : 0, vectors = listed ? G : Q * G;
+  const int n = listed ? max(n_seq - (Q - 1 - t0), 1) : n_seq;
+  const TokenList L = token_list(A, blockIdx.z, kvh, n);
+  const int c_base = round * 16 * NQT;
+
+  __shared__ __align__(16) int s_tok[kSlots];
+  __shared__ int s_at[kSlots];
+  __shared__ float4 s_o[kAttendWaves][4][E / 4][kWave];
+  __shared__ float s_m[kAttendWaves][16], s_l[kAttendWaves][16];
+
+  uint4 bq[NQT][S];
+  int seen[NQT];
+  int least = n;
+#pragma unroll
+  for (int nt = 0; nt < NQT; ++nt) {
+    const int c = min(c_base + nt * 16 + i16, vectors - 1);  // (columns beyond the last vector repeat it and are not stored)
+    const int t = t0 + c / G, g = c % G;
+    const uint16_t* src = A.q + (((int64_t)seq * Q + t) * A.Hq + (int64_t)kvh * G + g) * D;
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      bq[nt][s] = *reinterpret_cast<const uint4*>(src + (s / STEPS) * 4 * (STEPS * 8) + g4 * (STEPS * 8) + (s % STEPS) * 8);
+    seen[nt] = max(n_seq - (Q - 1 - t), 1);
+  }
+  if (!listed) least = max(n_seq - (Q - 1), 1);
+
+  f32x4_t acc[NQT][E];
+  float mrun[NQT], lrun[NQT];
+  bool any[NQT];
+#pragma unroll
+  for (int nt = 0; nt < NQT; ++nt) {
+    mrun[nt] = -INFINITY;
+    lrun[nt] = 0.f;
+    any[nt] = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[nt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int64_t head = (int64_t)seq * A.Hkv + kvh;
+  const int page8 = A.M.page_shift - 3;
+  auto row_of = [&](int slot, int r) -> int64_t {
+    const int at = s_at[slot];
+    if constexpr (PAGED) return ((((int64_t)(at >> page8) * A.Hkv + kvh)) << A.M.page_shift) + ((at & ((1 << page8) - 1)) << 3) + r;
+    else return head * A.M.n_max + min(at + r, n_seq - 1);
+  };
+  auto scale_row_of = [&](int slot, int r) -> int64_t {
+    if constexpr (PAGED) return row_of(slot, r);
+    else return head * A.M.n_scales + s_at[slot] + r;
+  };
+  uint32_t kr[2][KL][KB / 4], ks[2], vr[8][VW], vs[2][QUANT ? D / 32 : 1];
+  auto load_k = [&](int s0) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int slot = s0 + 2 * t + (i16 >> 3), r = i16 & 7;
+      const unsigned char* p = A.k + row_of(slot, r) * ROW + g4 * KB;
+#pragma unroll
+      for (int l = 0; l < KL; ++l) {
+        if constexpr (KB == 16) {
+          const uint4 x = *reinterpret_cast<const uint4*>(p + l * 4 * KB);
+          kr[t][l][0] = x.x; kr[t][l][1] = x.y; kr[t][l][2] = x.z; kr[t][l][3] = x.w;
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(p);
+          kr[t][l][0] = x.x; kr[t][l][1] = x.y;
+        }
+      }
+      if constexpr (QUANT) ks[t] = row_scales<D>(A.k + A.scale_off + scale_row_of(slot, r) * (D / 32));
+    }
+  };
+  auto load_v = [&](int s0) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int slot = s0 + (j < 4 ? 0 : 2) + (g4 >> 1), r = (g4 & 1) * 4 + (j & 3);
+      const unsigned char* p = A.v + row_of(slot, r) * ROW + i16 * VB;
+      if constexpr (VB == 16) {
+        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        vr[j][0] = x.x; vr[j][1] = x.y; vr[j][2] = x.z; vr[j][3] = x.w;
+      } else if constexpr (VB == 8) {
+        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        vr[j][0] = x.x; vr[j][1] = x.y;
+      } else if constexpr (VB == 4) {
+        vr[j][0] = *reinterpret_cast<const uint32_t*>(p);
+      } else {
+        vr[j][0] = *reinterpret_cast<const uint16_t*>(p);
+      }
+    }
+    if constexpr (QUANT) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {  // the scales of four rows, a whole number of words
+        const unsigned char* p = A.v + A.scale_off + scale_row_of(s0 + 2 * t + (g4 >> 1), (g4 & 1) * 4) * (D / 32);
+        if constexpr (D == 128) {
+          const uint4 x = *reinterpret_cast<const uint4*>(p);
+          vs[t][0] = x.x; vs[t][1] = x.y; vs[t][2] = x.z; vs[t][3] = x.w;
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(p);
+          vs[t][0] = x.x; vs[t][1] = x.y;
+        }
+      }
+    }
+  };
+
+  const int units = (L.count + 3) / 4, per = (units + A.splits - 1) / A.splits;
+  const int u_lo = split * per, u_hi = min(u_lo + per, units);
+  for (int u0 = u_lo; u0 < u_hi; u0 += kSlots / 4) {
+    const int u1 = min(u0 + kSlots / 4, u_hi);
+    __syncthreads();
+    for (int i = tid; i < (u1 - u0) * 4; i += kAttendThreads) {
+      const int tok = token_of(L, u0 * 4 + i), safe = tok == kNowhere ? 0 : tok;
+      s_tok[i] = tok;
+      if constexpr (PAGED) s_at[i] = (row_block<PAGED>(A.M, seq, safe) << page8) + ((safe & ((1 << A.M.page_shift) - 1)) >> 3);
+      else s_at[i] = safe;
+    }
+    __syncthreads();
+    int u = u0 + wave;
+    if (u >= u1) continue;
+    load_k((u - u0) * 4);
+    load_v((u - u0) * 4);
+    for (; u < u1; u += kAttendWaves) {
+      const int s0 = (u - u0) * 4, next = (min(u + kAttendWaves, u1 - 1) - u0) * 4;
+      f32x4_t sc[NQT][2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int nt = 0; nt < NQT; ++nt) sc[nt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+          uint4 ka;
+          const uint32_t* w = kr[t][s / STEPS];
+          if constexpr (FMT == VATT_KV_BF16) {
+            ka = make_uint4(w[0], w[1], w[2], w[3]);
+          } else {
+            // (the scale group of the columns of this load and lane; a load spans 4 lanes' 8 STEPS columns each)
+            const int group = ((s / STEPS) * 4 * STEPS * 8 + g4 * STEPS * 8 + (s % STEPS) * 8) / 32;
+            const float scale = scale_of((ks[t] >> (8 * group)) & 255u);
+            if constexpr (FMT == VATT_KV_E4M3) {
+              const uint2 x = e4m3_to_bf16(w[(s % STEPS) * 2], scale), y = e4m3_to_bf16(w[(s % STEPS) * 2 + 1], scale);
+              ka = make_uint4(x.x, x.y, y.x, y.y);
+            } else {
+              const uint32_t x = w[s % STEPS];
+              ka = make_uint4(e2m1_to_bf16<0>(x, scale), e2m1_to_bf16<1>(x, scale), e2m1_to_bf16<2>(x, scale), e2m1_to_bf16<3>(x, scale));
+            }
+          }
+#pragma unroll
+          for (int nt = 0; nt < NQT; ++nt)
+            sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka), __builtin_bit_cast(bf16x8_t, bq[nt][s]),
+                                                                sc[nt][t], 0, 0, 0);
+        }
+      }
+      load_k(next);
+      const int4 tok = *reinterpret_cast<const int4*>(&s_tok[s0]);
+      const int far = max(max(tok.x, tok.y), max(tok.z, tok.w)) + 8;
+      const bool edge = far > least;  // some column does not see all of the 32 keys
+      // tokens of this lane's result rows: 4 g + r, then 16 + 4 g + r
+      const int ta = ((g4 >> 1) ? tok.y : tok.x) + (g4 & 1) * 4, tb = ((g4 >> 1) ? tok.w : tok.z) + (g4 & 1) * 4;
+      uint4 pb[NQT][3];
+#pragma unroll
+      for (int nt = 0; nt < NQT; ++nt) {
+        float s[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = sc[nt][j >> 2][j & 3] * A.sm_scale;
+        bool ok[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ok[j] = true;
+        if (edge) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            ok[j] = (j < 4 ? ta : tb) + (j & 3) < seen[nt];
+            s[j] = ok[j] ? s[j] : -INFINITY;
+            any[nt] |= ok[j];
+          }
+        } else {
+          any[nt] = true;
+        }
+        float top = s[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
+        if (__ballot(top > mrun[nt] + kLazy)) {
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float mnew = fmaxf(mrun[nt], top);
+          const float alpha = mrun[nt] == mnew ? 1.f : __expf(mrun[nt] - mnew);
+          mrun[nt] = mnew;
+          lrun[nt] *= alpha;
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[nt][e] *= alpha;
+        }
+        const float m = mrun[nt] == -INFINITY ? 0.f : mrun[nt];  // (so far every score is -Inf: weights 0)
+        uint32_t w[3][8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          float p = __builtin_amdgcn_exp2f((s[j] - m) * kLog2e);
+          if (edge) p = ok[j] ? p : 0.f;
+          lrun[nt] += p;
+          const float r1 = p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
+          const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
+          w[0][j] = __float_as_uint(p);
+          w[1][j] = __float_as_uint(r1);
+          w[2][j] = __float_as_uint(r2);
+        }
+#pragma unroll
+        for (int x = 0; x < 3; ++x)
+          pb[nt][x] = make_uint4(upper_halves(w[x][0], w[x][1]), upper_halves(w[x][2], w[x][3]), upper_halves(w[x][4], w[x][5]),
+                                 upper_halves(w[x][6], w[x][7]));
+      }
+      float vscale[8];
+      if constexpr (QUANT) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t w = D == 128 ? vs[j >> 2][(j & 3) % (D / 32)] : vs[j >> 2][(j & 3) / 2] >> (16 * (j & 1));
+          vscale[j] = scale_of((w >> (8 * (i16 * E / 32))) & 255u);
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < E / 2; ++x) {  // columns 2 x and 2 x + 1 of the lane
+        uint32_t col[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (FMT == VATT_KV_BF16) {
+            col[j] = vr[j][x];
+          } else if constexpr (FMT == VATT_KV_E4M3) {
+            const uint2 y = e4m3_to_bf16(vr[j][x / 2], vscale[j]);
+            col[j] = (x & 1) ? y.y : y.x;
+          } else {
+            col[j] = x == 0 ? e2m1_to_bf16<0>(vr[j][0], vscale[j]) : x == 1 ? e2m1_to_bf16<1>(vr[j][0], vscale[j])
+                   : x == 2 ? e2m1_to_bf16<2>(vr[j][0], vscale[j]) : e2m1_to_bf16<3>(vr[j][0], vscale[j]);
+          }
+        }
+        if (edge) {  // (rows that nobody sees: whatever lies there has no say)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) col[j] = (j < 4 ? ta : tb) + (j & 3) < n ? col[j] : 0u;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t a[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) a[j] = h ? upper_halves(col[2 * j], col[2 * j + 1]) : lower_halves(col[2 * j], col[2 * j + 1]);
+          const uint4 va = make_uint4(a[0], a[1], a[2], a[3]);
+#pragma unroll
+          for (int nt = 0; nt < NQT; ++nt) {
+#pragma unroll
+            for (int y = 2; y >= 0; --y)
+              acc[nt][2 * x + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va), __builtin_bit_cast(bf16x8_t, pb[nt][y]),
+                                                                           acc[nt][2 * x + h], 0, 0, 0);
+          }
+        }
+      }
+      load_v(next);
+    }
+  }
+
+  // The waves' sums together, one 16-vector tile at a time, in the result layout: wave w finishes rows 4 g + w.
+#pragma unroll
+  for (int nt = 0; nt < NQT; ++nt) {
+    float l = lrun[nt];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    int saw = any[nt];
+    saw |= __shfl_xor(saw, 16);
+    saw |= __shfl_xor(saw, 32);
+    // (a piece all of whose scores are -Inf is no piece without a token)
+    const float m_own = saw && mrun[nt] == -INFINITY ? -3.0e38f : mrun[nt];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+      for (int e = 0; e < E; e += 4)
+        s_o[wave][r][e / 4][lane] = make_float4(acc[nt][e][r], acc[nt][e + 1][r], acc[nt][e + 2][r], acc[nt][e + 3][r]);
+    }
+    if (g4 == 0) {
+      s_m[wave][i16] = m_own;
+      s_l[wave][i16] = l;
+    }
+    __syncthreads();
+    float m = -INFINITY, fac[kAttendWaves];
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kAttendWaves; ++w) m = fmaxf(m, s_m[w][i16]);
+#pragma unroll
+    for (int w = 0; w < kAttendWaves; ++w) {
+      fac[w] = s_m[w][i16] == -INFINITY ? 0.f : s_m[w][i16] == m ? 1.f : __expf(s_m[w][i16] - m);
+      l += s_l[w][i16] * fac[w];
+    }
+    const int c = c_base + nt * 16 + i16;
+    if (c < vectors) {
+      const int t = t0 + c / G, g = c % G;
+      const int64_t place = (((int64_t)seq * Q + t) * A.Hq + (int64_t)kvh * G + g) * A.splits + split;
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kAttendWaves; ++w) {
+          const float4 x = s_o[w][wave][e / 4][lane];
+          o.x += x.x * fac[w];
+          o.y += x.y * fac[w];
+          o.z += x.z * fac[w];
+          o.w += x.w * fac[w];
+        }
+        *reinterpret_cast<float4*>(A.part + place * D + E * (4 * g4 + wave) + e) = o;
+      }
+      if (wave == 0 && g4 == 0) A.part_ml[place] = make_float2(m, l);
+    }
+  }
+}
+
+// The tokens of one list again for one head, by the whole workgroup: dot products, every row only where it is seen.
+template <int D, int FMT, bool PAGED>
+__device__ __forceinline__ void attend_again(const AttendArgs& A, int64_t vb, int h, int seq, int kvh, const TokenList& L, float (&s_acc)[kAttendWaves][D],
+                                             float (&s_m)[kAttendWaves], float (&s_l)[kAttendWaves]) {
+  constexpr int LPR = D / 8, RPW = kWave / LPR;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane % LPR, rsub = lane / LPR;
+  const uint4 qv = *reinterpret_cast<const uint4*>(A.q + (vb * A.Hq + h) * D + sub * 8);
+  const uint32_t qw[4] = {qv.x, qv.y, qv.z, qv.w};
+  float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int64_t i = wave * RPW + rsub; i < (int64_t)L.count * 8; i += kAttendWaves * RPW) {
+    const int tok = token_of(L, (int)(i >> 3)) + (int)(i & 7);
+    if (tok >= L.n) continue;
+    const RowAt at = row_at<PAGED>(A.M, seq, kvh, tok, row_block<PAGED>(A.M, seq, tok));
+    uint4 x[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const unsigned char* buf = y ? A.v : A.k;
+      uint32_t byte = 0;
+      if constexpr (FMT != VATT_KV_BF16) byte = buf[A.scale_off + at.scales * (D / 32) + sub / 4];
+      x[y] = chunk_bf16<FMT>(load_chunk<FMT>(buf + at.row * kRowBytes<FMT, D> + sub * (kRowBytes<FMT, D> / LPR)), byte);
+    }
+    const uint32_t kw[4] = {x[0].x, x[0].y, x[0].z, x[0].w}, vw[4] = {x[1].x, x[1].y, x[1].z, x[1].w};
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s += bf16_lo(kw[j]) * bf16_lo(qw[j]) + bf16_hi(kw[j]) * bf16_hi(qw[j]);
+    s = group_sum<LPR>(s) * A.sm_scale;
+    const float mnew = fmaxf(m, s), shift = mnew == -INFINITY ? -3.0e38f : mnew;
+    const float alpha = m == -INFINITY ? 0.f : m == shift ? 1.f : __expf(m - shift);
+    const float p = __expf(s - shift);
+    m = shift;
+    l = l * alpha + p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      acc[2 * j] = acc[2 * j] * alpha + p * bf16_lo(vw[j]);
+      acc[2 * j + 1] = acc[2 * j + 1] * alpha + p * bf16_hi(vw[j]);
+    }
+  }
+  float all = m;
+#pragma unroll
+  for (int o = LPR; o < kWave; o <<= 1) all = fmaxf(all, __shfl_xor(all, o));
+  const float f = m == -INFINITY ? 0.f : m == all ? 1.f : __expf(m - all);
+  l = f == 0.f ? 0.f : l * f;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) acc[c] = f == 0.f ? 0.f : acc[c] * f;
+#pragma unroll
+  for (int o = LPR; o < kWave; o <<= 1) {
+    l += __shfl_xor(l, o);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[c] += __shfl_xor(acc[c], o);
+  }
+  __syncthreads();
+  if (rsub == 0) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) s_acc[wave][sub * 8 + c] = acc[c];
+  }
+  if (lane == 0) {
+    s_m[wave] = all;
+    s_l[wave] = l;
+  }
+  __syncthreads();
+}
+
+// Merge of a head's partial sums.  A result with an Inf or a NaN is worked out again: the second product of attend_kernel gives every
+// column every V row of a step, with weight 0 where the column does not see the token, and in three terms of which some are 0, so that a
+// row with an Inf or a NaN makes a NaN where it has no say.
+template <int D, int FMT, bool PAGED>
+__global__ __launch_bounds__(kAttendThreads) void attend_merge_kernel(AttendArgs A) {
+  __shared__ float s_acc[kAttendWaves][D], s_m[kAttendWaves], s_l[kAttendWaves];
+  const int h = blockIdx.x, tid = threadIdx.x, c = tid % D;
+  const int64_t vb = blockIdx.y, head = vb * A.Hq + h;
+  const float2* ml = A.part_ml + head * A.splits;
+  float m = -INFINITY, l = 0.f, a = 0.f;
+  for (int s = 0; s < A.splits; ++s) m = fmaxf(m, ml[s].x);
+  for (int s = 0; s < A.splits; ++s) {
+    const float2 x = ml[s];
+    if (x.x == -INFINITY) continue;
+    const float w = x.x == m ? 1.f : __expf(x.x - m);
+    l += x.y * w;
+    a += A.part[(head * A.splits + s) * D + c] * w;
+  }
+  if (__syncthreads_or(!(fabsf(a) < INFINITY) || !(l < INFINITY))) {
+    const int kvh = h / (A.Hq / A.Hkv), seq = seq_of_pair((int)vb, A.q_len), t = (int)vb - seq * A.q_len;
+    const int n = max(min(max(A.seq_lens[seq], 1), A.M.n_max) - (A.q_len - 1 - t), 1);
+    attend_again<D, FMT, PAGED>(A, vb, h, seq, kvh, token_list(A, (int)vb, kvh, n), s_acc, s_m, s_l);
+    m = s_m[0];
+    for (int w = 1; w < kAttendWaves; ++w) m = fmaxf(m, s_m[w]);
+    l = a = 0.f;
+    for (int w = 0; w < kAttendWaves; ++w) {
+      if (s_m[w] == -INFINITY) continue;
+      const float f = s_m[w] == m ? 1.f : __expf(s_m[w] - m);
+      l += s_l[w] * f;
+      a += s_acc[w][c] * f;
+    }
+  }
+  if (tid < D) {
+    A.out_o[head * D + c] = m == -INFINITY ? 0.f : a / l;
+    if (tid == 0 && A.out_lse) A.out_lse[head] = m == -INFINITY ? -INFINITY : m + logf(l);
+  }
+}
+
+template <int D, int FMT, bool PAGED>
+hipError_t launch_attend_f(const Plan& pl, const AttendArgs& A, hipStream_t st) {
+  const int vectors = A.blocks ? pl.group : pl.group * pl.q_len;
+  const dim3 grid(A.Hkv, A.splits * A.rounds, A.blocks ? pl.vbatch : pl.p.batch);
+  if (vectors <= 16) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, 1>), grid, dim3(kAttendThreads), 0, st, A);
+  else hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, 2>), grid, dim3(kAttendThreads), 0, st, A);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((attend_merge_kernel<D, FMT, PAGED>), dim3(A.Hq, pl.vbatch), dim3(kAttendThreads), 0, st, A);
+  return hipGetLastError();
+}
+template <int D, int FMT>
+hipError_t launch_attend_d(const Plan& pl, const AttendArgs& A, hipStream_t st) {
+  return pl.p.kv_layout == VATT_LAYOUT_PAGED ? launch_attend_f<D, FMT, true>(pl, A, st) : launch_attend_f<D, FMT, false>(pl, A, st);
+}
+template <int D>
+hipError_t launch_attend_p(const Plan& pl, const AttendArgs& A, hipStream_t st) {
+  if (pl.kv_format == VATT_KV_E4M3) return launch_attend_d<D, VATT_KV_E4M3>(pl, A, st);
+  if (pl.kv_format == VATT_KV_E2M1) return launch_attend_d<D, VATT_KV_E2M1>(pl, A, st);
+  return launch_attend_d<D, VATT_KV_BF16>(pl, A, st);
+}
+
+}  // namespace
+
+hipError_t launch_attend(const Plan& pl, const void* q, const void* k, const void* v, const int32_t* block_table,
+                         const int32_t* seq_lens, const int32_t* blocks, const int32_t* block_count, void* ws, float* out_o,
+                         float* out_lse, hipStream_t st) {
+  AttendArgs A = {};
+  A.q = static_cast<const uint16_t*>(q);
+  A.k = static_cast<const unsigned char*>(k);
+  A.v = static_cast<const unsigned char*>(v);
+  A.scale_off = (int64_t)kv_scale_offset(pl);
+  A.seq_lens = seq_lens;
+  A.blocks = blocks;
+  A.block_count = block_count;
+  A.out_o = out_o;
+  A.out_lse = out_lse;
+  A.M = row_map(pl, block_table);
+  A.Hq = pl.p.n_q_heads;
+  A.Hkv = pl.p.n_kv_heads;
+  A.q_len = pl.q_len;
+  A.capacity = block_list_capacity(pl);
+  A.block_shift = pl.block_tokens ? 31 - __builtin_clz(pl.block_tokens) : 0;
+  A.sm_scale = pl.sm_scale;
+  const int vectors = blocks ? pl.group : pl.group * pl.q_len;
+  A.rounds = vectors <= 16 ? 1 : (vectors + 31) / 32;
+  // Four workgroups per CU in all, none with less than a unit of keys per wave at the longest; the partial sums fit the workspace.
+  const int64_t rows = (int64_t)pl.vbatch * A.Hq, jobs = (int64_t)(blocks ? pl.vbatch : pl.p.batch) * A.Hkv * A.rounds;
+  const int64_t longest = blocks ? (int64_t)A.capacity * pl.block_tokens : pl.p.n_max;
+  int64_t splits = std::min<int64_t>((4 * pl.num_cus + jobs - 1) / jobs, (longest + kUnit * kAttendWaves - 1) / (kUnit * kAttendWaves));
+  splits = std::min<int64_t>({splits, 128, (int64_t)(pl.ws_bytes / (rows * (pl.p.head_dim + 2) * sizeof(float)))});
+  A.splits = (int)std::max<int64_t>(splits, 1);
+  A.part = static_cast<float*>(ws);
+  A.part_ml = reinterpret_cast<float2*>(A.part + rows * A.splits * pl.p.head_dim);
+  return pl.p.head_dim == 128 ? launch_attend_p<128>(pl, A, st) : launch_attend_p<64>(pl, A, st);
+}
+
+}  // namespace vatt

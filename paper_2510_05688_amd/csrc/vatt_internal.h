@@ -110,6 +110,10 @@ struct Plan {
   int prework;                    // the sampler streams' first batches are made by workgroups of the score launch
   int fuse_splits;                // > 0: the selection kernel also gathers, with this many workgroups per head
   int cache_slots;                // slots per (sequence, KV head) of the random cache of base-sample rows
+  int kv_format;                  // VATT_KV_*
+  int block_tokens;               // tokens per block of the block calls (0: pages are too small for them)
+  int rotary_dim, rotary_pairs;   // rotated columns (0: none); pairs of neighbours instead of halves
+  double rotary_attention, rotary_freq[64];
   // workspace offsets (bytes)
   size_t off_scores, off_sub_max, off_sparse, off_head_rec, off_gather_part,
       off_debug, off_vstat_part, off_dense_part, off_pre_tok, off_pre_flags, off_base_slot, ws_bytes;
@@ -160,6 +164,12 @@ inline double* fixed_sums_of(const Plan& pl, void* ws) { return reinterpret_cast
 // what else passes through it.
 inline size_t score_bytes(const Plan& pl) { return (size_t)pl.vbatch * pl.p.n_q_heads * pl.p.n_max * sizeof(float); }
 constexpr size_t kScoreBytesLarge = 32000000;
+
+inline size_t kv_row_bytes(const Plan& pl) {
+  return pl.kv_format == VATT_KV_BF16 ? 2 * (size_t)pl.p.head_dim : pl.kv_format == VATT_KV_E4M3 ? pl.p.head_dim : pl.p.head_dim / 2;
+}
+size_t kv_scale_offset(const Plan& pl);  // bytes of all rows' codes, up to the scales (if any)
+int block_list_capacity(const Plan& pl);
 
 // Every launcher returns a hipError_t from hipGetLastError() after the launch.
 // seq_seeds: needed (may be nullptr otherwise) when score_prework(pl)
@@ -238,6 +248,20 @@ hipError_t launch_dense(const Plan& pl, const void* q, const void* k, const void
                         const int32_t* seq_lens, void* ws, float* out_o, float* out_lse, hipStream_t st);
 hipError_t launch_append(const Plan& pl, const void* k_new, const void* v_new, void* k, void* v,
                          const int32_t* block_table, int32_t* seq_lens, hipStream_t st);
+// The cache's rows in the plan's format, and blocks of them (vatt_write_kv and what follows it in vatt.h).
+hipError_t launch_write(const Plan& pl, const void* q, const void* k_new, const void* v_new, int64_t q_stride, int64_t k_stride,
+                        int64_t v_stride, int n_new, const int32_t* first, const int32_t* new_lens, void* k, void* v,
+                        const int32_t* block_table, void* summary, void* out_q, int32_t* out_lens, hipStream_t st);
+hipError_t launch_block_summary(const Plan& pl, const void* k, const int32_t* block_table, const int32_t* seq_lens, void* summary,
+                                hipStream_t st);
+hipError_t launch_read(const Plan& pl, const void* k, const void* v, const int32_t* block_table, const int32_t* seq_lens,
+                       const int32_t* first, int n_rows, void* out_k, void* out_v, hipStream_t st);
+hipError_t launch_select_blocks(const Plan& pl, const void* q, const void* summary, const int32_t* block_table, const int32_t* seq_lens,
+                                void* ws, int32_t* out_blocks, int32_t* out_count, int32_t* topk_idx, int32_t* topk_cnt, hipStream_t st);
+// blocks == nullptr: all tokens of every sequence
+hipError_t launch_attend(const Plan& pl, const void* q, const void* k, const void* v, const int32_t* block_table,
+                         const int32_t* seq_lens, const int32_t* blocks, const int32_t* block_count, void* ws, float* out_o,
+                         float* out_lse, hipStream_t st);
 hipError_t set_kernel_attributes(const Plan& pl);        // every selection kernel: dynamic LDS limit
 hipError_t set_budget_kernel_attributes();
 hipError_t set_given_kernel_attributes(const Plan& pl);  // (its part for the caller-supplied-top-k kernels)

@@ -1,0 +1,438 @@
+// New rows into the cache (rotated, in the cache's format, with the summaries of the blocks they touch), and rows of it back.
+#include <algorithm>
+#include <type_traits>
+
+#include "vatt_format.h"
+
+namespace vatt {
+namespace {
+
+constexpr int kWriteThreads = 256;
+
+struct WriteArgs {
+  const uint16_t* q;
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t* first;
+  const int32_t* new_lens;
+  unsigned char* k;
+  unsigned char* v;
+  int64_t scale_off;
+  uint16_t* summary;
+  uint16_t* out_q;
+  int32_t* out_lens;
+  RowMap M;
+  int n_new, Hq, Hkv;
+  int block_shift, head_blocks;  // tokens per block; blocks per KV head of a sequence (contiguous) or of a page
+  int k_jobs, k_groups, k_heads;       // workgroups with summaries per sequence, groups of KV heads, and KV heads of one
+  int row_groups, row_passes, row_tokens_shift;  // the other rows: groups of heads, passes of a workgroup, tokens of one
+  int rot, pairs;
+  double attention;
+  double freq[64];
+};
+
+// sin and cos of a >= 0 in 64 bits, rounded to 32 with a factor: a minus the nearest multiple of pi / 2 (pi / 2 in two parts, so that the
+// difference is right to 2^-60 of a), then the Taylor series to x^13 and x^12, whose next terms are below 2^-36 for |x| <= pi / 4.
+__device__ __forceinline__ float2 turn(double a, double factor) {
+  const double k = rint(a * 0.63661977236758134308);
+  const double x = fma(-k, 6.123233995736766036e-17, fma(-k, 1.57079632679489661923, a));
+  const double x2 = x * x;
+  double s = fma(x2, 1.0 / 6227020800.0, -1.0 / 39916800.0);
+  s = fma(x2, s, 1.0 / 362880.0);
+  s = fma(x2, s, -1.0 / 5040.0);
+  s = fma(x2, s, 1.0 / 120.0);
+  s = fma(x2, s, -1.0 / 6.0);
+  s = fma(x * x2, s, x);
+  double c = fma(x2, 1.0 / 479001600.0, -1.0 / 3628800.0);
+  c = fma(x2, c, 1.0 / 40320.0);
+  c = fma(x2, c, -1.0 / 720.0);
+  c = fma(x2, c, 1.0 / 24.0);
+  c = fma(x2, c, -0.5);
+  c = fma(x2, c, 1.0);
+  const int quarter = (int)k & 3;
+  const double cs = (quarter & 1) ? s : c, sn = (quarter & 1) ? c : s;
+  return make_float2((float)(factor * ((quarter == 1 || quarter == 2) ? -cs : cs)), (float)(factor * (quarter >= 2 ? -sn : sn)));
+}
+
+// (cos, sin) of the pairs of the positions from `base` on, `tokens` of them, as far as they lie in [first, end); by the whole
+// workgroup, to be followed by a barrier.
+template <int D>
+__device__ __forceinline__ void make_turns(const WriteArgs& A, float2 (*turns)[D / 2], int base, int tokens, int first, int end) {
+  for (int x = threadIdx.x; x < tokens * (D / 2); x += kWriteThreads) {
+    const int i = x % (D / 2), t = x / (D / 2);
+    if (i < A.rot / 2 && base + t >= first && base + t < end) turns[t][i] = turn((double)(base + t) * A.freq[i], A.attention);
+  }
+}
+
+// Columns 8 c .. 8 c + 7 of a row, and the columns that they are rotated with.
+struct RowPart {
+  uint4 own, other;
+};
+__device__ __forceinline__ RowPart load_part(const WriteArgs& A, const uint16_t* row, int c, bool rotate) {
+  RowPart x;
+  x.own = x.other = *reinterpret_cast<const uint4*>(row + 8 * c);
+  const int half = A.rot / 2;
+  if (rotate && !A.pairs && 8 * c < A.rot) x.other = *reinterpret_cast<const uint4*>(row + (8 * c < half ? 8 * c + half : 8 * c - half));
+  return x;
+}
+__device__ __forceinline__ void rotated(const WriteArgs& A, const RowPart& x, int c, bool rotate, const float2* turns, float (&y)[8]) {
+  const uint32_t w[4] = {x.own.x, x.own.y, x.own.z, x.own.w}, o[4] = {x.other.x, x.other.y, x.other.z, x.other.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[2 * i] = bf16_lo(w[i]);
+    y[2 * i + 1] = bf16_hi(w[i]);
+  }
+  if (!rotate || 8 * c >= A.rot) return;
+  if (A.pairs) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 t = turns[4 * c + i];
+      const float a = y[2 * i], b = y[2 * i + 1];
+      y[2 * i] = a * t.x - b * t.y;
+      y[2 * i + 1] = b * t.x + a * t.y;
+    }
+  } else {
+    const int half = A.rot / 2;
+    const bool lower = 8 * c < half;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 t = turns[(lower ? 8 * c : 8 * c - half) + i];
+      const float z = (i & 1) ? bf16_hi(o[i / 2]) : bf16_lo(o[i / 2]);
+      y[i] = y[i] * t.x + (lower ? -z : z) * t.y;
+    }
+  }
+}
+
+__device__ __forceinline__ uint4 packed(const float (&y)[8]) {
+  return make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+}
+
+// Columns 8 c .. of a row of K or V to the cache; what they stand for there comes back in bf16.  (All four lanes of a quad that share a
+// scale are in the same row.)
+template <int D, int FMT>
+__device__ __forceinline__ uint4 store_row(unsigned char* buf, int64_t scale_off, const RowAt& at, int c, const float (&y)[8]) {
+  unsigned char* dst = buf + at.row * kRowBytes<FMT, D> + c * (kRowBytes<FMT, D> / (D / 8));
+  if constexpr (FMT == VATT_KV_BF16) {
+    const uint4 x = packed(y);
+    *reinterpret_cast<uint4*>(dst) = x;
+    return x;
+  } else {
+    uint32_t byte;
+    const Chunk<FMT> x = quantise<FMT>(y, byte);
+    store_chunk<FMT>(dst, x);
+    if ((c & 3) == 0) buf[scale_off + at.scales * (D / 32) + c / 4] = (unsigned char)byte;
+    return chunk_bf16<FMT>(x, byte);
+  }
+}
+
+// The larger (smaller) of two values; NaN where one is.
+__device__ __forceinline__ float top_of(float a, float b) { return (a > b || a != a) ? a : b; }
+__device__ __forceinline__ float low_of(float a, float b) { return (a < b || a != a) ? a : b; }
+
+// Summaries of the blocks of one tile of KV head kvh, whose new rows (from position `first` on; none with FILL) are written on the way.
+// One lane per 8 columns, D / 8 lanes per row, every row of a pass of kWriteThreads / (D / 8) tokens from tile_lo on.
+// The old rows of a block that is only begun are read again rather than taken from its summary: it then follows from the cache alone, also
+// after a sequence was cut back.  That is up to 15 rows with blocks of 16, beside the row written.
+template <int D, int FMT, bool PAGED, bool FILL>
+__device__ __forceinline__ void summary_tile(const WriteArgs& A, int b, int kvh, int tile_lo, int tile, int first, int end,
+                                             float2 (*turns)[D / 2], bool turns_made, float (*s_ends)[2][D]) {
+  constexpr int LPR = D / 8, TT = kWriteThreads / LPR, WAVES = kWriteThreads / kWave;
+  const int tid = threadIdx.x, c = tid % LPR, r = tid / LPR, lane = tid & 63, wave = tid >> 6;
+  const int bs = 1 << A.block_shift;
+  float top[8], low[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    top[i] = -INFINITY;
+    low[i] = INFINITY;
+  }
+  for (int p = 0; p < tile; p += TT) {
+    const int tok = tile_lo + p + r;
+    const bool fresh = !FILL && tok >= first;
+    RowAt at;
+    RowPart part;
+    Chunk<FMT> code;
+    uint32_t byte = 0;
+    if (tok < end) {
+      if (fresh) part = load_part(A, A.k_new + ((int64_t)b * A.n_new + (tok - first)) * A.k_stride + kvh * D, c, A.rot > 0);
+      at = row_at<PAGED>(A.M, b, kvh, tok, row_block<PAGED>(A.M, b, tok));
+      if (!fresh) {
+        code = load_chunk<FMT>(A.k + at.row * kRowBytes<FMT, D> + c * (kRowBytes<FMT, D> / LPR));
+        if constexpr (FMT != VATT_KV_BF16) byte = A.k[A.scale_off + at.scales * (D / 32) + c / 4];
+      }
+    }
+    if (!FILL && A.rot > 0 && !(turns_made && p == 0)) {
+      if (p > 0 || turns_made) __syncthreads();
+      make_turns<D>(A, turns, tile_lo + p, TT, first, end);
+      __syncthreads();
+    }
+    if (tok < end) {
+      uint4 x;
+      if (fresh) {
+        float y[8];
+        rotated(A, part, c, A.rot > 0, turns[r], y);
+        x = store_row<D, FMT>(A.k, A.scale_off, at, c, y);
+      } else {
+        x = chunk_bf16<FMT>(code, byte);
+      }
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float z = (i & 1) ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+        top[i] = top_of(z, top[i]);
+        low[i] = low_of(z, low[i]);
+      }
+    }
+    if ((p + TT) % bs != 0 && bs > TT) continue;  // the block goes on
+    // (a wave's rows belong to one block)
+#pragma unroll
+    for (int o = LPR; o < kWave; o <<= 1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        top[i] = top_of(__shfl_xor(top[i], o), top[i]);
+        low[i] = low_of(__shfl_xor(low[i], o), low[i]);
+      }
+    }
+    if (lane < LPR) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        s_ends[wave][0][8 * c + i] = top[i];
+        s_ends[wave][1][8 * c + i] = low[i];
+      }
+    }
+    __syncthreads();
+    const int blocks = bs < TT ? TT / bs : 1, per = WAVES / blocks;
+    if (tid < blocks * 2 * LPR) {
+      const int which = (tid / LPR) & 1, k = tid / (2 * LPR);
+      const int lo = bs <= TT ? tile_lo + p + k * bs : tile_lo + p + TT - bs;
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        y[i] = s_ends[k * per][which][8 * c + i];
+        for (int w = 1; w < per; ++w) {
+          const float z = s_ends[k * per + w][which][8 * c + i];
+          y[i] = which == 0 ? top_of(z, y[i]) : low_of(z, y[i]);
+        }
+      }
+      if (lo < end && lo + bs > first) {
+        int64_t place;
+        if constexpr (PAGED)
+          place = ((int64_t)row_block<PAGED>(A.M, b, lo) * A.Hkv + kvh) * A.head_blocks + ((lo >> A.block_shift) & (A.head_blocks - 1));
+        else
+          place = ((int64_t)b * A.Hkv + kvh) * A.head_blocks + (lo >> A.block_shift);
+        *reinterpret_cast<uint4*>(A.summary + (place * 2 + which) * D + 8 * c) = packed(y);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      top[i] = -INFINITY;
+      low[i] = INFINITY;
+    }
+  }
+}
+
+// One launch for everything a write does.  The first k_jobs workgroups of a sequence each take a tile of whole blocks of some KV
+// heads' K rows, with their summaries; the others take the remaining rows (q, V, and K without summaries), tokens of a tile times heads.
+template <int D, int FMT, bool PAGED>
+__global__ __launch_bounds__(kWriteThreads) void write_kernel(WriteArgs A) {
+  constexpr int LPR = D / 8, TT = kWriteThreads / LPR;
+  __shared__ float2 turns[TT][D / 2];
+  __shared__ float s_ends[kWriteThreads / kWave][2][D];
+  const int b = blockIdx.y, tid = threadIdx.x, c = tid % LPR, r = tid / LPR;
+  const int first = A.first[b];
+  int end = first;
+  if (first >= 0 && first < A.M.n_max) end = min(first + (A.new_lens ? min(max(A.new_lens[b], 0), A.n_new) : A.n_new), A.M.n_max);
+  if (blockIdx.x == 0 && tid == 0 && A.out_lens) A.out_lens[b] = end;
+  if (end <= first) return;
+  int x = blockIdx.x;
+  if (x < A.k_jobs) {
+    const int tile = max(1 << A.block_shift, TT), at = x / A.k_groups, group = x - at * A.k_groups;
+    const int tile_lo = (first / tile + at) * tile;
+    if (tile_lo >= end) return;
+    for (int h = 0; h < A.k_heads && group * A.k_heads + h < A.Hkv; ++h)
+      summary_tile<D, FMT, PAGED, false>(A, b, group * A.k_heads + h, tile_lo, tile, first, end, turns, h > 0 && tile == TT, s_ends);
+    return;
+  }
+  x -= A.k_jobs;
+  const int at = x / A.row_groups, group = x - at * A.row_groups;
+  const int tokens = 1 << A.row_tokens_shift, per_pass = TT >> A.row_tokens_shift;
+  const int j0 = at << A.row_tokens_shift, t = r & (tokens - 1);
+  if (first + j0 >= end) return;
+  const int n_q = A.out_q ? A.Hq : 0, n_k = A.k_jobs ? 0 : A.Hkv, heads = n_q + n_k + A.Hkv;
+  const int h0 = group * A.row_passes * per_pass;
+  if (A.rot > 0 && h0 < n_q + n_k) {
+    make_turns<D>(A, turns, first + j0, tokens, first, end);
+    __syncthreads();
+  }
+  const int tok = first + j0 + t;
+  if (tok >= end) return;
+  const int blk = row_block<PAGED>(A.M, b, tok);
+  const int64_t src_row = (int64_t)b * A.n_new + j0 + t;
+  for (int p = 0; p < A.row_passes; ++p) {
+    const int h = h0 + p * per_pass + (r >> A.row_tokens_shift);
+    if (h >= heads) return;
+    float y[8];
+    if (h < n_q) {
+      const RowPart part = load_part(A, A.q + src_row * A.q_stride + h * D, c, true);
+      rotated(A, part, c, true, turns[t], y);
+      *reinterpret_cast<uint4*>(A.out_q + (src_row * A.Hq + h) * D + 8 * c) = packed(y);
+    } else {
+      const bool is_k = h < n_q + n_k;
+      const int kvh = is_k ? h - n_q : h - n_q - n_k;
+      const RowPart part = load_part(A, (is_k ? A.k_new + src_row * A.k_stride : A.v_new + src_row * A.v_stride) + kvh * D, c, is_k && A.rot > 0);
+      rotated(A, part, c, is_k && A.rot > 0, turns[t], y);
+      store_row<D, FMT>(is_k ? A.k : A.v, A.scale_off, row_at<PAGED>(A.M, b, kvh, tok, blk), c, y);
+    }
+  }
+}
+
+template <int D, int FMT, bool PAGED>
+__global__ __launch_bounds__(kWriteThreads) void summary_kernel(WriteArgs A) {
+  constexpr int TT = kWriteThreads / (D / 8);
+  __shared__ float s_ends[kWriteThreads / kWave][2][D];
+  const int b = blockIdx.y, tile = max(1 << A.block_shift, TT);
+  const int at = blockIdx.x / A.Hkv, kvh = blockIdx.x - at * A.Hkv;
+  const int end = min(max(A.first[b], 0), A.M.n_max);
+  if (at * tile >= end) return;
+  summary_tile<D, FMT, PAGED, true>(A, b, kvh, at * tile, tile, 0, end, nullptr, false, s_ends);
+}
+
+struct ReadArgs {
+  const unsigned char* buf[2];
+  uint16_t* out[2];
+  int64_t scale_off;
+  const int32_t* seq_lens;
+  const int32_t* first;
+  RowMap M;
+  int n_rows;
+};
+
+// One lane per 8 columns of a row.
+template <int D, int FMT, bool PAGED>
+__global__ __launch_bounds__(kWriteThreads) void read_kernel(ReadArgs A) {
+  constexpr int LPR = D / 8, TT = kWriteThreads / LPR;
+  const int b = blockIdx.y, tid = threadIdx.x, c = tid % LPR, r = tid / LPR;
+  const int at = blockIdx.x / A.M.Hkv, kvh = blockIdx.x - at * A.M.Hkv;
+  const int first = A.first ? max(A.first[b], 0) : 0, end = min(max(A.seq_lens[b], 0), A.M.n_max);
+  const int j = at * TT + r;
+  if (j >= A.n_rows || first >= end || j >= end - first) return;
+  const unsigned char* buf = A.buf[blockIdx.z];
+  const RowAt row = row_at<PAGED>(A.M, b, kvh, first + j, row_block<PAGED>(A.M, b, first + j));
+  uint32_t byte = 0;
+  if constexpr (FMT != VATT_KV_BF16) byte = buf[A.scale_off + row.scales * (D / 32) + c / 4];
+  const Chunk<FMT> code = load_chunk<FMT>(buf + row.row * kRowBytes<FMT, D> + c * (kRowBytes<FMT, D> / LPR));
+  *reinterpret_cast<uint4*>(A.out[blockIdx.z] + (((int64_t)b * A.M.Hkv + kvh) * A.n_rows + j) * D + 8 * c) = chunk_bf16<FMT>(code, byte);
+}
+
+// Calls f with the plan's head_dim, format and layout as constants.
+template <class F>
+hipError_t with_format(const Plan& pl, F f) {
+  auto layout = [&](auto d, auto fmt) {
+    return pl.p.kv_layout == VATT_LAYOUT_PAGED ? f(d, fmt, std::true_type{}) : f(d, fmt, std::false_type{});
+  };
+  auto format = [&](auto d) {
+    if (pl.kv_format == VATT_KV_E4M3) return layout(d, std::integral_constant<int, VATT_KV_E4M3>{});
+    if (pl.kv_format == VATT_KV_E2M1) return layout(d, std::integral_constant<int, VATT_KV_E2M1>{});
+    return layout(d, std::integral_constant<int, VATT_KV_BF16>{});
+  };
+  return pl.p.head_dim == 128 ? format(std::integral_constant<int, 128>{}) : format(std::integral_constant<int, 64>{});
+}
+
+void set_blocks(const Plan& pl, WriteArgs& A) {
+  A.block_shift = 31 - __builtin_clz(pl.block_tokens);
+  A.head_blocks = pl.p.kv_layout == VATT_LAYOUT_PAGED ? pl.p.page_size / pl.block_tokens : (pl.p.n_max + pl.block_tokens - 1) / pl.block_tokens;
+}
+
+}  // namespace
+
+hipError_t launch_write(const Plan& pl, const void* q, const void* k_new, const void* v_new, int64_t q_stride, int64_t k_stride,
+                        int64_t v_stride, int n_new, const int32_t* first, const int32_t* new_lens, void* k, void* v,
+                        const int32_t* block_table, void* summary, void* out_q, int32_t* out_lens, hipStream_t st) {
+  WriteArgs A = {};
+  A.q = static_cast<const uint16_t*>(q);
+  A.k_new = static_cast<const uint16_t*>(k_new);
+  A.v_new = static_cast<const uint16_t*>(v_new);
+  A.q_stride = q_stride;
+  A.k_stride = k_stride;
+  A.v_stride = v_stride;
+  A.first = first;
+  A.new_lens = new_lens;
+  A.k = static_cast<unsigned char*>(k);
+  A.v = static_cast<unsigned char*>(v);
+  A.scale_off = (int64_t)kv_scale_offset(pl);
+  A.summary = static_cast<uint16_t*>(summary);
+  A.out_q = static_cast<uint16_t*>(out_q);
+  A.out_lens = out_lens;
+  A.M = row_map(pl, block_table);
+  A.n_new = n_new;
+  A.Hq = pl.p.n_q_heads;
+  A.Hkv = pl.p.n_kv_heads;
+  A.rot = pl.rotary_dim;
+  A.pairs = pl.rotary_pairs;
+  A.attention = pl.rotary_attention;
+  std::copy(pl.rotary_freq, pl.rotary_freq + 64, A.freq);
+  const int tokens = kWriteThreads / (pl.p.head_dim / 8), batch = pl.p.batch;
+  if (summary) {
+    set_blocks(pl, A);
+    const int tile = std::max(pl.block_tokens, tokens), tiles = (n_new + tile - 2) / tile + 1;
+    A.k_heads = std::max(1, std::min({8, A.Hkv, (int)((int64_t)batch * tiles * A.Hkv / (8 * pl.num_cus))}));
+    A.k_groups = (A.Hkv + A.k_heads - 1) / A.k_heads;
+    A.k_jobs = tiles * A.k_groups;
+  }
+  while ((1 << A.row_tokens_shift) < std::min(n_new, tokens)) ++A.row_tokens_shift;
+  const int heads = (out_q ? A.Hq : 0) + (summary ? 0 : A.Hkv) + A.Hkv, per_pass = tokens >> A.row_tokens_shift;
+  const int passes = (heads + per_pass - 1) / per_pass, tiles = (n_new + (1 << A.row_tokens_shift) - 1) >> A.row_tokens_shift;
+  A.row_passes = std::max(1, std::min({8, passes, (int)((int64_t)batch * tiles * passes / (8 * pl.num_cus))}));
+  A.row_groups = (passes + A.row_passes - 1) / A.row_passes;
+  const dim3 grid(A.k_jobs + tiles * A.row_groups, batch);
+  return with_format(pl, [&](auto d, auto fmt, auto paged) {
+    hipLaunchKernelGGL((write_kernel<d(), fmt(), paged()>), grid, dim3(kWriteThreads), 0, st, A);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_block_summary(const Plan& pl, const void* k, const int32_t* block_table, const int32_t* seq_lens, void* summary,
+                                hipStream_t st) {
+  WriteArgs A = {};
+  A.k = static_cast<unsigned char*>(const_cast<void*>(k));
+  A.first = seq_lens;
+  A.scale_off = (int64_t)kv_scale_offset(pl);
+  A.summary = static_cast<uint16_t*>(summary);
+  A.M = row_map(pl, block_table);
+  A.Hkv = pl.p.n_kv_heads;
+  set_blocks(pl, A);
+  const int tile = std::max(pl.block_tokens, kWriteThreads / (pl.p.head_dim / 8));
+  const dim3 grid((pl.p.n_max + tile - 1) / tile * A.Hkv, pl.p.batch);
+  return with_format(pl, [&](auto d, auto fmt, auto paged) {
+    hipLaunchKernelGGL((summary_kernel<d(), fmt(), paged()>), grid, dim3(kWriteThreads), 0, st, A);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_read(const Plan& pl, const void* k, const void* v, const int32_t* block_table, const int32_t* seq_lens,
+                       const int32_t* first, int n_rows, void* out_k, void* out_v, hipStream_t st) {
+  ReadArgs A = {};
+  int n = 0;
+  if (out_k) {
+    A.buf[n] = static_cast<const unsigned char*>(k);
+    A.out[n++] = static_cast<uint16_t*>(out_k);
+  }
+  if (out_v) {
+    A.buf[n] = static_cast<const unsigned char*>(v);
+    A.out[n++] = static_cast<uint16_t*>(out_v);
+  }
+  A.scale_off = (int64_t)kv_scale_offset(pl);
+  A.seq_lens = seq_lens;
+  A.first = first;
+  A.M = row_map(pl, block_table);
+  A.n_rows = n_rows;
+  const int tokens = kWriteThreads / (pl.p.head_dim / 8);
+  const dim3 grid((n_rows + tokens - 1) / tokens * A.M.Hkv, pl.p.batch, n);
+  return with_format(pl, [&](auto d, auto fmt, auto paged) {
+    hipLaunchKernelGGL((read_kernel<d(), fmt(), paged()>), grid, dim3(kWriteThreads), 0, st, A);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace vatt

@@ -1,0 +1,729 @@
+"""The cache operators against their 64-bit oracle: written rows and summaries, rows read back, blocks chosen, attention over blocks and
+over quantised caches, and all of them in a row as a serving loop calls them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_ops as co
+
+pytestmark = pytest.mark.gpu
+
+HALF_BF16 = 2.0 ** -8  # half a step of bf16, relative to the value
+
+
+def _bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(torch.bfloat16).cuda()
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+class Setup:
+    """A plan, a cache with arbitrary contents, and its rows as the oracle sees them."""
+
+    def __init__(self, batch=2, hq=4, hkv=2, d=128, n_max=100, page=0, fmt=0, block=None, q_len=1, rotary=None, seed=0, **over):
+        from paper_2510_05688_amd import binding as vb
+        self.vb, self.rng = vb, np.random.default_rng(seed)
+        self.batch, self.hq, self.hkv, self.d, self.n_max, self.page, self.fmt, self.q_len = batch, hq, hkv, d, n_max, page, fmt, q_len
+        self.block = block or 16
+        pages = -(-n_max // page) if page else 0
+        self.pages = batch * pages + 2 if page else 0
+        self.params = dict(batch=batch, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, n_max=n_max, kv_layout=1 if page else 0, page_size=page,
+                           num_blocks=self.pages, sink=20, window=10, topk_abs=0, topk_frac=0.3, base_abs=0, base_frac=0.05, epsilon=0.1,
+                           delta=0.1, target=0, sm_scale=0.0, budget_cap_frac=1.0)
+        self.params.update(over)
+        self.plan = vb.vatt_plan_create_chunk(self.params, q_len, 0)
+        vb.vatt_plan_set_option(self.plan, vb.VATT_OPT_KV_FORMAT, fmt)
+        if block:
+            vb.vatt_plan_set_option(self.plan, vb.VATT_OPT_BLOCK_TOKENS, block)
+        self.rotary = rotary
+        if rotary:
+            vb.vatt_plan_set_rotary(self.plan, rotary)
+        self.table = None
+        if page:
+            self.table = torch.from_numpy(self.rng.permutation(self.pages)[:batch * pages].reshape(batch, pages).astype(np.int32)).cuda()
+        self.ws = torch.empty(vb.vatt_plan_workspace_bytes(self.plan), dtype=torch.uint8, device="cuda")
+        self.k, self.v = self.random_cache(), self.random_cache()
+
+    def __del__(self):
+        self.vb.vatt_plan_destroy(self.plan)
+
+    def random_cache(self):
+        vb, rng = self.vb, self.rng
+        size, off = vb.vatt_kv_cache_bytes(self.plan), vb.vatt_kv_scale_offset(self.plan)
+        if self.fmt == co.BF16:
+            return _bf16(rng.normal(size=size // 2)).view(torch.uint8)
+        raw = rng.integers(0, 256, size=size, dtype=np.uint8)
+        if self.fmt == co.E4M3:
+            raw[:off] = np.where(raw[:off] & 0x7f == 0x7f, 0x3c, raw[:off])  # no NaN
+        raw[off:] = rng.integers(117, 121, size=size - off) + (3 if self.fmt == co.E2M1 else 0)
+        return torch.from_numpy(raw).cuda()
+
+    def row_index(self, b, h, tok, scales=False):
+        if self.page:
+            return (int(self.table[b, tok // self.page]) * self.hkv + h) * self.page + tok % self.page
+        return (b * self.hkv + h) * ((self.n_max + 7) // 8 * 8 if scales else self.n_max) + tok
+
+    def raw(self, host, b, h, tok):
+        """(bytes of a row's codes, scale bytes) of a host copy of a buffer."""
+        size = {0: 2 * self.d, 1: self.d, 2: self.d // 2}[self.fmt]
+        off = self.vb.vatt_kv_scale_offset(self.plan)
+        r, s = self.row_index(b, h, tok), self.row_index(b, h, tok, True)
+        return host[r * size:(r + 1) * size], host[off + s * (self.d // 32):off + (s + 1) * (self.d // 32)]
+
+    def rows(self, buf, b, h, tokens):
+        """Values of rows, [len(tokens), d]."""
+        host = buf.cpu().numpy()
+        out = np.zeros((len(tokens), self.d))
+        for i, tok in enumerate(tokens):
+            codes, scales = self.raw(host, b, h, int(tok))
+            if self.fmt == co.BF16:
+                out[i] = torch.from_numpy(codes.copy()).view(torch.bfloat16).double().numpy()
+            else:
+                out[i] = co.decode(co.unpack(codes, self.fmt), scales, self.fmt)
+        return out
+
+    def set_row(self, buf, b, h, tok, codes=None, scales=None, values=None):
+        size = {0: 2 * self.d, 1: self.d, 2: self.d // 2}[self.fmt]
+        off = self.vb.vatt_kv_scale_offset(self.plan)
+        r, s = self.row_index(b, h, tok), self.row_index(b, h, tok, True)
+        if values is not None:
+            buf[r * size:(r + 1) * size] = _bf16(values).view(torch.uint8)
+            return
+        if codes is not None:
+            buf[r * size:(r + 1) * size] = torch.from_numpy(codes).cuda()
+        if scales is not None:
+            buf[off + s * (self.d // 32):off + (s + 1) * (self.d // 32)] = torch.from_numpy(scales).cuda()
+
+    def summary_shape(self):
+        if self.page:
+            return (self.pages, self.hkv, self.page // self.block, 2, self.d)
+        return (self.batch, self.hkv, -(-self.n_max // self.block), 2, self.d)
+
+    def summary_of(self, s, b, h, j):
+        if self.page:
+            per = self.page // self.block
+            return s[int(self.table[b, j // per]), h, j % per]
+        return s[b, h, j]
+
+    def ints(self, x):
+        return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+    def write(self, q, k_new, v_new, first, new_lens=None, summary=None, out_q=None, out_lens=None):
+        n_new = k_new.shape[1]
+        strides = [0 if t is None else self.vb.token_stride(t) for t in (q, k_new, v_new)]
+        self.vb.vatt_write_kv(self.plan, q, k_new, v_new, *strides, n_new, first, new_lens, self.k, self.v, self.table, summary, out_q,
+                              out_lens, torch.cuda.current_stream().cuda_stream)
+
+
+# ---- writing -----------------------------------------------------------------------------------------------------------------
+
+YARN = dict(theta=10000.0, scaling=3, factor=4.0, low=1.0, high=32.0, original_len=64)
+WAVES = dict(theta=500000.0, scaling=2, factor=8.0, low=1.0, high=4.0, original_len=128)
+WRITES = [
+    # (batch, hq, hkv, d, n_max, page, fmt, block, n_new, first, new_lens, rotation, fused)
+    (1, 1, 1, 64, 1, 0, 0, 16, 1, [0], None, dict(theta=1e4), False),
+    (2, 4, 2, 128, 50, 0, 0, 16, 1, [17, 0], None, dict(theta=1e4), False),
+    (2, 4, 2, 128, 77, 0, 0, None, 5, [70, 75], None, dict(theta=1e4, layout=1, rotary_dim=32), True),   # the last ones have no room
+    (3, 8, 1, 64, 130, 0, 1, 32, 33, [1, 31, 90], [33, 0, 20], dict(theta=1e4, rotary_dim=48), True),
+    (2, 2, 2, 128, 96, 16, 1, 16, 40, [0, 13], [40, 11], YARN, False),
+    (2, 8, 2, 128, 192, 64, 2, 64, 70, [60, 3], None, dict(WAVES, layout=1), True),
+    (2, 4, 4, 64, 300, 0, 2, 256, 300, [0, 0], [300, 41], dict(theta=1e4, scaling=1, factor=2.0), False),
+    (1, 4, 2, 64, 64, 8, 0, None, 20, [7], None, WAVES, False),                                          # pages smaller than a block
+    (4, 2, 1, 128, 60, 32, 0, 32, 3, [-1, 60, 59, 8], None, dict(theta=1e4), True),                      # sequences out of range
+    (2, 4, 2, 128, 513, 0, 1, 128, 400, [100, 5], None, None, False),                                    # no rotation
+    (33, 4, 2, 64, 40, 8, 1, None, 1, list(range(33)), None, dict(theta=1e4), True),
+]
+
+
+@pytest.mark.parametrize("case", WRITES, ids=lambda c: "-".join(str(x) for x in c[:9]))
+def test_write(case):
+    batch, hq, hkv, d, n_max, page, fmt, block, n_new, first, new_lens, rotary, fused = case
+    s = Setup(batch, hq, hkv, d, n_max, page, fmt, block, rotary=rotary, seed=n_new)
+    wide = (hq + 2 * hkv) * d + 8
+    x = _bf16(s.rng.normal(size=(batch, n_new, wide)) * np.exp(s.rng.normal(size=(batch, n_new, 1)) * 2))
+    at = [0, hq * d, (hq + hkv) * d, (hq + 2 * hkv) * d]
+    q, kn, vn = (x[..., at[i]:at[i + 1]].unflatten(-1, (-1, d)) for i in range(3))
+    if not fused:
+        q, kn, vn = q.contiguous(), kn.contiguous(), vn.contiguous()
+    before = [s.k.clone(), s.v.clone()]
+    out_q = torch.full((batch, n_new, hq, d), 7.5, dtype=torch.bfloat16, device="cuda") if rotary else None
+    summary = torch.full(s.summary_shape(), 3.25, dtype=torch.bfloat16, device="cuda") if block else None
+    out_lens = s.ints([-5] * batch)
+    s.write(q if rotary else None, kn, vn, s.ints(first), None if new_lens is None else s.ints(new_lens), summary, out_q, out_lens)
+    torch.cuda.synchronize()
+    after = [s.k.cpu().numpy(), s.v.cpu().numpy()]
+    expect = [t.cpu().numpy().copy() for t in before]
+    size = {0: 2 * d, 1: d, 2: d // 2}[fmt]
+    off = s.vb.vatt_kv_scale_offset(s.plan)
+    qh, kh, vh = _np(q), _np(kn), _np(vn)
+    touched = np.zeros(s.summary_shape()[:3], dtype=bool) if block else None
+    for b in range(batch):
+        m = n_new if new_lens is None else new_lens[b]
+        count = max(0, min(m, n_max - first[b])) if 0 <= first[b] < n_max else 0
+        assert int(out_lens[b]) == first[b] + count
+        for j in range(n_new):
+            if j >= count:
+                assert rotary is None or (_np(out_q[b, j]) == 7.5).all()
+                continue
+            pos = first[b] + j
+            for h in range(hq if rotary else 0):
+                want = co.rotate(qh[b, j, h], pos, rotary)
+                # products and their sum in fp32 with cos and sin rounded: 4 half steps of 2^-24 on the pair; then bf16
+                slack = 4 * 2.0 ** -24 * 1.2 * np.abs(qh[b, j, h]).max() * 2
+                assert (np.abs(_np(out_q[b, j, h]) - want) <= HALF_BF16 * np.abs(want) + 1.01 * slack + 2.0 ** -133).all(), (b, j, h)
+            for h in range(hkv):
+                for which, new in ((0, kh), (1, vh)):
+                    codes, scales = s.raw(after[which], b, h, pos)
+                    r, sr = s.row_index(b, h, pos), s.row_index(b, h, pos, True)
+                    expect[which][r * size:(r + 1) * size] = codes
+                    expect[which][off + sr * (d // 32):off + (sr + 1) * (d // 32)] = scales
+                    if which == 1 or rotary is None:  # to the bit
+                        if fmt == 0:
+                            assert np.array_equal(torch.from_numpy(codes.copy()).view(torch.bfloat16).double().numpy(), new[b, j, h])
+                        else:
+                            c, e = co.encode(new[b, j, h], fmt)
+                            assert np.array_equal(co.unpack(codes, fmt), c) and np.array_equal(scales, e), (b, j, h, which)
+                        continue
+                    want = co.rotate(new[b, j, h], pos, rotary)
+                    slack = 4 * 2.0 ** -24 * 1.2 * np.abs(new[b, j, h]).max() * 2
+                    if fmt == 0:
+                        got = torch.from_numpy(codes.copy()).view(torch.bfloat16).double().numpy()
+                        assert (np.abs(got - want) <= HALF_BF16 * np.abs(want) + 1.01 * slack + 2.0 ** -133).all()
+                        continue
+                    got = co.decode(co.unpack(codes, fmt), scales, fmt)
+                    unit = 2.0 ** (scales.astype(np.float64) - 127)
+                    top, limit = np.abs(want).reshape(-1, 32).max(1), 448.0 if fmt == 1 else 6.0
+                    assert (top <= limit * unit + slack).all() and (top > limit * unit / 2 - slack).all()  # the smallest that holds them
+                    unit = np.repeat(unit, 32)
+                    # half a step: e4m3 2^-4 of the value or 2^-10 of the scale, e2m1 a quarter of the value or of the scale
+                    half = np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10 * unit) if fmt == 1 else np.maximum(np.abs(want), unit) / 4
+                    assert (np.abs(got - want) <= half + 1.3 * slack).all(), (b, j, h)
+        if block and count:
+            for j in range(first[b] // block, -(-(first[b] + count) // block)):
+                for h in range(hkv):
+                    toks = range(j * block, min(j * block + block, first[b] + count))
+                    top, low = co.summary(s.rows(s.k, b, h, toks))
+                    got = _np(s.summary_of(summary, b, h, j))
+                    assert np.array_equal(got[0], top) and np.array_equal(got[1], low), (b, h, j)
+                    s.summary_of(summary, b, h, j).fill_(3.25)
+    # nothing else has changed
+    assert np.array_equal(after[0], expect[0]) and np.array_equal(after[1], expect[1])
+    if block:
+        assert (_np(summary) == 3.25).all()
+
+
+@pytest.mark.parametrize("fmt", [1, 2])
+def test_quantised_extremes(fmt):
+    """Zeros, subnormals, the largest values, ties, groups with Inf and NaN: to the bit."""
+    s = Setup(1, 2, 2, 128, 64, 0, fmt, 16)
+    tiny, big = 2.0 ** -133, (2.0 - 2.0 ** -7) * 2.0 ** 127
+    rows = np.zeros((20, 128))
+    rows[0, 3] = -0.0
+    rows[1] = tiny * s.rng.integers(-100, 100, size=128)
+    rows[2] = big * s.rng.uniform(-1, 1, size=128)
+    rows[3, ::7] = [big] * 19
+    rows[4, 5], rows[4, 40], rows[4, 100] = math.inf, -math.inf, math.nan
+    rows[5] = np.tile(co.code_values(2), 8) * 2.0 ** -126
+    rows[6] = 2.0 ** s.rng.integers(-133, 127, size=128)
+    rows[7, :32] = 2.0 ** -119 * np.linspace(-1, 1, 32)
+    rows[8, :32] = 2.0 ** -125 * np.linspace(-6, 6, 32)
+    for i in range(9, 20):
+        rows[i] = np.round(s.rng.uniform(-64, 64, size=128)) / 4 * 2.0 ** (i - 14)
+    new = _bf16(np.stack([rows, rows[::-1]], 1)[None])
+    s.write(None, new, new, s.ints([3]))
+    host, vals = [s.k.cpu().numpy(), s.v.cpu().numpy()], _np(new)
+    for j in range(20):
+        for h in range(2):
+            c, e = co.encode(vals[0, j, h], fmt)
+            for which in range(2):
+                codes, scales = s.raw(host[which], 0, h, 3 + j)
+                assert np.array_equal(scales, e), (j, h)
+                assert np.array_equal(co.unpack(codes, fmt), c), (j, h)
+    # and what they stand for
+    out = torch.zeros((1, 2, 20, 128), dtype=torch.bfloat16, device="cuda")
+    s.vb.vatt_read_kv(s.plan, s.k, None, None, s.ints([23]), s.ints([3]), 20, out, None, torch.cuda.current_stream().cuda_stream)
+    for h in range(2):
+        assert np.array_equal(_np(out[0, h]), s.rows(s.k, 0, h, range(3, 23)), equal_nan=True)
+
+
+def test_summaries_of_nan_and_infinity():
+    s = Setup(1, 2, 2, 64, 64, 0, 0, 16)
+    rows = s.rng.normal(size=(1, 40, 2, 64))
+    rows[0, 3, 0, 5], rows[0, 20, 1, 6], rows[0, 21, 1, 7] = math.nan, math.inf, -math.inf
+    new = _bf16(rows)
+    summary = torch.zeros(s.summary_shape(), dtype=torch.bfloat16, device="cuda")
+    s.write(None, new, new, s.ints([0]), summary=summary)
+    again = torch.zeros_like(summary)
+    s.vb.vatt_block_summary_fill(s.plan, s.k, None, s.ints([40]), again, torch.cuda.current_stream().cuda_stream)
+    for h in range(2):
+        for j in range(3):
+            top, low = co.summary(s.rows(s.k, 0, h, range(16 * j, min(16 * j + 16, 40))))
+            for got in (_np(summary[0, h, j]), _np(again[0, h, j])):
+                assert np.array_equal(got[0], top, equal_nan=True) and np.array_equal(got[1], low, equal_nan=True)
+
+
+@pytest.mark.parametrize("case", [(1, 64, 0, 0, 16), (7, 128, 16, 1, 16), (300, 128, 0, 2, 32), (300, 64, 64, 1, 64), (515, 128, 256, 0, 256)])
+def test_summary_fill(case):
+    n, d, page, fmt, block = case
+    s = Setup(2, 4, 2, d, n, page, fmt, block)
+    lens = [n, n // 2]
+    summary = torch.full(s.summary_shape(), 3.25, dtype=torch.bfloat16, device="cuda")
+    s.vb.vatt_block_summary_fill(s.plan, s.k, s.table, s.ints(lens), summary, torch.cuda.current_stream().cuda_stream)
+    for b in range(2):
+        for h in range(2):
+            for j in range(-(-lens[b] // block)):
+                top, low = co.summary(s.rows(s.k, b, h, range(j * block, min(j * block + block, lens[b]))))
+                got = _np(s.summary_of(summary, b, h, j))
+                assert np.array_equal(got[0], top) and np.array_equal(got[1], low), (b, h, j)
+                s.summary_of(summary, b, h, j).fill_(3.25)
+    assert (_np(summary) == 3.25).all()
+
+
+@pytest.mark.parametrize("case", [
+    # (d, n_max, page, fmt, lens, first, n_rows)
+    (64, 1, 0, 0, [1, 0], None, 1), (128, 333, 0, 1, [333, 100], [330, 99], 5), (128, 320, 16, 2, [317, 5], [-3, 7], 320),
+    (64, 333, 0, 2, [333, 17], [0, 9], 333), (64, 64, 8, 1, [64, 33], None, 40), (128, 256, 64, 0, [1000, -4], [11, 0], 256)])
+def test_read(case):
+    d, n_max, page, fmt, lens, first, n_rows = case
+    s = Setup(2, 4, 2, d, n_max, page, fmt)
+    out = [torch.full((2, 2, n_rows, d), 7.5, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    s.vb.vatt_read_kv(s.plan, s.k, s.v, s.table, s.ints(lens), None if first is None else s.ints(first), n_rows, *out,
+                      torch.cuda.current_stream().cuda_stream)
+    for b in range(2):
+        lo, hi = max(0, first[b] if first else 0), max(0, min(lens[b], n_max))
+        count = max(0, min(n_rows, hi - lo))
+        for h in range(2):
+            for buf, got in ((s.k, out[0]), (s.v, out[1])):
+                assert np.array_equal(_np(got[b, h, :count]), s.rows(buf, b, h, range(lo, lo + count)))
+                assert (_np(got[b, h, count:]) == 7.5).all()
+
+
+# ---- choosing ----------------------------------------------------------------------------------------------------------------
+
+SELECTS = [
+    # (batch, hq, hkv, d, n_max, page, block, q_len, lens, over)
+    (1, 1, 1, 64, 1, 0, 16, 1, [1], {}),
+    (2, 8, 2, 128, 1000, 0, 16, 1, [1000, 333], {}),
+    (3, 8, 1, 64, 2048, 64, 32, 1, [2048, 5, 700], dict(topk_frac=0.9)),
+    (2, 4, 4, 128, 900, 0, 16, 3, [900, 2], dict(sink=0, window=0)),
+    (2, 4, 2, 128, 4096, 256, 256, 2, [4096, 3001], dict(topk_abs=1024, sink=300, window=1)),
+    (2, 16, 8, 64, 5000, 0, 16, 5, [5000, 4097], dict(topk_frac=0.02)),
+    (2, 4, 2, 128, 640, 16, 16, 1, [640, 639], dict(topk_frac=0.0)),
+    (1, 2, 2, 64, 640, 16, 16, 1, [640], dict(topk_frac=1.0)),
+]
+
+
+def _select(s, q, summary, lens, lists):
+    rows, cap = s.batch * s.q_len, s.vb.vatt_block_list_capacity(s.plan)
+    k_max = s.vb.vatt_plan_index_segment(s.plan, 3) - s.vb.vatt_plan_index_segment(s.plan, 2)
+    blocks, count = torch.full((rows, s.hkv, cap), -9, dtype=torch.int32, device="cuda"), s.ints([[-9] * s.hkv] * rows)
+    topk = torch.full((rows, s.hq, max(k_max, 1)), -9, dtype=torch.int32, device="cuda") if lists else None
+    cnt = s.ints([[-9] * s.hq] * rows) if lists else None
+    s.vb.vatt_select_blocks(s.plan, q, summary, s.table, s.ints(lens), s.ws, blocks, count, topk, cnt, torch.cuda.current_stream().cuda_stream)
+    return blocks, count, topk, cnt
+
+
+def _check_select(s, q, summary, lens, got):
+    blocks, count, topk, cnt = (None if x is None else x.cpu().numpy() for x in got)
+    qh, sh, g = _np(q).reshape(s.batch, s.q_len, s.hq, s.d), _np(summary), s.hq // s.hkv
+    for b in range(s.batch):
+        total = -(-lens[b] // s.block)
+        for h in range(s.hkv):
+            ends = np.stack([s.summary_of(sh, b, h, j) for j in range(total)])
+            for t in range(s.q_len):
+                n = max(lens[b] - (s.q_len - 1 - t), 1)
+                u = co.bound(qh[b, t, h * g:(h + 1) * g], ends[:, 0], ends[:, 1])
+                taken, chosen = co.select(u, n, s.params, s.block)
+                r = b * s.q_len + t
+                assert count[r, h] == len(taken) and blocks[r, h, :len(taken)].tolist() == taken, (b, h, t)
+                assert (blocks[r, h, len(taken):] == -9).all()
+                if topk is not None:
+                    want = co.tokens_of(chosen, n, s.block).tolist()
+                    for x in range(g):
+                        assert cnt[r, h * g + x] == len(want) and topk[r, h * g + x, :len(want)].tolist() == want
+                        assert (topk[r, h * g + x, len(want):] == -9).all()
+
+
+@pytest.mark.parametrize("kind", ["normal", "ties", "odd"])
+@pytest.mark.parametrize("case", SELECTS, ids=lambda c: "-".join(str(x) for x in c[:8]))
+def test_select(case, kind):
+    batch, hq, hkv, d, n_max, page, block, q_len, lens, over = case
+    s = Setup(batch, hq, hkv, d, n_max, page, 0, block, q_len, seed=n_max, **over)
+    q = s.rng.normal(size=(batch, q_len, hq, d))
+    ends = s.rng.normal(size=s.summary_shape())
+    if kind == "ties":  # few different scores, -0 among them
+        q, ends = np.sign(q) * (np.abs(q) > 1.5), np.round(ends * 0.7)
+    ends = np.sort(ends, axis=-2)[..., ::-1, :].copy()
+    if kind == "odd":
+        at = s.rng.integers(0, 12, size=s.summary_shape()[:3])
+        for x, value in ((0, math.nan), (1, math.inf), (2, -math.inf)):
+            ends[at == x, x % 2, 5] = value
+        ends[at == 3] *= 1e30
+        q[..., 7] = 0.0
+    q, summary = _bf16(q), _bf16(ends)
+    _check_select(s, q, summary, lens, _select(s, q, summary, lens, kind != "normal"))
+
+
+def test_select_scores_that_differ_by_their_last_bits():
+    """Two halves of the columns that cancel but for a little: sums in 32 bits would take the wrong blocks."""
+    s = Setup(1, 4, 1, 128, 3200, 0, 0, 16, topk_frac=0.25, sink=0, window=0)
+    base = s.rng.normal(size=(1, 1, 200, 2, 128)) * 0.01
+    base[..., :32] += 1000.0
+    base[..., 32:64] -= 1000.0
+    q = s.rng.normal(size=(1, 1, 4, 128))
+    q[..., :64] = np.abs(q[..., :64]) + 1.0
+    q[..., 32:64] = q[..., :32]
+    base[..., 32:64] = -base[..., :32]  # cancels to the last bit; the other columns decide
+    base[..., 0, :], base[..., 1, :] = base.max(-2), base.min(-2)
+    base[..., 1, :64] = base[..., 0, :64]
+    base[..., 0, 32:64] = -base[..., 0, :32]
+    q, summary = _bf16(q), _bf16(base)
+    _check_select(s, q, summary, [3200], _select(s, q, summary, [3200], True))
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------------
+
+def _check_attention(s, q, lens, lists, o, lse):
+    """lists[b * q_len + t][kvh]: tokens."""
+    qh, g = _np(q).reshape(s.batch, s.q_len, s.hq, s.d), s.hq // s.hkv
+    oh, lh = _np(o), _np(lse)
+    scale = s.params["sm_scale"] or 1 / math.sqrt(s.d)
+    for b in range(s.batch):
+        for h in range(s.hkv):
+            k, v = s.rows(s.k, b, h, range(lens[b])), s.rows(s.v, b, h, range(lens[b]))
+            for t in range(s.q_len):
+                toks = lists[b * s.q_len + t][h]
+                for x in range(g):
+                    with np.errstate(invalid="ignore"):
+                        want, total = co.attend(qh[b, t, h * g + x], k[toks], v[toks], scale)
+                    got, at = oh[b * s.q_len + t, h * g + x], (b, t, h * g + x)
+                    ok = np.isfinite(want)
+                    assert np.array_equal(got[~ok], want[~ok], equal_nan=True), at
+                    size = np.linalg.norm(want[ok])
+                    # 32-bit scores and weights: as vatt_dense_decode
+                    assert np.linalg.norm((got - want)[ok]) <= 2e-5 * size, at
+                    if math.isfinite(total):
+                        assert abs(lh[b * s.q_len + t, h * g + x] - total) <= 2e-5 * max(1.0, abs(total)), at
+                    else:
+                        assert np.array_equal(lh[b * s.q_len + t, h * g + x], total, equal_nan=True), at
+
+
+def _block_decode(s, q, lens, blocks, count):
+    rows = s.batch * s.q_len
+    o, lse = (torch.full(x, 7.5, device="cuda") for x in ((rows, s.hq, s.d), (rows, s.hq)))
+    s.vb.vatt_block_decode(s.plan, q, s.k, s.v, s.table, s.ints(lens), blocks, count, s.ws, o, lse, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    return o, lse
+
+
+def _dense(s, q, lens):
+    rows = s.batch * s.q_len
+    o, lse = (torch.full(x, 7.5, device="cuda") for x in ((rows, s.hq, s.d), (rows, s.hq)))
+    s.vb.vatt_dense_decode(s.plan, q, s.k, s.v, s.table, s.ints(lens), s.ws, o, lse, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    return o, lse
+
+
+def _seen(s, lens):
+    return [max(n - (s.q_len - 1 - t), 1) for n in lens for t in range(s.q_len)]
+
+
+DENSE = [
+    # (batch, hq, hkv, d, n_max, page, fmt, q_len, lens)
+    (1, 1, 1, 64, 1, 0, 1, 1, [1]), (2, 4, 1, 128, 33, 0, 2, 1, [33, 31]), (2, 8, 1, 64, 130, 16, 1, 2, [130, 1]),
+    (3, 8, 8, 128, 700, 64, 2, 1, [700, 129, 513]), (2, 8, 2, 128, 401, 0, 1, 4, [401, 3]), (1, 8, 1, 64, 260, 0, 2, 5, [257]),
+    (2, 4, 2, 128, 300, 8, 1, 17, [300, 40]), (1, 8, 1, 128, 200, 32, 2, 12, [199]), (1, 4, 1, 64, 3001, 0, 1, 1, [3001]),
+    (1, 2, 1, 128, 9000, 256, 2, 1, [8999]), (40, 2, 1, 64, 64, 16, 1, 1, [1 + (i * 37) % 64 for i in range(40)]),
+]
+
+
+@pytest.mark.parametrize("case", DENSE, ids=lambda c: "-".join(str(x) for x in c[:8]))
+def test_dense_on_a_quantised_cache(case):
+    batch, hq, hkv, d, n_max, page, fmt, q_len, lens = case
+    s = Setup(batch, hq, hkv, d, n_max, page, fmt, None, q_len, seed=n_max)
+    q = _bf16(s.rng.normal(size=(batch, q_len, hq, d)))
+    lists = [[np.arange(n)] * hkv for n in _seen(s, lens)]
+    _check_attention(s, q, lens, lists, *_dense(s, q, lens))
+
+
+BLOCKS = [
+    # (batch, hq, hkv, d, n_max, page, fmt, block, q_len, lens, over)
+    (1, 1, 1, 64, 1, 0, 0, 16, 1, [1], {}), (2, 8, 2, 128, 500, 0, 0, 16, 1, [500, 17], {}), (2, 8, 1, 64, 512, 64, 1, 32, 3, [500, 2], {}),
+    (2, 4, 4, 128, 640, 16, 2, 16, 2, [640, 333], {}), (1, 16, 2, 128, 2000, 0, 1, 64, 1, [1999], dict(topk_frac=1.0)),
+    (2, 4, 1, 64, 1000, 0, 2, 256, 1, [1000, 255], dict(topk_frac=0.9)), (1, 4, 2, 128, 8192, 256, 0, 256, 1, [8001], dict(topk_frac=1.0)),
+    (3, 2, 2, 64, 333, 0, 0, 16, 1, [333, 332, 9], dict(sm_scale=0.3)),
+]
+
+
+@pytest.mark.parametrize("case", BLOCKS, ids=lambda c: "-".join(str(x) for x in c[:9]))
+def test_attention_over_blocks(case):
+    batch, hq, hkv, d, n_max, page, fmt, block, q_len, lens, over = case
+    s = Setup(batch, hq, hkv, d, n_max, page, fmt, block, q_len, seed=n_max, **over)
+    q = _bf16(s.rng.normal(size=(batch, q_len, hq, d)))
+    rows, cap = batch * q_len, s.vb.vatt_block_list_capacity(s.plan)
+    blocks, count = np.zeros((rows, hkv, cap), dtype=np.int32), np.zeros((rows, hkv), dtype=np.int32)
+    lists = [[None] * hkv for _ in range(rows)]
+    for r, n in enumerate(_seen(s, lens)):
+        total = -(-n // block)
+        for h in range(hkv):
+            m = int(s.rng.integers(1, min(cap, total) + 1))
+            pick = s.rng.permutation(total)[:m]  # any order
+            blocks[r, h] = s.rng.integers(-5, 1 << 30, size=cap)  # what lies behind the list has no say
+            blocks[r, h, :m], count[r, h] = pick, m
+            lists[r][h] = co.tokens_of(pick, n, block)
+    _check_attention(s, q, lens, lists, *_block_decode(s, q, lens, torch.from_numpy(blocks).cuda(), torch.from_numpy(count).cuda()))
+
+
+def test_lists_with_strays_repeats_and_nothing():
+    s = Setup(2, 8, 2, 128, 300, 0, 0, 16, 2, seed=3, topk_frac=1.0)
+    lens, cap = [300, 100], s.vb.vatt_block_list_capacity(s.plan)
+    q = _bf16(s.rng.normal(size=(2, 2, 8, 128)))
+    blocks, count = np.full((4, 2, cap), 2 ** 31 - 1, dtype=np.int32), np.zeros((4, 2), dtype=np.int32)
+    entries = [[[3, 3, 3, -1, 18], [-2 ** 31, 2 ** 31 - 1, 19, 2 ** 27]], [[], [0]], [[6, 7, 18, 5], [6]], [[6, 6], [99, -7]]]
+    lists = [[None] * 2 for _ in range(4)]
+    for r, n in enumerate(_seen(s, lens)):
+        for h in range(2):
+            e = entries[r][h]
+            blocks[r, h, :len(e)], count[r, h] = e, len(e)
+            lists[r][h] = co.tokens_of(e, n, 16)
+    count[1, 0] = -3
+    assert len(lists[0][1]) == len(lists[1][0]) == len(lists[3][1]) == 0  # 0 and -Inf
+    _check_attention(s, q, lens, lists, *_block_decode(s, q, lens, torch.from_numpy(blocks).cuda(), torch.from_numpy(count).cuda()))
+    count[:] = 10 ** 6  # more than the list holds: all of it
+    full = np.tile(np.arange(cap, dtype=np.int32), (4, 2, 1))
+    lists = [[co.tokens_of(range(cap), n, 16)] * 2 for n in _seen(s, lens)]
+    _check_attention(s, q, lens, lists, *_block_decode(s, q, lens, torch.from_numpy(full).cuda(), torch.from_numpy(count).cuda()))
+
+
+INF, NAN = math.inf, math.nan
+
+
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("q_len", [1, 3])
+def test_infinity_and_nan_reach_only_the_queries_that_see_them(page, q_len):
+    s = Setup(2, 8, 2, 128, 336, page, 0, 16, q_len, seed=5, topk_frac=1.0)
+    lens, cap = [333, 90], s.vb.vatt_block_list_capacity(s.plan)
+    for b, n in enumerate(lens):
+        for h in range(2):
+            for tok, value in ((n - 1, [INF, 1.0, NAN]), (n // 2, [INF, -INF, 1.0]), (n // 3, [-INF, 1.0, 1.0])):
+                row = s.rng.normal(size=128)
+                row[3:6] = value
+                s.set_row(s.v, b, h, tok, values=row)
+            for tok in range(n, min(n + 16, 336)):  # behind the sequence
+                s.set_row(s.v, b, h, tok, values=np.full(128, NAN))
+                s.set_row(s.k, b, h, tok, values=np.full(128, INF))
+            low = s.rng.normal(size=128)
+            low[0] = -INF
+            s.set_row(s.k, b, h, 40, values=low)  # a score of -Inf (or Inf, by the query's sign)
+    q = s.rng.normal(size=(2, q_len, 8, 128))
+    q[..., 0] = np.abs(q[..., 0]) + 0.1
+    q = _bf16(q)
+    blocks = torch.arange(cap, dtype=torch.int32, device="cuda").expand(2 * q_len, 2, -1).contiguous()
+    lists = [[np.arange(n)] * 2 for n in _seen(s, lens)]
+    _check_attention(s, q, lens, lists, *_block_decode(s, q, lens, blocks, s.ints([[cap] * 2] * (2 * q_len))))
+    # one block whose scores are all -Inf, alone and beside another
+    for tok in range(32, 48):
+        low = s.rng.normal(size=128)
+        low[0] = -INF
+        for b in range(2):
+            for h in range(2):
+                s.set_row(s.k, b, h, tok, values=low)
+    for pick in ([2], [2, 0], [0, 2, 1]):
+        e = torch.full((2 * q_len, 2, cap), 7, dtype=torch.int32, device="cuda")
+        e[..., :len(pick)] = s.ints(pick)
+        lists = [[co.tokens_of(pick, n, 16)] * 2 for n in _seen(s, lens)]
+        _check_attention(s, q, lens, lists, *_block_decode(s, q, lens, e, s.ints([[len(pick)] * 2] * (2 * q_len))))
+
+
+@pytest.mark.parametrize("fmt", [1, 2])
+@pytest.mark.parametrize("q_len", [1, 6])
+def test_groups_that_are_nan_reach_only_the_queries_that_see_them(fmt, q_len):
+    s = Setup(2, 8, 2, 128, 203, 0, fmt, 16, q_len, seed=6)
+    lens = [203, 64]
+    odd = np.array([120, 255, 120, 120], dtype=np.uint8)
+    for h in range(2):
+        s.set_row(s.v, 0, h, 202, scales=odd)
+        s.set_row(s.v, 0, h, 199, scales=odd[::-1].copy())
+        s.set_row(s.k, 1, 0, 63, scales=odd)
+        for tok in (64, 65):
+            s.set_row(s.v, 1, h, tok, scales=odd)
+            s.set_row(s.k, 1, h, tok, scales=odd)
+    q = _bf16(s.rng.normal(size=(2, q_len, 8, 128)))
+    _check_attention(s, q, lens, [[np.arange(n)] * 2 for n in _seen(s, lens)], *_dense(s, q, lens))
+
+
+def test_scores_far_apart():
+    """Weights over the whole range of exp, the largest score first, last and in the middle."""
+    s = Setup(3, 2, 1, 64, 700, 0, 0, 16, topk_frac=1.0, sm_scale=1.0)
+    for b, at in enumerate((0, 350, 699)):
+        for tok in range(700):
+            s.set_row(s.k, b, 0, tok, values=np.full(64, -abs(tok - at) / 64.0 / 4.0))
+    q, cap = _bf16(np.ones((3, 1, 2, 64)) * np.array([1.0, 8.0])[:, None]), s.vb.vatt_block_list_capacity(s.plan)
+    blocks = torch.arange(cap, dtype=torch.int32, device="cuda").expand(3, 1, -1).contiguous()
+    _check_attention(s, q, [700] * 3, [[np.arange(700)]] * 3, *_block_decode(s, q, [700] * 3, blocks, s.ints([[cap]] * 3)))
+
+
+# ---- together ------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt,page", [(0, 0), (0, 64), (1, 64), (2, 0)])
+def test_a_prompt_in_pieces_then_tokens(fmt, page):
+    """Prompt in two writes, tokens one by one, a sequence cut back: cache and summaries are those of the whole, and every step's choice
+    and attention the oracle's on them; on a bf16 cache the chosen tokens also go through the verified step."""
+    rot = dict(theta=10000.0)
+    s = Setup(2, 8, 2, 128, 640, page, fmt, 32, rotary=rot, seed=8, topk_frac=0.2)
+    whole = Setup(2, 8, 2, 128, 640, page, fmt, 32, rotary=rot, seed=8, topk_frac=0.2)
+    x = [_bf16(s.rng.normal(size=(2, 600, h, 128))) for h in (8, 2, 2)]
+    summary = torch.zeros(s.summary_shape(), dtype=torch.bfloat16, device="cuda")
+    full = torch.zeros_like(summary)
+    lens = [s.ints([0, 0]), s.ints([0, 0])]
+
+    def write(t0, t1, new=None, junk=False):
+        part = [t[:, t0:t1].contiguous() for t in x]
+        if junk:
+            part = [t + 9 for t in part]
+        out_q = torch.zeros_like(part[0])
+        s.write(*part, lens[0], None if new is None else s.ints(new), summary, out_q, lens[1])
+        lens.reverse()
+        return out_q
+
+    write(0, 301)
+    write(301, 590)
+    write(590, 600, junk=True)  # tokens that are taken back
+    lens[0].copy_(s.ints([590, 590]))
+    for t in range(590, 594):
+        q = write(t, t + 1)
+        n = [t + 1] * 2
+        assert lens[0].tolist() == n
+        got = _select(s, q, summary, n, True)
+        torch.cuda.synchronize()
+        _check_select(s, q, summary, n, got)
+        blocks, count = got[0].cpu().numpy(), got[1].cpu().numpy()
+        lists = [[co.tokens_of(blocks[b, h, :count[b, h]], n[b], 32) for h in range(2)] for b in range(2)]
+        o, lse = _block_decode(s, q, n, got[0], got[1])
+        _check_attention(s, q, n, lists, o, lse)
+        if fmt == 0:
+            _verified(s, q, n, got)
+    out_q = torch.zeros((2, 594, 8, 128), dtype=torch.bfloat16, device="cuda")
+    part = [t[:, :594].contiguous() for t in x]
+    whole.table = s.table
+    whole.k.copy_(s.k), whole.v.copy_(s.v)
+    whole.write(*part, s.ints([0, 0]), None, full, out_q, None)
+    torch.cuda.synchronize()
+    for b in range(2):
+        for h in range(2):
+            for buf, other in ((s.k, whole.k), (s.v, whole.v)):
+                assert np.array_equal(s.rows(buf, b, h, range(594)), whole.rows(other, b, h, range(594)))
+            for j in range(19):
+                assert torch.equal(s.summary_of(summary, b, h, j), s.summary_of(full, b, h, j))
+    refill = torch.zeros_like(summary)
+    s.vb.vatt_block_summary_fill(s.plan, s.k, s.table, lens[0], refill, torch.cuda.current_stream().cuda_stream)
+    for b in range(2):
+        for j in range(19):
+            assert torch.equal(s.summary_of(refill, b, 1, j), s.summary_of(full, b, 1, j))
+
+
+def _verified(s, q, lens, got):
+    """vatt_decode_given_topk takes the chosen tokens as its top-k set."""
+    vb, rows = s.vb, s.batch
+    cap = vb.vatt_plan_index_capacity(s.plan)
+    seg = [vb.vatt_plan_index_segment(s.plan, i) for i in range(5)]
+    o, lse = torch.zeros((rows, s.hq, s.d), device="cuda"), torch.zeros((rows, s.hq), device="cuda")
+    idx, counts = torch.zeros((rows, s.hq, cap), dtype=torch.int32, device="cuda"), torch.zeros((rows, s.hq, 8), dtype=torch.int32, device="cuda")
+    seeds = torch.arange(rows, dtype=torch.int64, device="cuda")
+    vb.vatt_decode_given_topk(s.plan, q, s.k, s.v, s.table, s.ints(lens), seeds, got[2], got[3], s.ws, o, lse, idx, counts, None, None,
+                              torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    for b in range(rows):
+        for h in range(s.hq):
+            m = int(got[3][b, h])
+            assert int(counts[b, h, 2]) == m and torch.equal(idx[b, h, seg[2]:seg[2] + m], got[2][b, h, :m])
+    assert torch.isfinite(o).all()
+
+
+def test_all_blocks_on_bf16_are_dense_attention():
+    s = Setup(2, 8, 2, 128, 1500, 0, 0, 16, seed=9, topk_frac=1.0)
+    q, lens, cap = _bf16(s.rng.normal(size=(2, 1, 8, 128))), [1500, 700], s.vb.vatt_block_list_capacity(s.plan)
+    blocks = torch.arange(cap, dtype=torch.int32, device="cuda").expand(2, 2, -1).contiguous()
+    o, lse = _block_decode(s, q, lens, blocks, s.ints([[cap] * 2] * 2))
+    do, dlse = _dense(s, q, lens)
+    assert float((o - do).norm() / do.norm()) < 1e-5 and float((lse - dlse).abs().max()) < 1e-5
+
+
+@pytest.mark.parametrize("fmt,page", [(1, 16), (0, 0)])
+def test_a_captured_step(fmt, page):
+    """Write, choice and attention captured once and replayed with other inputs in the same buffers, the program's own work between."""
+    s = Setup(3, 8, 2, 128, 512, page, fmt, 16, rotary=dict(theta=10000.0), seed=10)
+    s.rng = np.random.default_rng(11)
+    x = [_bf16(s.rng.normal(size=(3, 1, h, 128))) for h in (8, 2, 2)]
+    first, after = s.ints([500, 17, 255]), s.ints([0, 0, 0])
+    summary = torch.zeros(s.summary_shape(), dtype=torch.bfloat16, device="cuda")
+    s.vb.vatt_block_summary_fill(s.plan, s.k, s.table, first, summary, torch.cuda.current_stream().cuda_stream)
+    cap = s.vb.vatt_block_list_capacity(s.plan)
+    out_q = torch.zeros((3, 1, 8, 128), dtype=torch.bfloat16, device="cuda")
+    blocks, count = torch.zeros((3, 2, cap), dtype=torch.int32, device="cuda"), s.ints([[0, 0]] * 3)
+    o, lse = torch.zeros((3, 8, 128), device="cuda"), torch.zeros((3, 8), device="cuda")
+
+    def step():
+        st = torch.cuda.current_stream().cuda_stream
+        s.write(*x, first, None, summary, out_q, after)
+        s.vb.vatt_select_blocks(s.plan, out_q, summary, s.table, after, s.ws, blocks, count, None, None, st)
+        s.vb.vatt_block_decode(s.plan, out_q, s.k, s.v, s.table, after, blocks, count, s.ws, o, lse, st)
+
+    outs = (summary, out_q, blocks, count, o, lse, after)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        for t in x:
+            t.copy_(_bf16(s.rng.normal(size=tuple(t.shape))))
+        first.copy_(s.ints([500 + i, 17 + 3 * i, 255 + 80 * i]))
+        saved = [t.clone() for t in (s.k, s.v, summary)]
+        for t in (out_q, o, lse, count):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs] + [s.k.clone(), s.v.clone()]
+        for t, old in zip((s.k, s.v, summary), saved):
+            t.copy_(old)
+        step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, [*outs, s.k, s.v]):
+            assert torch.equal(a, b)
+
+
+def test_another_stream():
+    s = Setup(2, 8, 2, 128, 512, 0, 1, 16, rotary=dict(theta=10000.0), seed=12)
+    x = [_bf16(s.rng.normal(size=(2, 200, h, 128))) for h in (8, 2, 2)]
+    side, res = torch.cuda.Stream(), []
+    for stream in (torch.cuda.current_stream(), side):
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            summary = torch.zeros(s.summary_shape(), dtype=torch.bfloat16, device="cuda")
+            out_q, after = torch.zeros_like(x[0]), s.ints([0, 0])
+            s.write(*x, s.ints([5, 100]), None, summary, out_q, after)
+            q = out_q[:, -1].contiguous()
+            got = _select(s, q, summary, [205, 300], False)
+            o, lse = _block_decode(s, q, [205, 300], got[0], got[1])
+        stream.synchronize()
+        res.append([t.clone() for t in (summary, out_q, o, lse, got[0], s.k)])
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
+def test_calls_for_bf16_caches_refuse_others():
+    s = Setup(1, 4, 2, 128, 64, 0, 1)
+    vb, x, i, z = s.vb, torch.zeros(1 << 16, device="cuda"), s.ints([1]), torch.zeros(1, dtype=torch.int64, device="cuda")
+    for call in (lambda: vb.vatt_decode(s.plan, x, s.k, s.v, None, i, z, s.ws, x, x, x, x, None, None),
+                 lambda: vb.vatt_decode_given_topk(s.plan, x, s.k, s.v, None, i, z, x, x, s.ws, x, x, x, x, None, None),
+                 lambda: vb.vatt_score(s.plan, x, s.k, None, i, s.ws), lambda: vb.vatt_append_kv(s.plan, x, x, s.k, s.v, None, i),
+                 lambda: vb.vatt_random_cache_fill(s.plan, s.k, s.v, None, i, z, x),
+                 lambda: vb.vatt_append_kv_cached(s.plan, x, x, s.k, s.v, None, i, z, x),
+                 lambda: vb.vatt_decode_static(s.plan, x, s.k, s.v, None, i, z, x, x, x, x, None, None)):
+        with pytest.raises(vb.VattError) as e:
+            call()
+        assert e.value.status == vb.VATT_E_UNSUPPORTED_SHAPE
