@@ -171,11 +171,7 @@ _lib = _load()
 
 def _ptr(x) -> Optional[int]:
     """Device/host address of a tensor-like (anything with data_ptr()), an int, or None."""
-    if x is None:
-        return None
-    if isinstance(x, int):
-        return x
-    return int(x.data_ptr())
+    return x if x is None or isinstance(x, int) else x.data_ptr()
 
 
 def _nbytes(x) -> int:

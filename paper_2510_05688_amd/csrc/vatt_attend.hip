@@ -13,7 +13,9 @@ __device__ __forceinline__ uint32_t lower_halves(uint32_t a, uint32_t b) { retur
 
 constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / kWave;
 constexpr int kUnit = 32;          // keys that a wave takes at a time
+constexpr int kChunk = 16;         // groups of 8 tokens that a workgroup takes at a time: a unit for each wave
 constexpr int kSlots = 1024;       // groups of 8 tokens that a workgroup looks up at a time
+constexpr int kSplitsMax = 128;
 constexpr int kNowhere = 0x7fffff00;  // token of a group that does not exist: beyond every sequence
 
 struct AttendArgs {
@@ -36,10 +38,10 @@ struct AttendArgs {
 // A list of tokens in groups of 8: how many groups, and the first token of each (kNowhere where there is none).
 struct TokenList {
   const int32_t* blocks;
-  int count, shift, n;  // n: tokens of the sequence that count
+  int count, capacity, shift, n;  // n: tokens of the sequence that count
 };
 __device__ __forceinline__ TokenList token_list(const AttendArgs& A, int vb, int kvh, int n) {
-  TokenList L = {nullptr, 0, A.block_shift, n};
+  TokenList L = {nullptr, 0, A.capacity, A.block_shift, n};
   if (A.blocks) {
     const int64_t row = (int64_t)vb * A.Hkv + kvh;
     L.blocks = A.blocks + row * A.capacity;
@@ -49,10 +51,13 @@ __device__ __forceinline__ TokenList token_list(const AttendArgs& A, int vb, int
   }
   return L;
 }
-__device__ __forceinline__ int token_of(const TokenList& L, int group) {
+// (an entry is read without waiting for the length of its list)
+__device__ __forceinline__ int entry_of(const TokenList& L, int group) {
+  return L.blocks ? L.blocks[min(group >> (L.shift - 3), L.capacity - 1)] : 0;
+}
+__device__ __forceinline__ int token_of(const TokenList& L, int group, int blk) {
   if (group >= L.count) return kNowhere;
   if (!L.blocks) return group * 8;
-  const int blk = L.blocks[group >> (L.shift - 3)];
   if ((uint32_t)blk > (uint32_t)(L.n - 1) >> L.shift) return kNowhere;
   return (blk << L.shift) + ((group << 3) & ((1 << L.shift) - 1));
 }
@@ -103,8 +108,11 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
   __shared__ int s_at[kSlots];
   __shared__ float4 s_o[kAttendWaves][4][E / 4][kWave];
   __shared__ float s_m[kAttendWaves][16], s_l[kAttendWaves][16];
+  // (with two tiles of vectors the queries stay in LDS: there are no registers for them)
+  constexpr bool kQueriesInLds = NQT > 1;
+  __shared__ uint4 s_q[kQueriesInLds ? NQT * S : 1][kWave];
 
-  uint4 bq[NQT][S];
+  uint4 bq[kQueriesInLds ? 1 : NQT][S];
   int seen[NQT];
   int least = n;
 #pragma unroll
@@ -113,8 +121,11 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
     const int t = t0 + c / G, g = c % G;
     const uint16_t* src = A.q + (((int64_t)seq * Q + t) * A.Hq + (int64_t)kvh * G + g) * D;
 #pragma unroll
-    for (int s = 0; s < S; ++s)
-      bq[nt][s] = *reinterpret_cast<const uint4*>(src + (s / STEPS) * 4 * (STEPS * 8) + g4 * (STEPS * 8) + (s % STEPS) * 8);
+    for (int s = 0; s < S; ++s) {
+      const uint4 x = *reinterpret_cast<const uint4*>(src + (s / STEPS) * 4 * (STEPS * 8) + g4 * (STEPS * 8) + (s % STEPS) * 8);
+      if constexpr (!kQueriesInLds) bq[nt][s] = x;
+      else if (wave == 0) s_q[nt * S + s][lane] = x;  // (a barrier follows before the first unit)
+    }
     seen[nt] = max(n_seq - (Q - 1 - t), 1);
   }
   if (!listed) least = max(n_seq - (Q - 1), 1);
@@ -193,24 +204,28 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
     }
   };
 
-  const int units = (L.count + 3) / 4, per = (units + A.splits - 1) / A.splits;
-  const int u_lo = split * per, u_hi = min(u_lo + per, units);
-  for (int u0 = u_lo; u0 < u_hi; u0 += kSlots / 4) {
-    const int u1 = min(u0 + kSlots / 4, u_hi);
-    __syncthreads();
-    for (int i = tid; i < (u1 - u0) * 4; i += kAttendThreads) {
-      const int tok = token_of(L, u0 * 4 + i), safe = tok == kNowhere ? 0 : tok;
+  // The chunks of the list go round the workgroups, so that which entries a workgroup looks up first does not depend on the length.
+  auto group_of = [&](int i) { return (split + (i / kChunk) * A.splits) * kChunk + i % kChunk; };
+  const int entry0 = entry_of(L, group_of(tid));
+  const int chunks = (L.count + kChunk - 1) / kChunk, mine = split < chunks ? (chunks - split + A.splits - 1) / A.splits : 0;
+  for (int c0 = 0; c0 < mine; c0 += kSlots / kChunk) {
+    const int c_n = min(kSlots / kChunk, mine - c0);
+    if (c0 > 0) __syncthreads();
+    for (int i = tid; i < c_n * kChunk; i += kAttendThreads) {
+      const int group = group_of(c0 * kChunk + i);
+      const int tok = token_of(L, group, c0 == 0 && i == tid ? entry0 : entry_of(L, group)), safe = tok == kNowhere ? 0 : tok;
       s_tok[i] = tok;
       if constexpr (PAGED) s_at[i] = (row_block<PAGED>(A.M, seq, safe) << page8) + ((safe & ((1 << A.M.page_shift) - 1)) >> 3);
       else s_at[i] = safe;
     }
     __syncthreads();
-    int u = u0 + wave;
-    if (u >= u1) continue;
-    load_k((u - u0) * 4);
-    load_v((u - u0) * 4);
-    for (; u < u1; u += kAttendWaves) {
-      const int s0 = (u - u0) * 4, next = (min(u + kAttendWaves, u1 - 1) - u0) * 4;
+    load_k(wave * 4);
+    load_v(wave * 4);
+    for (int c = 0; c < c_n; ++c) {
+      const int s0 = c * kChunk + wave * 4;
+      const bool more = c + 1 < c_n;
+      int my = lane;
+      if constexpr (kQueriesInLds) asm volatile("" : "+v"(my));  // (read again in every round, not kept)
       f32x4_t sc[NQT][2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -235,12 +250,15 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
             }
           }
 #pragma unroll
-          for (int nt = 0; nt < NQT; ++nt)
-            sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka), __builtin_bit_cast(bf16x8_t, bq[nt][s]),
-                                                                sc[nt][t], 0, 0, 0);
+          for (int nt = 0; nt < NQT; ++nt) {
+            uint4 b;
+            if constexpr (kQueriesInLds) b = s_q[nt * S + s][my];
+            else b = bq[nt][s];
+            sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka), __builtin_bit_cast(bf16x8_t, b), sc[nt][t], 0, 0, 0);
+          }
         }
       }
-      load_k(next);
+      if (more) load_k(s0 + kChunk);
       const int4 tok = *reinterpret_cast<const int4*>(&s_tok[s0]);
       const int far = max(max(tok.x, tok.y), max(tok.z, tok.w)) + 8;
       const bool edge = far > least;  // some column does not see all of the 32 keys
@@ -338,7 +356,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
           }
         }
       }
-      load_v(next);
+      if (more) load_v(s0 + kChunk);
     }
   }
 
@@ -406,7 +424,7 @@ __device__ __forceinline__ void attend_again(const AttendArgs& A, int64_t vb, in
   const uint32_t qw[4] = {qv.x, qv.y, qv.z, qv.w};
   float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (int64_t i = wave * RPW + rsub; i < (int64_t)L.count * 8; i += kAttendWaves * RPW) {
-    const int tok = token_of(L, (int)(i >> 3)) + (int)(i & 7);
+    const int group = (int)(i >> 3), tok = token_of(L, group, entry_of(L, group)) + (int)(i & 7);
     if (tok >= L.n) continue;
     const RowAt at = row_at<PAGED>(A.M, seq, kvh, tok, row_block<PAGED>(A.M, seq, tok));
     uint4 x[2];
@@ -458,25 +476,47 @@ __device__ __forceinline__ void attend_again(const AttendArgs& A, int64_t vb, in
   __syncthreads();
 }
 
-// Merge of a head's partial sums.  A result with an Inf or a NaN is worked out again: the second product of attend_kernel gives every
-// column every V row of a step, with weight 0 where the column does not see the token, and in three terms of which some are 0, so that a
-// row with an Inf or a NaN makes a NaN where it has no say.
+// Merge of a head's partial sums: bound by two dependent loads.  Every wave looks at all (max, sum) pairs, one or two per lane; the threads of
+// a column take every PARTS-th partial sum each, the first ones asked for before it is known which count.
+// A result with an Inf or a NaN is worked out again: the second product of attend_kernel gives every column every V row of a step, with
+// weight 0 where the column does not see the token, and in three terms of which some are 0, so that a row with an Inf or a NaN makes a NaN
+// where it has no say.
 template <int D, int FMT, bool PAGED>
 __global__ __launch_bounds__(kAttendThreads) void attend_merge_kernel(AttendArgs A) {
+  constexpr int PARTS = kAttendThreads / D, kAhead = 4;
+  static_assert(kSplitsMax == 2 * kWave, "two pairs per lane");
   __shared__ float s_acc[kAttendWaves][D], s_m[kAttendWaves], s_l[kAttendWaves];
-  const int h = blockIdx.x, tid = threadIdx.x, c = tid % D;
+  const int h = blockIdx.x, tid = threadIdx.x, c = tid % D, part = tid / D, lane = tid & 63;
   const int64_t vb = blockIdx.y, head = vb * A.Hq + h;
   const float2* ml = A.part_ml + head * A.splits;
-  float m = -INFINITY, l = 0.f, a = 0.f;
-  for (int s = 0; s < A.splits; ++s) m = fmaxf(m, ml[s].x);
-  for (int s = 0; s < A.splits; ++s) {
-    const float2 x = ml[s];
-    if (x.x == -INFINITY) continue;
-    const float w = x.x == m ? 1.f : __expf(x.x - m);
-    l += x.y * w;
-    a += A.part[(head * A.splits + s) * D + c] * w;
+  const float* p = A.part + head * A.splits * D + c;
+  const float2 none = make_float2(-INFINITY, 0.f);
+  const float2 x0 = lane < A.splits ? ml[lane] : none, x1 = kWave + lane < A.splits ? ml[kWave + lane] : none;
+  float first[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) first[u] = p[min(part + u * PARTS, A.splits - 1) * D];
+  float m = wave_max(fmaxf(x0.x, x1.x));
+  auto weight_of = [&](float x) { return x == -INFINITY ? 0.f : x == m ? 1.f : __expf(x - m); };
+  const float w0 = weight_of(x0.x), w1 = weight_of(x1.x);
+  float l = wave_sum_f32((w0 != 0.f ? x0.y * w0 : 0.f) + (w1 != 0.f ? x1.y * w1 : 0.f)), a = 0.f;
+  // (pieces without a token, whose sums nobody wrote, have weight 0)
+  auto weight = [&](int s) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s < kWave ? w0 : w1), s & (kWave - 1))); };
+  const int wave_part = __builtin_amdgcn_readfirstlane(part);
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    const int s = wave_part + u * PARTS;
+    if (s < A.splits && weight(s) != 0.f) a += first[u] * weight(s);
   }
-  if (__syncthreads_or(!(fabsf(a) < INFINITY) || !(l < INFINITY))) {
+  for (int s = wave_part + kAhead * PARTS; s < A.splits; s += PARTS) {
+    const float x = p[s * D];
+    if (weight(s) != 0.f) a += x * weight(s);
+  }
+  s_acc[part][c] = a;
+  const bool odd = __syncthreads_or(!(fabsf(a) < INFINITY) || !(l < INFINITY));
+  a = 0.f;
+#pragma unroll
+  for (int x = 0; x < PARTS; ++x) a += s_acc[x][c];
+  if (odd) {
     const int kvh = h / (A.Hq / A.Hkv), seq = seq_of_pair((int)vb, A.q_len), t = (int)vb - seq * A.q_len;
     const int n = max(min(max(A.seq_lens[seq], 1), A.M.n_max) - (A.q_len - 1 - t), 1);
     attend_again<D, FMT, PAGED>(A, vb, h, seq, kvh, token_list(A, (int)vb, kvh, n), s_acc, s_m, s_l);
@@ -546,7 +586,7 @@ hipError_t launch_attend(const Plan& pl, const void* q, const void* k, const voi
   const int64_t rows = (int64_t)pl.vbatch * A.Hq, jobs = (int64_t)(blocks ? pl.vbatch : pl.p.batch) * A.Hkv * A.rounds;
   const int64_t longest = blocks ? (int64_t)A.capacity * pl.block_tokens : pl.p.n_max;
   int64_t splits = std::min<int64_t>((4 * pl.num_cus + jobs - 1) / jobs, (longest + kUnit * kAttendWaves - 1) / (kUnit * kAttendWaves));
-  splits = std::min<int64_t>({splits, 128, (int64_t)(pl.ws_bytes / (rows * (pl.p.head_dim + 2) * sizeof(float)))});
+  splits = std::min<int64_t>({splits, kSplitsMax, (int64_t)(pl.ws_bytes / (rows * (pl.p.head_dim + 2) * sizeof(float)))});
   A.splits = (int)std::max<int64_t>(splits, 1);
   A.part = static_cast<float*>(ws);
   A.part_ml = reinterpret_cast<float2*>(A.part + rows * A.splits * pl.p.head_dim);
