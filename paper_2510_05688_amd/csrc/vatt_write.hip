@@ -1,5 +1,6 @@
 // New rows into the cache (rotated, in the cache's format, with the summaries of the blocks they touch), and rows of it back.
 #include <algorithm>
+#include <cstddef>
 #include <type_traits>
 
 #include "vatt_format.h"
@@ -8,6 +9,11 @@ namespace vatt {
 namespace {
 
 constexpr int kWriteThreads = 256;
+constexpr int kAhead = 4;  // rows that a thread of the write kernel has under way
+// Tokens of a workgroup for the rows without summaries: as many heads' rows of a token as fit lie side by side, and the turns are made for so
+// many tokens (us, 4 / 8 / 16 tokens: prompts of 2 x 16K into e2m1 174 / 171 / 176, of 4 x 0.3K - 2K out of a fused projection 38.4 /
+// 32.4 / 33.4).
+constexpr int kRowTokens = 8;
 
 struct WriteArgs {
   const uint16_t* q;
@@ -59,48 +65,60 @@ __device__ __forceinline__ float2 turn(double a, double factor) {
 // workgroup, to be followed by a barrier.
 template <int D>
 __device__ __forceinline__ void make_turns(const WriteArgs& A, float2 (*turns)[D / 2], int base, int tokens, int first, int end) {
+  // (the frequencies are read where the kernel's arguments lie)
+  typedef const __attribute__((address_space(4))) double* Frequencies;
+  const Frequencies freq = (Frequencies)((const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(WriteArgs, freq));
+#pragma unroll 1
   for (int x = threadIdx.x; x < tokens * (D / 2); x += kWriteThreads) {
     const int i = x % (D / 2), t = x / (D / 2);
-    if (i < A.rot / 2 && base + t >= first && base + t < end) turns[t][i] = turn((double)(base + t) * A.freq[i], A.attention);
+    if (i < A.rot / 2 && base + t >= first && base + t < end) turns[t][i] = turn((double)(base + t) * freq[i], A.attention);
   }
 }
 
-// Columns 8 c .. 8 c + 7 of a row, and the columns that they are rotated with.
-struct RowPart {
-  uint4 own, other;
-};
-__device__ __forceinline__ RowPart load_part(const WriteArgs& A, const uint16_t* row, int c, bool rotate) {
-  RowPart x;
-  x.own = x.other = *reinterpret_cast<const uint4*>(row + 8 * c);
-  const int half = A.rot / 2;
-  if (rotate && !A.pairs && 8 * c < A.rot) x.other = *reinterpret_cast<const uint4*>(row + (8 * c < half ? 8 * c + half : 8 * c - half));
-  return x;
+__device__ __forceinline__ uint4 load_part(const uint16_t* row, int c) { return *reinterpret_cast<const uint4*>(row + 8 * c); }
+// The columns that a lane's 8 are rotated with in the layout of halves, from the lane of the row that has them.
+template <int D>
+__device__ __forceinline__ uint4 other_half(const WriteArgs& A, const uint4& own, int c) {
+  const uint32_t w[4] = {own.x, own.y, own.z, own.w};
+  uint32_t o[4];
+  if (A.rot == D) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = D == 128 ? dpp_u32<0x128>(w[i]) : dpp_u32<0x1B>(dpp_u32<0x141>(w[i]));  // lane ^ 8; lane ^ 4
+  } else {
+    const int half = A.rot / 16, from = (int)(threadIdx.x & 63) - c + (c < half ? c + half : c < 2 * half ? c - half : c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = (uint32_t)__shfl((int)w[i], from);
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
 }
-__device__ __forceinline__ void rotated(const WriteArgs& A, const RowPart& x, int c, bool rotate, const float2* turns, float (&y)[8]) {
-  const uint32_t w[4] = {x.own.x, x.own.y, x.own.z, x.own.w}, o[4] = {x.other.x, x.other.y, x.other.z, x.other.w};
+
+// A lane's share of a token's turns: column i becomes own_i cos_i + partner_i sin_i, the sign of the sine included.
+struct LaneTurns {
+  float cos[8], sin[8];
+};
+__device__ __forceinline__ LaneTurns lane_turns(const WriteArgs& A, const float2* turns, int c) {
+  LaneTurns t;
+  const bool lower = 8 * c < A.rot / 2;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 x = turns[A.pairs ? 4 * c + i / 2 : (lower ? 8 * c : 8 * c - A.rot / 2) + i];
+    t.cos[i] = x.x;
+    t.sin[i] = (A.pairs ? (i & 1) == 0 : lower) ? -x.y : x.y;
+  }
+  return t;
+}
+template <int D>
+__device__ __forceinline__ void rotated(const WriteArgs& A, const uint4& own, int c, bool rotate, const LaneTurns& t, float (&y)[8]) {
+  uint4 other = own;
+  if (rotate && !A.pairs) other = other_half<D>(A, own, c);
+  const uint32_t w[4] = {own.x, own.y, own.z, own.w}, o[4] = {other.x, other.y, other.z, other.w};
+  const bool turned = rotate && 8 * c < A.rot;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    y[2 * i] = bf16_lo(w[i]);
-    y[2 * i + 1] = bf16_hi(w[i]);
-  }
-  if (!rotate || 8 * c >= A.rot) return;
-  if (A.pairs) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 t = turns[4 * c + i];
-      const float a = y[2 * i], b = y[2 * i + 1];
-      y[2 * i] = a * t.x - b * t.y;
-      y[2 * i + 1] = b * t.x + a * t.y;
-    }
-  } else {
-    const int half = A.rot / 2;
-    const bool lower = 8 * c < half;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 t = turns[(lower ? 8 * c : 8 * c - half) + i];
-      const float z = (i & 1) ? bf16_hi(o[i / 2]) : bf16_lo(o[i / 2]);
-      y[i] = y[i] * t.x + (lower ? -z : z) * t.y;
-    }
+    const float a = bf16_lo(w[i]), b = bf16_hi(w[i]);
+    const float pa = A.pairs ? b : bf16_lo(o[i]), pb = A.pairs ? a : bf16_hi(o[i]);
+    y[2 * i] = turned ? fmaf(a, t.cos[2 * i], pa * t.sin[2 * i]) : a;
+    y[2 * i + 1] = turned ? fmaf(b, t.cos[2 * i + 1], pb * t.sin[2 * i + 1]) : b;
   }
 }
 
@@ -127,55 +145,97 @@ __device__ __forceinline__ uint4 store_row(unsigned char* buf, int64_t scale_off
 }
 
 // The larger (smaller) of two values; NaN where one is.
-__device__ __forceinline__ float top_of(float a, float b) { return (a > b || a != a) ? a : b; }
-__device__ __forceinline__ float low_of(float a, float b) { return (a < b || a != a) ? a : b; }
+__device__ __forceinline__ float top_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float low_of(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 
-// Summaries of the blocks of one tile of KV head kvh, whose new rows (from position `first` on; none with FILL) are written on the way.
-// One lane per 8 columns, D / 8 lanes per row, every row of a pass of kWriteThreads / (D / 8) tokens from tile_lo on.
+// The largest (smallest) over the 64 / LPR rows of a wave; lane l ends with columns lane_groups_column(l) and the next, as in add_lane_groups.
+template <int LPR, class Pick>
+__device__ __forceinline__ float2 pick_lane_groups(const float (&v)[8], Pick pick) {
+  float half[4], two[2];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[c]), __float_as_uint(v[c + 4]), false, false);
+    half[c] = pick(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(half[c]), __float_as_uint(half[c + 2]), false, false);
+    two[c] = pick(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    if constexpr (LPR == 8) two[c] = pick(two[c], dpp_f32<0x128>(two[c]));  // row_ror:8
+  }
+  return make_float2(two[0], two[1]);
+}
+
+// Summaries of the blocks of one tile of tokens for `heads` KV heads from kvh0 on, whose new rows (from position `first` on; none with FILL)
+// are written on the way.  One lane per 8 columns, D / 8 lanes per row, a pass over kWriteThreads / (D / 8) tokens at a time, head after
+// head, the next row under way; the turns of a lane's columns stay in registers where a tile is one pass.
 // The old rows of a block that is only begun are read again rather than taken from its summary: it then follows from the cache alone, also
 // after a sequence was cut back.  That is up to 15 rows with blocks of 16, beside the row written.
 template <int D, int FMT, bool PAGED, bool FILL>
-__device__ __forceinline__ void summary_tile(const WriteArgs& A, int b, int kvh, int tile_lo, int tile, int first, int end,
-                                             float2 (*turns)[D / 2], bool turns_made, float (*s_ends)[2][D]) {
+__device__ __forceinline__ void summary_tile(const WriteArgs& A, int b, int kvh0, int heads, int tile_lo, int tile, int first, int end,
+                                             float2 (*turns)[D / 2], float (*s_ends)[kWriteThreads / kWave][2][D]) {
   constexpr int LPR = D / 8, TT = kWriteThreads / LPR, WAVES = kWriteThreads / kWave;
   const int tid = threadIdx.x, c = tid % LPR, r = tid / LPR, lane = tid & 63, wave = tid >> 6;
-  const int bs = 1 << A.block_shift;
-  float top[8], low[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    top[i] = -INFINITY;
-    low[i] = INFINITY;
-  }
-  for (int p = 0; p < tile; p += TT) {
-    const int tok = tile_lo + p + r;
-    const bool fresh = !FILL && tok >= first;
-    RowAt at;
-    RowPart part;
+  const int bs = 1 << A.block_shift, passes = tile / TT, items = heads * passes;
+  struct Row {
+    uint4 part;
     Chunk<FMT> code;
-    uint32_t byte = 0;
-    if (tok < end) {
-      if (fresh) part = load_part(A, A.k_new + ((int64_t)b * A.n_new + (tok - first)) * A.k_stride + kvh * D, c, A.rot > 0);
-      at = row_at<PAGED>(A.M, b, kvh, tok, row_block<PAGED>(A.M, b, tok));
-      if (!fresh) {
-        code = load_chunk<FMT>(A.k + at.row * kRowBytes<FMT, D> + c * (kRowBytes<FMT, D> / LPR));
-        if constexpr (FMT != VATT_KV_BF16) byte = A.k[A.scale_off + at.scales * (D / 32) + c / 4];
-      }
+    uint32_t byte;
+  };
+  auto place = [&](int item) {
+    const int h = passes == 1 ? item : item / passes, tok = tile_lo + (passes == 1 ? 0 : (item - h * passes) * TT) + r;
+    return make_int2(kvh0 + h, tok);
+  };
+  auto load = [&](int item, int blk) {
+    const int2 x = place(item);
+    Row row = {};
+    if (x.y >= end) return row;
+    if (!FILL && x.y >= first) {
+      row.part = load_part(A.k_new + ((int64_t)b * A.n_new + (x.y - first)) * A.k_stride + x.x * D, c);
+    } else {
+      const RowAt at = row_at<PAGED>(A.M, b, x.x, x.y, blk);
+      row.code = load_chunk<FMT>(A.k + at.row * kRowBytes<FMT, D> + c * (kRowBytes<FMT, D> / LPR));
+      if constexpr (FMT != VATT_KV_BF16) row.byte = A.k[A.scale_off + at.scales * (D / 32) + c / 4];
     }
-    if (!FILL && A.rot > 0 && !(turns_made && p == 0)) {
-      if (p > 0 || turns_made) __syncthreads();
-      make_turns<D>(A, turns, tile_lo + p, TT, first, end);
+    return row;
+  };
+  auto block_of = [&](int item) { return row_block<PAGED>(A.M, b, min(place(item).y, end - 1)); };
+  float top[8], low[8];
+  LaneTurns lt = {};
+  int blk = block_of(0), buffer = 0;
+  Row next = load(0, blk);
+  for (int item = 0; item < items; ++item) {
+    const int2 x = place(item);
+    const int kvh = x.x, tok = x.y, p = passes == 1 ? 0 : item % passes;
+    if (!FILL && A.rot > 0 && (passes > 1 || item == 0)) {
+      if (item > 0) __syncthreads();
+      make_turns<D>(A, turns, tile_lo + p * TT, TT, first, end);
       __syncthreads();
+      if (8 * c < A.rot) lt = lane_turns(A, turns[r], c);
+    }
+    const Row row = next;
+    const int row_blk = blk;
+    if (item + 1 < items) {
+      if (passes > 1) blk = block_of(item + 1);
+      next = load(item + 1, blk);
+    }
+    if (p == 0 || bs <= TT) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        top[i] = -INFINITY;
+        low[i] = INFINITY;
+      }
     }
     if (tok < end) {
-      uint4 x;
-      if (fresh) {
+      uint4 v;
+      if (!FILL && tok >= first) {
         float y[8];
-        rotated(A, part, c, A.rot > 0, turns[r], y);
-        x = store_row<D, FMT>(A.k, A.scale_off, at, c, y);
+        rotated<D>(A, row.part, c, A.rot > 0, lt, y);
+        v = store_row<D, FMT>(A.k, A.scale_off, row_at<PAGED>(A.M, b, kvh, tok, row_blk), c, y);
       } else {
-        x = chunk_bf16<FMT>(code, byte);
+        v = chunk_bf16<FMT>(row.code, row.byte);
       }
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float z = (i & 1) ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
@@ -183,62 +243,53 @@ __device__ __forceinline__ void summary_tile(const WriteArgs& A, int b, int kvh,
         low[i] = low_of(z, low[i]);
       }
     }
-    if ((p + TT) % bs != 0 && bs > TT) continue;  // the block goes on
-    // (a wave's rows belong to one block)
-#pragma unroll
-    for (int o = LPR; o < kWave; o <<= 1) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        top[i] = top_of(__shfl_xor(top[i], o), top[i]);
-        low[i] = low_of(__shfl_xor(low[i], o), low[i]);
-      }
-    }
-    if (lane < LPR) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        s_ends[wave][0][8 * c + i] = top[i];
-        s_ends[wave][1][8 * c + i] = low[i];
-      }
+    if (p + 1 < passes && bs > TT) continue;  // the block goes on (a tile of several passes is one block)
+    // (a wave's rows belong to one block; two places for the waves' extremes take turns, so that one barrier is enough)
+    const float2 t2 = pick_lane_groups<LPR>(top, [](float a, float b) { return top_of(a, b); });
+    const float2 l2 = pick_lane_groups<LPR>(low, [](float a, float b) { return low_of(a, b); });
+    float(*ends)[2][D] = s_ends[buffer];
+    buffer ^= 1;
+    if (LPR == 16 || !(lane & 8)) {
+      const int col = lane_groups_column<LPR>(lane);
+      *reinterpret_cast<float2*>(&ends[wave][0][col]) = t2;
+      *reinterpret_cast<float2*>(&ends[wave][1][col]) = l2;
     }
     __syncthreads();
     const int blocks = bs < TT ? TT / bs : 1, per = WAVES / blocks;
     if (tid < blocks * 2 * LPR) {
-      const int which = (tid / LPR) & 1, k = tid / (2 * LPR);
-      const int lo = bs <= TT ? tile_lo + p + k * bs : tile_lo + p + TT - bs;
+      const int which = (tid / LPR) & 1, k = tid / (2 * LPR), lo = tile_lo + k * bs;
       float y[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        y[i] = s_ends[k * per][which][8 * c + i];
-        for (int w = 1; w < per; ++w) {
-          const float z = s_ends[k * per + w][which][8 * c + i];
+      for (int i = 0; i < 8; ++i) y[i] = ends[k * per][which][8 * c + i];
+      for (int w = 1; w < per; ++w) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float z = ends[k * per + w][which][8 * c + i];
           y[i] = which == 0 ? top_of(z, y[i]) : low_of(z, y[i]);
         }
       }
       if (lo < end && lo + bs > first) {
-        int64_t place;
+        int64_t at;
         if constexpr (PAGED)
-          place = ((int64_t)row_block<PAGED>(A.M, b, lo) * A.Hkv + kvh) * A.head_blocks + ((lo >> A.block_shift) & (A.head_blocks - 1));
+          at = ((int64_t)row_block<PAGED>(A.M, b, lo) * A.Hkv + kvh) * A.head_blocks + ((lo >> A.block_shift) & (A.head_blocks - 1));
         else
-          place = ((int64_t)b * A.Hkv + kvh) * A.head_blocks + (lo >> A.block_shift);
-        *reinterpret_cast<uint4*>(A.summary + (place * 2 + which) * D + 8 * c) = packed(y);
+          at = ((int64_t)b * A.Hkv + kvh) * A.head_blocks + (lo >> A.block_shift);
+        *reinterpret_cast<uint4*>(A.summary + (at * 2 + which) * D + 8 * c) = packed(y);
       }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      top[i] = -INFINITY;
-      low[i] = INFINITY;
     }
   }
 }
 
 // One launch for everything a write does.  The first k_jobs workgroups of a sequence each take a tile of whole blocks of some KV
 // heads' K rows, with their summaries; the others take the remaining rows (q, V, and K without summaries), tokens of a tile times heads.
+// What bounds it: prompts the bytes (2 x 16K tokens of 32 + 2 x 8 heads into e2m1, 707 MB, 171 us = 4.1 TB/s, a copy runs at 4.8), single
+// tokens the chain first -> block-table entry -> old rows of the block -> its summary (4.2 us for one, 5.9 for 32).  With one row of a
+// thread under way instead of four, and the partner columns loaded a second time instead of fetched from their lane, 247 us.
 template <int D, int FMT, bool PAGED>
 __global__ __launch_bounds__(kWriteThreads) void write_kernel(WriteArgs A) {
   constexpr int LPR = D / 8, TT = kWriteThreads / LPR;
   __shared__ float2 turns[TT][D / 2];
-  __shared__ float s_ends[kWriteThreads / kWave][2][D];
+  __shared__ float s_ends[2][kWriteThreads / kWave][2][D];
   const int b = blockIdx.y, tid = threadIdx.x, c = tid % LPR, r = tid / LPR;
   const int first = A.first[b];
   int end = first;
@@ -250,8 +301,8 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(WriteArgs A) {
     const int tile = max(1 << A.block_shift, TT), at = x / A.k_groups, group = x - at * A.k_groups;
     const int tile_lo = (first / tile + at) * tile;
     if (tile_lo >= end) return;
-    for (int h = 0; h < A.k_heads && group * A.k_heads + h < A.Hkv; ++h)
-      summary_tile<D, FMT, PAGED, false>(A, b, group * A.k_heads + h, tile_lo, tile, first, end, turns, h > 0 && tile == TT, s_ends);
+    const int kvh0 = group * A.k_heads;
+    summary_tile<D, FMT, PAGED, false>(A, b, kvh0, min(A.k_heads, A.Hkv - kvh0), tile_lo, tile, first, end, turns, s_ends);
     return;
   }
   x -= A.k_jobs;
@@ -269,20 +320,33 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(WriteArgs A) {
   if (tok >= end) return;
   const int blk = row_block<PAGED>(A.M, b, tok);
   const int64_t src_row = (int64_t)b * A.n_new + j0 + t;
-  for (int p = 0; p < A.row_passes; ++p) {
+  auto row_of = [&](int h) {
+    if (h < n_q) return A.q + src_row * A.q_stride + h * D;
+    if (h < n_q + n_k) return A.k_new + src_row * A.k_stride + (h - n_q) * D;
+    return A.v_new + src_row * A.v_stride + (h - n_q - n_k) * D;
+  };
+  // kAhead heads' rows under way at a time; the turns of the lane's columns stay in registers.
+  LaneTurns lt = {};
+  if (A.rot > 0 && h0 < n_q + n_k && 8 * c < A.rot) lt = lane_turns(A, turns[t], c);
+  for (int p = 0; p < A.row_passes; p += kAhead) {
     const int h = h0 + p * per_pass + (r >> A.row_tokens_shift);
-    if (h >= heads) return;
-    float y[8];
-    if (h < n_q) {
-      const RowPart part = load_part(A, A.q + src_row * A.q_stride + h * D, c, true);
-      rotated(A, part, c, true, turns[t], y);
-      *reinterpret_cast<uint4*>(A.out_q + (src_row * A.Hq + h) * D + 8 * c) = packed(y);
-    } else {
-      const bool is_k = h < n_q + n_k;
-      const int kvh = is_k ? h - n_q : h - n_q - n_k;
-      const RowPart part = load_part(A, (is_k ? A.k_new + src_row * A.k_stride : A.v_new + src_row * A.v_stride) + kvh * D, c, is_k && A.rot > 0);
-      rotated(A, part, c, is_k && A.rot > 0, turns[t], y);
-      store_row<D, FMT>(is_k ? A.k : A.v, A.scale_off, row_at<PAGED>(A.M, b, kvh, tok, blk), c, y);
+    uint4 part[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (p + u < A.row_passes && h + u * per_pass < heads) part[u] = load_part(row_of(h + u * per_pass), c);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int hu = h + u * per_pass;
+      if (p + u >= A.row_passes || hu >= heads) break;
+      float y[8];
+      if (hu < n_q) {
+        rotated<D>(A, part[u], c, true, lt, y);
+        *reinterpret_cast<uint4*>(A.out_q + (src_row * A.Hq + hu) * D + 8 * c) = packed(y);
+      } else {
+        const bool is_k = hu < n_q + n_k;
+        rotated<D>(A, part[u], c, is_k && A.rot > 0, lt, y);
+        store_row<D, FMT>(is_k ? A.k : A.v, A.scale_off, row_at<PAGED>(A.M, b, is_k ? hu - n_q : hu - n_q - n_k, tok, blk), c, y);
+      }
     }
   }
 }
@@ -290,12 +354,12 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(WriteArgs A) {
 template <int D, int FMT, bool PAGED>
 __global__ __launch_bounds__(kWriteThreads) void summary_kernel(WriteArgs A) {
   constexpr int TT = kWriteThreads / (D / 8);
-  __shared__ float s_ends[kWriteThreads / kWave][2][D];
+  __shared__ float s_ends[2][kWriteThreads / kWave][2][D];
   const int b = blockIdx.y, tile = max(1 << A.block_shift, TT);
   const int at = blockIdx.x / A.Hkv, kvh = blockIdx.x - at * A.Hkv;
   const int end = min(max(A.first[b], 0), A.M.n_max);
   if (at * tile >= end) return;
-  summary_tile<D, FMT, PAGED, true>(A, b, kvh, at * tile, tile, 0, end, nullptr, false, s_ends);
+  summary_tile<D, FMT, PAGED, true>(A, b, kvh, 1, at * tile, tile, 0, end, nullptr, s_ends);
 }
 
 struct ReadArgs {
@@ -380,7 +444,7 @@ hipError_t launch_write(const Plan& pl, const void* q, const void* k_new, const 
     A.k_groups = (A.Hkv + A.k_heads - 1) / A.k_heads;
     A.k_jobs = tiles * A.k_groups;
   }
-  while ((1 << A.row_tokens_shift) < std::min(n_new, tokens)) ++A.row_tokens_shift;
+  while ((1 << A.row_tokens_shift) < std::min(n_new, kRowTokens)) ++A.row_tokens_shift;
   const int heads = (out_q ? A.Hq : 0) + (summary ? 0 : A.Hkv) + A.Hkv, per_pass = tokens >> A.row_tokens_shift;
   const int passes = (heads + per_pass - 1) / per_pass, tiles = (n_new + (1 << A.row_tokens_shift) - 1) >> A.row_tokens_shift;
   A.row_passes = std::max(1, std::min({8, passes, (int)((int64_t)batch * tiles * passes / (8 * pl.num_cus))}));
