@@ -369,12 +369,10 @@ def vatt_plan_set_rotary(plan, rotary) -> None:
 def token_stride(x) -> int:
     """Elements between the tokens of a tensor [B, n_new, heads, d].  (torch's strides say nothing in dimensions of size 1.)"""
     b, n_new, heads, d = x.shape
-    rows = (heads == 1 or x.stride(2) == d) and x.stride(3) == 1 and (b == 1 or n_new == 1 or x.stride(0) == n_new * x.stride(1))
-    if not rows:
+    of_seq, of_token, of_head, of_column = x.stride()
+    if (heads > 1 and of_head != d) or of_column != 1 or (b > 1 and n_new > 1 and of_seq != n_new * of_token):
         raise ValueError("heads have to lie one behind the other, sequences n_new tokens apart")
-    if n_new > 1:
-        return x.stride(1)
-    return x.stride(0) if b > 1 else heads * d
+    return of_token if n_new > 1 else of_seq if b > 1 else heads * d
 
 
 def vatt_write_kv(plan, q, k_new, v_new, q_stride, k_stride, v_stride, n_new, first, new_lens, k, v, block_table, summary, out_q,

@@ -27,12 +27,12 @@ struct AttendArgs {
   const int32_t* blocks;  // nullptr: all tokens
   const int32_t* block_count;
   float* part;     // [B * q_len * Hq][splits][d]: sums of the weighted V rows
-  float2* part_ml;  // [B * q_len * Hq][splits]: (max, sum of the weights); max -Inf: no token seen
+  float2* part_ml;  // [B * q_len * Hq][splits]: (max in units of log 2, sum of the weights); max -Inf: no token seen
   float* out_o;
   float* out_lse;
   RowMap M;
   int Hq, Hkv, q_len, splits, rounds, capacity, block_shift;
-  float sm_scale;
+  float log2_scale;  // softmax scale / ln 2
 };
 
 // A list of tokens in groups of 8: how many groups, and the first token of each (kNowhere where there is none).
@@ -62,6 +62,20 @@ __device__ __forceinline__ int token_of(const TokenList& L, int group, int blk) 
   return (blk << L.shift) + ((group << 3) & ((1 << L.shift) - 1));
 }
 
+// STREAM: read once.  All tokens' rows are, those of lists may be in the lists of several query tokens (16 x 32K tokens in e4m3 192 us
+// without the hint, 181 with it; lists of two query tokens, 12 x 4K - 64K, 29.0 without, 31.1 with).
+template <bool STREAM>
+__device__ __forceinline__ uint4 load_16(const unsigned char* p) {
+  return STREAM ? load_stream_16(reinterpret_cast<const uint16_t*>(p)) : *reinterpret_cast<const uint4*>(p);
+}
+template <bool STREAM>
+__device__ __forceinline__ uint2 load_8(const unsigned char* p) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  if constexpr (!STREAM) return *reinterpret_cast<const uint2*>(p);
+  const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+  return make_uint2(x.x, x.y);
+}
+
 // The scale bytes of one row (d / 32 of them).
 template <int D>
 __device__ __forceinline__ uint32_t row_scales(const unsigned char* p) {
@@ -78,9 +92,10 @@ __device__ __forceinline__ uint32_t row_scales(const unsigned char* p) {
 //     product is free as long as K and q agree: every lane loads 16 bytes of its row and takes the 8 to 32 values in them as one to
 //     four steps.
 //   * V is not transposed: a lane loads d / 16 columns of the eight rows of its group and pairs them by rows in registers.
-//   * P goes in as three bf16 terms that add up to the fp32 value, so that the sums keep fp32 accuracy.
+//   * P goes in as three bf16 terms that add up to the fp32 value, so that the sums keep fp32 accuracy.  Where the vectors fill five columns at
+//     most, their three terms are columns of one product (PACK 3); with up to eight, two of them are (PACK 2).
 // The running maximum of a column moves only when a score passes it by more than kLazy.
-template <int D, int FMT, bool PAGED, int NQT>
+template <int D, int FMT, bool PAGED, bool LIST, int NQT, int PACK>
 __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A) {
   constexpr int S = D / 32;  // steps over a row of K
   constexpr int E = D / 16;  // values of a V row per lane = tiles over the head dimension
@@ -90,22 +105,22 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
   constexpr int VB = ROW / 16;                                        // V: bytes per lane and row
   constexpr int VW = VB < 4 ? 1 : VB / 4;
   constexpr bool QUANT = FMT != VATT_KV_BF16;
-  constexpr float kLazy = 6.0f, kLog2e = 1.44269504088896340736f;
+  constexpr float kLazy = 8.0f;
+  static_assert(PACK == 1 || NQT == 1, "packed terms are of one tile");
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g4 = lane >> 4;
   const int kvh = blockIdx.x, split = (int)blockIdx.y / A.rounds, round = (int)blockIdx.y - split * A.rounds;
   const int G = A.Hq / A.Hkv, Q = A.q_len;
-  const bool listed = A.blocks != nullptr;
-  const int seq = listed ? seq_of_pair(blockIdx.z, Q) : blockIdx.z;
+  const int seq = LIST ? seq_of_pair(blockIdx.z, Q) : blockIdx.z;
   const int n_seq = min(max(A.seq_lens[seq], 1), A.M.n_max);
-  // listed: the vectors are the heads of one query token; else those of all query tokens
-  const int t0 = listed ? (int)blockIdx.z - seq * Q : 0, vectors = listed ? G : Q * G;
-  const int n = listed ? max(n_seq - (Q - 1 - t0), 1) : n_seq;
+  // LIST: the vectors are the heads of one query token; else those of all query tokens
+  const int t0 = LIST ? (int)blockIdx.z - seq * Q : 0, vectors = LIST ? G : Q * G;
+  const int n = LIST ? max(n_seq - (Q - 1 - t0), 1) : n_seq;
   const TokenList L = token_list(A, blockIdx.z, kvh, n);
   const int c_base = round * 16 * NQT;
 
   __shared__ __align__(16) int s_tok[kSlots];
-  __shared__ int s_at[kSlots];
+  __shared__ __align__(16) int s_at[kSlots];
   __shared__ float4 s_o[kAttendWaves][4][E / 4][kWave];
   __shared__ float s_m[kAttendWaves][16], s_l[kAttendWaves][16];
   // (with two tiles of vectors the queries stay in LDS: there are no registers for them)
@@ -117,7 +132,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
   int least = n;
 #pragma unroll
   for (int nt = 0; nt < NQT; ++nt) {
-    const int c = min(c_base + nt * 16 + i16, vectors - 1);  // (columns beyond the last vector repeat it and are not stored)
+    // (columns beyond the last vector repeat it and are not stored; with PACK > 1 they are its further terms)
+    const int c = PACK > 1 ? i16 % vectors : min(c_base + nt * 16 + i16, vectors - 1);
     const int t = t0 + c / G, g = c % G;
     const uint16_t* src = A.q + (((int64_t)seq * Q + t) * A.Hq + (int64_t)kvh * G + g) * D;
 #pragma unroll
@@ -128,10 +144,15 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
     }
     seen[nt] = max(n_seq - (Q - 1 - t), 1);
   }
-  if (!listed) least = max(n_seq - (Q - 1), 1);
+  if (!LIST) least = max(n_seq - (Q - 1), 1);
+
+  // what a lane takes away from its weights before they are cut to bf16: nothing, their leading term, the leading two
+  const int term = PACK > 1 ? i16 / vectors : 0;
+  const uint32_t first_term = term >= 1 ? 0xffff0000u : 0u, second_term = PACK == 3 && term >= 2 ? 0xffff0000u : 0u;
+  const uint32_t last_term = PACK == 2 && term == 1 ? 0xffffffffu : 0u;
 
   f32x4_t acc[NQT][E];
-  float mrun[NQT], lrun[NQT];
+  float mrun[NQT], lrun[NQT];  // running maxima of the scores in units of log 2
   bool any[NQT];
 #pragma unroll
   for (int nt = 0; nt < NQT; ++nt) {
@@ -142,57 +163,72 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
     for (int e = 0; e < E; ++e) acc[nt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  const int64_t head = (int64_t)seq * A.Hkv + kvh;
+  // Rows by groups of 8: paged, the group's place among all physical rows / 8; contiguous, its first token, behind a uniform base.
   const int page8 = A.M.page_shift - 3;
-  auto row_of = [&](int slot, int r) -> int64_t {
-    const int at = s_at[slot];
-    if constexpr (PAGED) return ((((int64_t)(at >> page8) * A.Hkv + kvh)) << A.M.page_shift) + ((at & ((1 << page8) - 1)) << 3) + r;
-    else return head * A.M.n_max + min(at + r, n_seq - 1);
+  const int64_t head = (int64_t)seq * A.Hkv + kvh;
+  const unsigned char* k_base = A.k + (PAGED ? 0 : head * A.M.n_max * ROW);
+  const unsigned char* v_base = A.v + (PAGED ? 0 : head * A.M.n_max * ROW);
+  const unsigned char* ks_base = A.k + A.scale_off + (PAGED ? 0 : head * A.M.n_scales * (D / 32));
+  const unsigned char* vs_base = A.v + A.scale_off + (PAGED ? 0 : head * A.M.n_scales * (D / 32));
+  // (a contiguous cache may end inside a group of 8: no row behind the sequence's last one)
+  auto row_of = [&](int slot, int r) {
+    if constexpr (PAGED) return (uint64_t)(uint32_t)s_at[slot] * (uint32_t)(8 * ROW) + (uint32_t)(r * ROW);
+    else return (uint32_t)(min(s_at[slot] + r, n_seq - 1) * ROW);
   };
-  auto scale_row_of = [&](int slot, int r) -> int64_t {
-    if constexpr (PAGED) return row_of(slot, r);
-    else return head * A.M.n_scales + s_at[slot] + r;
+  auto scales_of = [&](int slot, int r) {
+    if constexpr (PAGED) return (uint64_t)(uint32_t)s_at[slot] * (uint32_t)(8 * (D / 32)) + (uint32_t)(r * (D / 32));
+    else return (uint32_t)((s_at[slot] + r) * (D / 32));
   };
   uint32_t kr[2][KL][KB / 4], ks[2], vr[8][VW], vs[2][QUANT ? D / 32 : 1];
   auto load_k = [&](int s0) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int slot = s0 + 2 * t + (i16 >> 3), r = i16 & 7;
-      const unsigned char* p = A.k + row_of(slot, r) * ROW + g4 * KB;
+      const unsigned char* p = k_base + (row_of(slot, r) + g4 * KB);
 #pragma unroll
       for (int l = 0; l < KL; ++l) {
         if constexpr (KB == 16) {
-          const uint4 x = *reinterpret_cast<const uint4*>(p + l * 4 * KB);
+          const uint4 x = load_16<!LIST>(p + l * 4 * KB);
           kr[t][l][0] = x.x; kr[t][l][1] = x.y; kr[t][l][2] = x.z; kr[t][l][3] = x.w;
         } else {
           const uint2 x = *reinterpret_cast<const uint2*>(p);
           kr[t][l][0] = x.x; kr[t][l][1] = x.y;
         }
       }
-      if constexpr (QUANT) ks[t] = row_scales<D>(A.k + A.scale_off + scale_row_of(slot, r) * (D / 32));
+      if constexpr (QUANT) ks[t] = row_scales<D>(ks_base + scales_of(slot, r));
     }
   };
   auto load_v = [&](int s0) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int slot = s0 + (j < 4 ? 0 : 2) + (g4 >> 1), r = (g4 & 1) * 4 + (j & 3);
-      const unsigned char* p = A.v + row_of(slot, r) * ROW + i16 * VB;
+    auto row = [&](int j, const unsigned char* p) {
       if constexpr (VB == 16) {
-        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        const uint4 x = load_16<!LIST>(p);
         vr[j][0] = x.x; vr[j][1] = x.y; vr[j][2] = x.z; vr[j][3] = x.w;
       } else if constexpr (VB == 8) {
-        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        const uint2 x = load_8<!LIST>(p);
         vr[j][0] = x.x; vr[j][1] = x.y;
       } else if constexpr (VB == 4) {
         vr[j][0] = *reinterpret_cast<const uint32_t*>(p);
       } else {
         vr[j][0] = *reinterpret_cast<const uint16_t*>(p);
       }
+    };
+    const int half = (g4 & 1) * 4;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int slot = s0 + 2 * t + (g4 >> 1);
+      if constexpr (PAGED) {  // (four rows of one page)
+        const unsigned char* p = v_base + (row_of(slot, half) + i16 * VB);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) row(4 * t + j, p + j * ROW);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) row(4 * t + j, v_base + (row_of(slot, half + j) + i16 * VB));
+      }
     }
     if constexpr (QUANT) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {  // the scales of four rows, a whole number of words
-        const unsigned char* p = A.v + A.scale_off + scale_row_of(s0 + 2 * t + (g4 >> 1), (g4 & 1) * 4) * (D / 32);
+        const unsigned char* p = vs_base + scales_of(s0 + 2 * t + (g4 >> 1), half);
         if constexpr (D == 128) {
           const uint4 x = *reinterpret_cast<const uint4*>(p);
           vs[t][0] = x.x; vs[t][1] = x.y; vs[t][2] = x.z; vs[t][3] = x.w;
@@ -215,7 +251,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
       const int group = group_of(c0 * kChunk + i);
       const int tok = token_of(L, group, c0 == 0 && i == tid ? entry0 : entry_of(L, group)), safe = tok == kNowhere ? 0 : tok;
       s_tok[i] = tok;
-      if constexpr (PAGED) s_at[i] = (row_block<PAGED>(A.M, seq, safe) << page8) + ((safe & ((1 << A.M.page_shift) - 1)) >> 3);
+      if constexpr (PAGED) s_at[i] = (int)((((uint32_t)row_block<PAGED>(A.M, seq, safe) * A.Hkv + kvh) << page8) + ((safe & ((1 << A.M.page_shift) - 1)) >> 3));
       else s_at[i] = safe;
     }
     __syncthreads();
@@ -264,21 +300,19 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
       const bool edge = far > least;  // some column does not see all of the 32 keys
       // tokens of this lane's result rows: 4 g + r, then 16 + 4 g + r
       const int ta = ((g4 >> 1) ? tok.y : tok.x) + (g4 & 1) * 4, tb = ((g4 >> 1) ? tok.w : tok.z) + (g4 & 1) * 4;
-      uint4 pb[NQT][3];
+      constexpr int TERMS = PACK == 3 ? 1 : PACK == 2 ? 2 : 3;  // second products that the weights take
+      uint4 pb[NQT][TERMS];
 #pragma unroll
       for (int nt = 0; nt < NQT; ++nt) {
         float s[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] = sc[nt][j >> 2][j & 3] * A.sm_scale;
-        bool ok[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) ok[j] = true;
+        for (int j = 0; j < 8; ++j) s[j] = sc[nt][j >> 2][j & 3];
         if (edge) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            ok[j] = (j < 4 ? ta : tb) + (j & 3) < seen[nt];
-            s[j] = ok[j] ? s[j] : -INFINITY;
-            any[nt] |= ok[j];
+            const bool ok = (j < 4 ? ta : tb) + (j & 3) < seen[nt];
+            s[j] = ok ? s[j] : -INFINITY;
+            any[nt] |= ok;
           }
         } else {
           any[nt] = true;
@@ -286,31 +320,38 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
         float top = s[0];
 #pragma unroll
         for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
+        top *= A.log2_scale;
         if (__ballot(top > mrun[nt] + kLazy)) {
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
           const float mnew = fmaxf(mrun[nt], top);
-          const float alpha = mrun[nt] == mnew ? 1.f : __expf(mrun[nt] - mnew);
+          const float alpha = mrun[nt] == mnew ? 1.f : __builtin_amdgcn_exp2f(mrun[nt] - mnew);
           mrun[nt] = mnew;
           lrun[nt] *= alpha;
 #pragma unroll
           for (int e = 0; e < E; ++e) acc[nt][e] *= alpha;
         }
         const float m = mrun[nt] == -INFINITY ? 0.f : mrun[nt];  // (so far every score is -Inf: weights 0)
-        uint32_t w[3][8];
+        uint32_t w[TERMS][8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          float p = __builtin_amdgcn_exp2f((s[j] - m) * kLog2e);
-          if (edge) p = ok[j] ? p : 0.f;
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[j], A.log2_scale, -m));
           lrun[nt] += p;
-          const float r1 = p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
-          const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
-          w[0][j] = __float_as_uint(p);
-          w[1][j] = __float_as_uint(r1);
-          w[2][j] = __float_as_uint(r2);
+          if constexpr (PACK > 1) {
+            float r = p - __uint_as_float(__float_as_uint(p) & first_term);
+            if constexpr (PACK == 3) r -= __uint_as_float(__float_as_uint(r) & second_term);
+            w[0][j] = __float_as_uint(r);
+            if constexpr (PACK == 2) w[1][j] = __float_as_uint(r - __uint_as_float(__float_as_uint(r) & 0xffff0000u)) & last_term;
+          } else {
+            const float r1 = p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
+            const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
+            w[0][j] = __float_as_uint(p);
+            w[1][j] = __float_as_uint(r1);
+            w[2][j] = __float_as_uint(r2);
+          }
         }
 #pragma unroll
-        for (int x = 0; x < 3; ++x)
+        for (int x = 0; x < TERMS; ++x)
           pb[nt][x] = make_uint4(upper_halves(w[x][0], w[x][1]), upper_halves(w[x][2], w[x][3]), upper_halves(w[x][4], w[x][5]),
                                  upper_halves(w[x][6], w[x][7]));
       }
@@ -350,7 +391,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
 #pragma unroll
           for (int nt = 0; nt < NQT; ++nt) {
 #pragma unroll
-            for (int y = 2; y >= 0; --y)
+            for (int y = TERMS - 1; y >= 0; --y)
               acc[nt][2 * x + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va), __builtin_bit_cast(bf16x8_t, pb[nt][y]),
                                                                            acc[nt][2 * x + h], 0, 0, 0);
           }
@@ -389,7 +430,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
     for (int w = 0; w < kAttendWaves; ++w) m = fmaxf(m, s_m[w][i16]);
 #pragma unroll
     for (int w = 0; w < kAttendWaves; ++w) {
-      fac[w] = s_m[w][i16] == -INFINITY ? 0.f : s_m[w][i16] == m ? 1.f : __expf(s_m[w][i16] - m);
+      fac[w] = s_m[w][i16] == -INFINITY ? 0.f : s_m[w][i16] == m ? 1.f : __builtin_amdgcn_exp2f(s_m[w][i16] - m);
       l += s_l[w][i16] * fac[w];
     }
     const int c = c_base + nt * 16 + i16;
@@ -401,11 +442,14 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kAttendWaves; ++w) {
-          const float4 x = s_o[w][wave][e / 4][lane];
-          o.x += x.x * fac[w];
-          o.y += x.y * fac[w];
-          o.z += x.z * fac[w];
-          o.w += x.w * fac[w];
+#pragma unroll
+          for (int x = 0; x < PACK; ++x) {  // (the columns of a vector's terms)
+            const float4 y = s_o[w][wave][e / 4][lane + x * vectors];
+            o.x += y.x * fac[w];
+            o.y += y.y * fac[w];
+            o.z += y.z * fac[w];
+            o.w += y.w * fac[w];
+          }
         }
         *reinterpret_cast<float4*>(A.part + place * D + E * (4 * g4 + wave) + e) = o;
       }
@@ -439,10 +483,10 @@ __device__ __forceinline__ void attend_again(const AttendArgs& A, int64_t vb, in
     float s = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) s += bf16_lo(kw[j]) * bf16_lo(qw[j]) + bf16_hi(kw[j]) * bf16_hi(qw[j]);
-    s = group_sum<LPR>(s) * A.sm_scale;
+    s = group_sum<LPR>(s) * A.log2_scale;
     const float mnew = fmaxf(m, s), shift = mnew == -INFINITY ? -3.0e38f : mnew;
-    const float alpha = m == -INFINITY ? 0.f : m == shift ? 1.f : __expf(m - shift);
-    const float p = __expf(s - shift);
+    const float alpha = m == -INFINITY ? 0.f : m == shift ? 1.f : __builtin_amdgcn_exp2f(m - shift);
+    const float p = __builtin_amdgcn_exp2f(s - shift);
     m = shift;
     l = l * alpha + p;
 #pragma unroll
@@ -454,7 +498,7 @@ __device__ __forceinline__ void attend_again(const AttendArgs& A, int64_t vb, in
   float all = m;
 #pragma unroll
   for (int o = LPR; o < kWave; o <<= 1) all = fmaxf(all, __shfl_xor(all, o));
-  const float f = m == -INFINITY ? 0.f : m == all ? 1.f : __expf(m - all);
+  const float f = m == -INFINITY ? 0.f : m == all ? 1.f : __builtin_amdgcn_exp2f(m - all);
   l = f == 0.f ? 0.f : l * f;
 #pragma unroll
   for (int c = 0; c < 8; ++c) acc[c] = f == 0.f ? 0.f : acc[c] * f;
@@ -496,7 +540,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_merge_kernel(AttendArgs
 #pragma unroll
   for (int u = 0; u < kAhead; ++u) first[u] = p[min(part + u * PARTS, A.splits - 1) * D];
   float m = wave_max(fmaxf(x0.x, x1.x));
-  auto weight_of = [&](float x) { return x == -INFINITY ? 0.f : x == m ? 1.f : __expf(x - m); };
+  auto weight_of = [&](float x) { return x == -INFINITY ? 0.f : x == m ? 1.f : __builtin_amdgcn_exp2f(x - m); };
   const float w0 = weight_of(x0.x), w1 = weight_of(x1.x);
   float l = wave_sum_f32((w0 != 0.f ? x0.y * w0 : 0.f) + (w1 != 0.f ? x1.y * w1 : 0.f)), a = 0.f;
   // (pieces without a token, whose sums nobody wrote, have weight 0)
@@ -525,23 +569,32 @@ __global__ __launch_bounds__(kAttendThreads) void attend_merge_kernel(AttendArgs
     l = a = 0.f;
     for (int w = 0; w < kAttendWaves; ++w) {
       if (s_m[w] == -INFINITY) continue;
-      const float f = s_m[w] == m ? 1.f : __expf(s_m[w] - m);
+      const float f = s_m[w] == m ? 1.f : __builtin_amdgcn_exp2f(s_m[w] - m);
       l += s_l[w] * f;
       a += s_acc[w][c] * f;
     }
   }
   if (tid < D) {
     A.out_o[head * D + c] = m == -INFINITY ? 0.f : a / l;
-    if (tid == 0 && A.out_lse) A.out_lse[head] = m == -INFINITY ? -INFINITY : m + logf(l);
+    if (tid == 0 && A.out_lse) A.out_lse[head] = m == -INFINITY ? -INFINITY : m * 0.69314718055994530942f + logf(l);
   }
 }
 
 template <int D, int FMT, bool PAGED>
 hipError_t launch_attend_f(const Plan& pl, const AttendArgs& A, hipStream_t st) {
-  const int vectors = A.blocks ? pl.group : pl.group * pl.q_len;
-  const dim3 grid(A.Hkv, A.splits * A.rounds, A.blocks ? pl.vbatch : pl.p.batch);
-  if (vectors <= 16) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, 1>), grid, dim3(kAttendThreads), 0, st, A);
-  else hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, 2>), grid, dim3(kAttendThreads), 0, st, A);
+  const dim3 grid(A.Hkv, A.splits * A.rounds, A.blocks ? pl.vbatch : pl.p.batch), threads(kAttendThreads);
+  if (A.blocks) {  // (one to eight vectors)
+    if (pl.group <= 4) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, true, 1, 3>), grid, threads, 0, st, A);
+    else hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, true, 1, 2>), grid, threads, 0, st, A);
+  } else if constexpr (FMT != VATT_KV_BF16) {
+    const int vectors = pl.group * pl.q_len;
+    if (vectors <= 5) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, false, 1, 3>), grid, threads, 0, st, A);
+    else if (vectors <= 8) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, false, 1, 2>), grid, threads, 0, st, A);
+    else if (vectors <= 16) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, false, 1, 1>), grid, threads, 0, st, A);
+    else hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, false, 2, 1>), grid, threads, 0, st, A);
+  } else {
+    return hipErrorInvalidValue;  // (all tokens of a bf16 cache are dense_kernel's)
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((attend_merge_kernel<D, FMT, PAGED>), dim3(A.Hq, pl.vbatch), dim3(kAttendThreads), 0, st, A);
@@ -579,7 +632,7 @@ hipError_t launch_attend(const Plan& pl, const void* q, const void* k, const voi
   A.q_len = pl.q_len;
   A.capacity = block_list_capacity(pl);
   A.block_shift = pl.block_tokens ? 31 - __builtin_clz(pl.block_tokens) : 0;
-  A.sm_scale = pl.sm_scale;
+  A.log2_scale = (float)((double)pl.sm_scale * 1.4426950408889634);
   const int vectors = blocks ? pl.group : pl.group * pl.q_len;
   A.rounds = vectors <= 16 ? 1 : (vectors + 31) / 32;
   // Four workgroups per CU in all, none with less than a unit of keys per wave at the longest; the partial sums fit the workspace.
