@@ -366,7 +366,8 @@ int vatt_append_kv(vatt_plan* plan, const void* k_new, const void* v_new, void* 
  * sequence is its tokens j c .. j c + c - 1.  A block's summary is, for every column, the largest and the smallest value that its
  * tokens' K rows hold in the cache (bf16; exact for every format; NaN where one of them is NaN):
  *   contiguous: bf16 [batch, n_kv_heads, ceil(n_max / c), 2, head_dim], paged: [num_blocks, n_kv_heads, page_size / c, 2, head_dim],
- * vatt_block_summary_bytes(plan) bytes, the largest first.  The calls that take summaries or lists of blocks return
+ * vatt_block_summary_bytes(plan) bytes, the largest first.  Summaries follow vatt_write_kv and vatt_block_summary_fill only: rows
+ * that vatt_append_kv or the caller puts into the cache need a fill before the next choice.  The calls that take summaries or lists of blocks return
  * VATT_E_UNSUPPORTED_SHAPE for plans with pages of 8 tokens.
  */
 enum { VATT_OPT_KV_FORMAT = 17, VATT_OPT_BLOCK_TOKENS = 18 };

@@ -551,9 +551,15 @@ __global__ __launch_bounds__(kAttendThreads) void attend_merge_kernel(AttendArgs
     const int s = wave_part + u * PARTS;
     if (s < A.splits && weight(s) != 0.f) a += first[u] * weight(s);
   }
-  for (int s = wave_part + kAhead * PARTS; s < A.splits; s += PARTS) {
-    const float x = p[s * D];
-    if (weight(s) != 0.f) a += x * weight(s);
+  for (int s0 = wave_part + kAhead * PARTS; s0 < A.splits; s0 += kAhead * PARTS) {
+    float more[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) more[u] = p[min(s0 + u * PARTS, A.splits - 1) * D];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int s = s0 + u * PARTS;
+      if (s < A.splits && weight(s) != 0.f) a += more[u] * weight(s);
+    }
   }
   s_acc[part][c] = a;
   const bool odd = __syncthreads_or(!(fabsf(a) < INFINITY) || !(l < INFINITY));

@@ -20,8 +20,10 @@ def _bf16_from_bits(bits: np.ndarray, device) -> torch.Tensor:
 class DecodeSession:
     """Owns a plan, its workspace and output buffers on one GPU."""
 
-    def __init__(self, params: Dict, device: int = 0, q_len: int = 1):
-        """q_len > 1: a plan for multi-query steps; q is then [B, q_len, Hq, d] and every output has one row per
+    def __init__(self, params: Dict, device: int = 0, q_len: int = 1, kv_format: int = vb.VATT_KV_BF16,
+                 block_tokens: Optional[int] = None, rotary: Optional[Dict] = None):
+        """kv_format, block_tokens, rotary: the cache's format (VATT_KV_*), the tokens per block and the rotation
+        (fields of vatt_rotary) of the cache calls below.  q_len > 1: a plan for multi-query steps; q is then [B, q_len, Hq, d] and every output has one row per
         (sequence, query token) pair, b * q_len + t, where the single-token shapes have one per sequence."""
         if not torch.cuda.is_available():
             raise RuntimeError("DecodeSession needs a GPU; there is no CPU path")
@@ -31,6 +33,11 @@ class DecodeSession:
         self.q_len = int(q_len)
         self.plan = (vb.vatt_plan_create(self.params, device) if self.q_len == 1
                      else vb.vatt_plan_create_chunk(self.params, self.q_len, device))
+        vb.vatt_plan_set_option(self.plan, vb.VATT_OPT_KV_FORMAT, int(kv_format))
+        if block_tokens is not None:
+            vb.vatt_plan_set_option(self.plan, vb.VATT_OPT_BLOCK_TOKENS, int(block_tokens))
+        if rotary is not None:
+            vb.vatt_plan_set_rotary(self.plan, rotary)
         p = self.params
         self.Hq, self.Hkv, self.d = p["n_q_heads"], p["n_kv_heads"], p["head_dim"]
         self.B = p["batch"] * self.q_len  # rows of every per-query buffer
@@ -156,6 +163,50 @@ class DecodeSession:
     def append_device(self, k_new, v_new):
         """Append one token per sequence from tensors that are already on the device (bf16 [B, Hkv, d])."""
         vb.vatt_append_kv(self.plan, k_new, v_new, self.k, self.v, self.block_table, self.seq_lens, self._stream())
+
+    # ---- the cache from the projections' outputs to attention over blocks -----
+    def make_cache(self, block_table=None):
+        """Allocates an empty cache in the plan's format, summaries of its blocks and lists for the chosen ones."""
+        dev, rows = self.device, self.B
+        self.k, self.v = (torch.zeros(vb.vatt_kv_cache_bytes(self.plan), dtype=torch.uint8, device=dev) for _ in range(2))
+        self.block_table = None
+        if block_table is not None:
+            self.block_table = torch.from_numpy(np.ascontiguousarray(block_table, dtype=np.int32)).to(dev)
+        self.seq_lens = torch.zeros(self.params["batch"], dtype=torch.int32, device=dev)
+        self._next_lens = torch.zeros_like(self.seq_lens)
+        self.block_capacity = vb.vatt_block_list_capacity(self.plan)
+        self.summary = self.blocks = self.block_count = None
+        if self.block_capacity:
+            self.summary = torch.zeros(vb.vatt_block_summary_bytes(self.plan) // 2, dtype=torch.bfloat16, device=dev)
+            self.blocks = torch.zeros(rows, self.Hkv, self.block_capacity, dtype=torch.int32, device=dev)
+            self.block_count = torch.zeros(rows, self.Hkv, dtype=torch.int32, device=dev)
+        return self
+
+    def write(self, q, k_new, v_new, new_lens=None):
+        """Appends the tokens k_new, v_new (bf16 [B, n_new, Hkv, d], as far as new_lens says) to every sequence; returns the
+        rotated queries (bf16 [B, n_new, Hq, d]) or None without q."""
+        out_q = None if q is None else torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
+        vb.vatt_write_kv(self.plan, q, k_new, v_new, 0 if q is None else vb.token_stride(q), vb.token_stride(k_new),
+                         vb.token_stride(v_new), k_new.shape[1], self.seq_lens, new_lens, self.k, self.v, self.block_table,
+                         self.summary, out_q, self._next_lens, self._stream())
+        self.seq_lens, self._next_lens = self._next_lens, self.seq_lens
+        return out_q
+
+    def read_rows(self, first, n_rows: int):
+        """(K, V) rows first[b] .. first[b] + n_rows - 1 in bf16 [B, Hkv, n_rows, d]; zeros where a sequence has none."""
+        out = [torch.zeros(self.params["batch"], self.Hkv, n_rows, self.d, dtype=torch.bfloat16, device=self.device) for _ in range(2)]
+        vb.vatt_read_kv(self.plan, self.k, self.v, self.block_table, self.seq_lens, first, n_rows, out[0], out[1], self._stream())
+        return out
+
+    def select_blocks(self, q=None, topk_idx=None, topk_cnt=None):
+        """Fills self.blocks and self.block_count (and the token lists for decode_given_topk, if given)."""
+        vb.vatt_select_blocks(self.plan, self.q if q is None else q, self.summary, self.block_table, self.seq_lens, self.workspace,
+                              self.blocks, self.block_count, topk_idx, topk_cnt, self._stream())
+
+    def block_decode(self, q=None):
+        """Attention over the chosen blocks, into out_o and out_lse."""
+        vb.vatt_block_decode(self.plan, self.q if q is None else q, self.k, self.v, self.block_table, self.seq_lens, self.blocks,
+                             self.block_count, self.workspace, self.out_o, self.out_lse, self._stream())
 
     # ---- read-back -----------------------------------------------------------
     def scores_host(self) -> np.ndarray:

@@ -3,6 +3,7 @@ import math
 
 import numpy as np
 import pytest
+import torch  # (before the library: the HIP runtime that both use is the one that comes with it)
 
 from oracle import cache_ops as co
 from paper_2510_05688_amd import binding as vb
@@ -176,7 +177,6 @@ def test_refusals_of_the_other_calls():
 
 
 def test_oracle_formats():
-    import torch
     e4m3 = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
     assert np.array_equal(co.code_values(co.E4M3), e4m3, equal_nan=True)
     assert co.code_values(co.E2M1).tolist() == [0, .5, 1, 1.5, 2, 3, 4, 6, -0., -.5, -1, -1.5, -2, -3, -4, -6]

@@ -348,7 +348,7 @@ def _check_select(s, q, summary, lens, got):
                         assert (topk[r, h * g + x, len(want):] == -9).all()
 
 
-@pytest.mark.parametrize("kind", ["normal", "ties", "odd"])
+@pytest.mark.parametrize("kind", ["normal", "ties", "odd", "tiny"])
 @pytest.mark.parametrize("case", SELECTS, ids=lambda c: "-".join(str(x) for x in c[:8]))
 def test_select(case, kind):
     batch, hq, hkv, d, n_max, page, block, q_len, lens, over = case
@@ -364,6 +364,11 @@ def test_select(case, kind):
             ends[at == x, x % 2, 5] = value
         ends[at == 3] *= 1e30
         q[..., 7] = 0.0
+    if kind == "tiny":  # subnormal queries on huge keys, and the other way round
+        ends[..., :d // 2] *= 2.0 ** 122
+        q[..., :d // 2] *= 2.0 ** -129
+        ends[..., d // 2:] *= 2.0 ** -130
+        q[..., d // 2:] *= 2.0 ** 120
     q, summary = _bf16(q), _bf16(ends)
     _check_select(s, q, summary, lens, _select(s, q, summary, lens, kind != "normal"))
 
@@ -437,7 +442,9 @@ DENSE = [
     (1, 1, 1, 64, 1, 0, 1, 1, [1]), (2, 4, 1, 128, 33, 0, 2, 1, [33, 31]), (2, 8, 1, 64, 130, 16, 1, 2, [130, 1]),
     (3, 8, 8, 128, 700, 64, 2, 1, [700, 129, 513]), (2, 8, 2, 128, 401, 0, 1, 4, [401, 3]), (1, 8, 1, 64, 260, 0, 2, 5, [257]),
     (2, 4, 2, 128, 300, 8, 1, 17, [300, 40]), (1, 8, 1, 128, 200, 32, 2, 12, [199]), (1, 4, 1, 64, 3001, 0, 1, 1, [3001]),
-    (1, 2, 1, 128, 9000, 256, 2, 1, [8999]), (40, 2, 1, 64, 64, 16, 1, 1, [1 + (i * 37) % 64 for i in range(40)]),
+    (1, 2, 1, 128, 9000, 256, 2, 1, [8999]), (2, 2, 2, 128, 150, 0, 1, 3, [150, 2]), (1, 2, 2, 64, 99, 0, 2, 5, [99]),
+    (2, 4, 2, 128, 350, 16, 2, 3, [350, 64]), (1, 1, 1, 64, 300, 0, 1, 7, [300]), (2, 8, 1, 128, 290, 0, 1, 1, [290, 65]),
+    (1, 1, 1, 128, 200, 32, 2, 9, [197]), (40, 2, 1, 64, 64, 16, 1, 1, [1 + (i * 37) % 64 for i in range(40)]),
 ]
 
 
@@ -713,6 +720,31 @@ def test_another_stream():
         stream.synchronize()
         res.append([t.clone() for t in (summary, out_q, o, lse, got[0], s.k)])
     assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_a_session(fmt):
+    """The calls as a program makes them through DecodeSession: prompt, tokens, rows back, dense attention beside the chosen blocks."""
+    from paper_2510_05688_amd.session import DecodeSession
+    s = Setup(2, 8, 2, 128, 256, 32, fmt, 32, rotary=dict(theta=10000.0), seed=13, topk_frac=1.0)
+    sess = DecodeSession(s.params, kv_format=fmt, block_tokens=32, rotary=dict(theta=10000.0)).make_cache(s.table.cpu().numpy())
+    x = [_bf16(s.rng.normal(size=(2, 203, h, 128))) for h in (8, 2, 2)]
+    sess.write(*[t[:, :200].contiguous() for t in x], s.ints([200, 77]))
+    assert sess.seq_lens.tolist() == [200, 77]
+    for t in range(200, 203):
+        q = sess.write(*[y[:, t:t + 1].contiguous() for y in x])
+        sess.select_blocks(q)
+        sess.block_decode(q)
+        sess.dense(q)
+        assert float((sess.out_o - sess.dense_o).norm() / sess.dense_o.norm()) < 1e-5  # every block is taken
+    lens = [203, 80]
+    assert sess.seq_lens.tolist() == lens
+    s.k, s.v = sess.k, sess.v
+    _check_attention(s, q, lens, [[np.arange(n)] * 2 for n in lens], sess.out_o, sess.out_lse)
+    k, v = sess.read_rows(s.ints([198, 79]), 5)
+    assert np.array_equal(_np(k[0, 1]), s.rows(s.k, 0, 1, range(198, 203))) and np.array_equal(_np(v[1, 0, :1]), s.rows(s.v, 1, 0, [79]))
+    assert not v[1, :, 1:].any()
+    sess.close()
 
 
 def test_calls_for_bf16_caches_refuse_others():
