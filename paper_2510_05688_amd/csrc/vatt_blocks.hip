@@ -69,8 +69,8 @@ __device__ __forceinline__ uint4 magnitudes(const uint4& w) {
 // at a time (operand lane l: row or column l % 16, eight columns of the head); the same with magnitudes bounds the error.  A sum of 2 d
 // products in any order, every addition off by at most 2^-23 of the magnitudes so far, is off by at most 2 d 2^-23 of the sum of all
 // magnitudes; 2^-23 more covers the rounding of the exact sum to 32 bits.  (2^-100: products below the normal range.)
-// What bounds it: the summaries' bytes.  All of them in 64 bits on the vector units took 58 us for 12 sequences of 8K - 128K tokens with 4
-// heads (VALU busy 85 % of the time).
+// What bounds it: the summaries' bytes.  12 sequences of 8K - 128K tokens on pages, 213 MB of summaries, 39 us = 5.4 TB/s; all scores in 64 bits
+// on the vector units took 58 (they were busy 85 % of the time).
 template <int D, bool PAGED>
 __global__ __launch_bounds__(kScoreThreads) void block_score_kernel(SelectBlocksArgs A) {
   constexpr int S = D / 32, TILE = kScoreTile;
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(kScoreThreads) void block_score_kernel(SelectBlocks
   const int end = block_parts(A.sel, tokens_seen(A.seq_lens, seq, A.M.n_max, A.q_len, A.q_len - 1), A.block_shift).hi;
   if (split * TILE >= end) return;
   // A wave loads whole rows, LPR lanes each, and turns them round in LDS: with a row's 64 bytes per lane group and load instead, as the
-  // operands want them, 12 x 128K tokens (403 MB) take 76 us.
+  // operands want them, 12 x 128K tokens (403 MB) take 76 us, so 64.
   constexpr int LPR = 2 * D / 8, RPI = kWave / LPR, LOADS = 16 / RPI;  // lanes per block (both ends), blocks per load, loads
   __shared__ uint4 s_tile[kScoreThreads / kWave][16 * (LPR + 1)];
   uint4* rows = s_tile[wave];
@@ -258,8 +258,10 @@ __device__ __forceinline__ uint32_t score_key(float f) {  // (-0 counts as +0, N
 // ranked by it.
 // T: its bin comes from one histogram over equal steps between the least and the largest finite score (bins of the bits, which a radix
 // selection would begin with, hold nearly all scores of a row together, and their LDS atomics then wait for each other: 28.8 us for
-// 96 rows of up to 8192 blocks, 8.5 so); the few scores in that bin are ranked against each other.  Where one bin holds many (equal scores, or one
+// 96 rows of up to 8192 blocks); the few scores in that bin are ranked against each other.  Where one bin holds many (equal scores, or one
 // far from all others), and where many lie between, a radix selection takes its place.
+// What bounds it: a chain of some 14 barriers and three memory round trips; 96 rows of up to 8192 blocks 10.9 us, 8 of 2048 7.0, of which the
+// bounds in 64 bits are 2.
 template <int D, bool PAGED, int THREADS, int KPT>
 __global__ __launch_bounds__(THREADS) void choose_blocks_kernel(SelectBlocksArgs A) {
   constexpr int WAVES = THREADS / kWave, BINS = 1024, PER = BINS / THREADS, MOST = 256, LPR = D / 8;

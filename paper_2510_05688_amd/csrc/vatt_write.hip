@@ -9,10 +9,10 @@ namespace vatt {
 namespace {
 
 constexpr int kWriteThreads = 256;
-constexpr int kAhead = 4;  // rows that a thread of the write kernel has under way
+constexpr int kAhead = 4;  // rows that a thread of the write kernel has under way (with two, 2 x 16K into e2m1 165 instead of 153 us)
 // Tokens of a workgroup for the rows without summaries: as many heads' rows of a token as fit lie side by side, and the turns are made for so
-// many tokens (us, 4 / 8 / 16 tokens: prompts of 2 x 16K into e2m1 174 / 171 / 176, of 4 x 0.3K - 2K out of a fused projection 38.4 /
-// 32.4 / 33.4).
+// many tokens (us, 4 / 8 / 16 tokens: prompts of 2 x 16K into e2m1 151 / 153 / 155, of 4 x 0.3K - 2K out of a fused projection 34.4 /
+// 29.3 / 30.1).
 constexpr int kRowTokens = 8;
 
 struct WriteArgs {
@@ -32,7 +32,8 @@ struct WriteArgs {
   int n_new, Hq, Hkv;
   int block_shift, head_blocks;  // tokens per block; blocks per KV head of a sequence (contiguous) or of a page
   int k_jobs, k_groups, k_heads;       // workgroups with summaries per sequence, groups of KV heads, and KV heads of one
-  int row_groups, row_passes, row_tokens_shift;  // the other rows: groups of heads, passes of a workgroup, tokens of one
+  int row_groups, q_groups, v_groups;  // the other rows: groups of heads, of them those of q and of V
+  int row_passes, row_tokens_shift;    // passes of a workgroup over its heads, tokens of one
   int rot, pairs;
   double attention;
   double freq[64];
@@ -98,10 +99,11 @@ struct LaneTurns {
 };
 __device__ __forceinline__ LaneTurns lane_turns(const WriteArgs& A, const float2* turns, int c) {
   LaneTurns t;
-  const bool lower = 8 * c < A.rot / 2;
+  const bool lower = 8 * c < A.rot / 2, turned = 8 * c < A.rot;
+  if (!turned) c = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float2 x = turns[A.pairs ? 4 * c + i / 2 : (lower ? 8 * c : 8 * c - A.rot / 2) + i];
+    const float2 x = !turned ? make_float2(1.f, 0.f) : turns[A.pairs ? 4 * c + i / 2 : (lower ? 8 * c : 8 * c - A.rot / 2) + i];
     t.cos[i] = x.x;
     t.sin[i] = (A.pairs ? (i & 1) == 0 : lower) ? -x.y : x.y;
   }
@@ -109,16 +111,29 @@ __device__ __forceinline__ LaneTurns lane_turns(const WriteArgs& A, const float2
 }
 template <int D>
 __device__ __forceinline__ void rotated(const WriteArgs& A, const uint4& own, int c, bool rotate, const LaneTurns& t, float (&y)[8]) {
-  uint4 other = own;
-  if (rotate && !A.pairs) other = other_half<D>(A, own, c);
-  const uint32_t w[4] = {own.x, own.y, own.z, own.w}, o[4] = {other.x, other.y, other.z, other.w};
-  const bool turned = rotate && 8 * c < A.rot;
+  const uint32_t w[4] = {own.x, own.y, own.z, own.w};
+  if (!rotate) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[2 * i] = bf16_lo(w[i]);
+      y[2 * i + 1] = bf16_hi(w[i]);
+    }
+    return;
+  }
+  uint32_t o[4];
+  if (A.pairs) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = w[i] << 16 | w[i] >> 16;
+  } else {
+    const uint4 other = other_half<D>(A, own, c);
+    o[0] = other.x; o[1] = other.y; o[2] = other.z; o[3] = other.w;
+  }
+  const uint32_t turned = 8 * c < A.rot ? 0xffffffffu : 0u;  // (else cos 1 and sin 0, and nothing that 0 could make a NaN of)
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float a = bf16_lo(w[i]), b = bf16_hi(w[i]);
-    const float pa = A.pairs ? b : bf16_lo(o[i]), pb = A.pairs ? a : bf16_hi(o[i]);
-    y[2 * i] = turned ? fmaf(a, t.cos[2 * i], pa * t.sin[2 * i]) : a;
-    y[2 * i + 1] = turned ? fmaf(b, t.cos[2 * i + 1], pb * t.sin[2 * i + 1]) : b;
+    const uint32_t x = o[i] & turned;
+    y[2 * i] = fmaf(bf16_lo(w[i]), t.cos[2 * i], bf16_lo(x) * t.sin[2 * i]);
+    y[2 * i + 1] = fmaf(bf16_hi(w[i]), t.cos[2 * i + 1], bf16_hi(x) * t.sin[2 * i + 1]);
   }
 }
 
@@ -211,7 +226,7 @@ __device__ __forceinline__ void summary_tile(const WriteArgs& A, int b, int kvh0
       if (item > 0) __syncthreads();
       make_turns<D>(A, turns, tile_lo + p * TT, TT, first, end);
       __syncthreads();
-      if (8 * c < A.rot) lt = lane_turns(A, turns[r], c);
+      lt = lane_turns(A, turns[r], c);
     }
     const Row row = next;
     const int row_blk = blk;
@@ -282,9 +297,10 @@ __device__ __forceinline__ void summary_tile(const WriteArgs& A, int b, int kvh0
 
 // One launch for everything a write does.  The first k_jobs workgroups of a sequence each take a tile of whole blocks of some KV
 // heads' K rows, with their summaries; the others take the remaining rows (q, V, and K without summaries), tokens of a tile times heads.
-// What bounds it: prompts the bytes (2 x 16K tokens of 32 + 2 x 8 heads into e2m1, 707 MB, 171 us = 4.1 TB/s, a copy runs at 4.8), single
-// tokens the chain first -> block-table entry -> old rows of the block -> its summary (4.2 us for one, 5.9 for 32).  With one row of a
-// thread under way instead of four, and the partner columns loaded a second time instead of fetched from their lane, 247 us.
+// Every workgroup's rows are of one kind, so that source, stride and rotation are scalars.
+// What bounds it: prompts the bytes (2 x 16K tokens of 32 + 2 x 8 heads into e2m1, 707 MB, 152 us = 4.65 TB/s, a copy runs at 4.8; the vector
+// units are busy 60 % of it), single tokens the chain first -> block-table entry -> old rows of the block -> its summary (4.1 us
+// for one, 5.6 for 32).
 template <int D, int FMT, bool PAGED>
 __global__ __launch_bounds__(kWriteThreads) void write_kernel(WriteArgs A) {
   constexpr int LPR = D / 8, TT = kWriteThreads / LPR;
@@ -306,47 +322,48 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(WriteArgs A) {
     return;
   }
   x -= A.k_jobs;
-  const int at = x / A.row_groups, group = x - at * A.row_groups;
+  // groups of q heads, of KV heads for K (without summaries), of KV heads for V
+  const int at = x / A.row_groups;
+  int group = x - at * A.row_groups;
+  const bool is_q = group < A.q_groups;
+  if (!is_q) group -= A.q_groups;
+  const bool is_v = !is_q && group >= A.row_groups - A.q_groups - A.v_groups;
+  if (is_v) group -= A.row_groups - A.q_groups - A.v_groups;
+  const bool turned = !is_v && A.rot > 0;
   const int tokens = 1 << A.row_tokens_shift, per_pass = TT >> A.row_tokens_shift;
-  const int j0 = at << A.row_tokens_shift, t = r & (tokens - 1);
+  const int j0 = at << A.row_tokens_shift, t = r & (tokens - 1), tok = first + j0 + t;
   if (first + j0 >= end) return;
-  const int n_q = A.out_q ? A.Hq : 0, n_k = A.k_jobs ? 0 : A.Hkv, heads = n_q + n_k + A.Hkv;
-  const int h0 = group * A.row_passes * per_pass;
-  if (A.rot > 0 && h0 < n_q + n_k) {
-    make_turns<D>(A, turns, first + j0, tokens, first, end);
-    __syncthreads();
-  }
-  const int tok = first + j0 + t;
-  if (tok >= end) return;
-  const int blk = row_block<PAGED>(A.M, b, tok);
-  const int64_t src_row = (int64_t)b * A.n_new + j0 + t;
-  auto row_of = [&](int h) {
-    if (h < n_q) return A.q + src_row * A.q_stride + h * D;
-    if (h < n_q + n_k) return A.k_new + src_row * A.k_stride + (h - n_q) * D;
-    return A.v_new + src_row * A.v_stride + (h - n_q - n_k) * D;
-  };
+  const int heads = is_q ? A.Hq : A.Hkv, h0 = group * A.row_passes * per_pass;
+  const int64_t src_row = (int64_t)b * A.n_new + j0 + t, stride = is_q ? A.q_stride : is_v ? A.v_stride : A.k_stride;
+  int h = h0 + (r >> A.row_tokens_shift);
+  const uint16_t* src = (is_q ? A.q : is_v ? A.v_new : A.k_new) + src_row * stride + h * D + 8 * c;
+  uint16_t* dst = A.out_q + (src_row * A.Hq + h) * D + 8 * c;  // (q)
+  const int left = min(A.row_passes, (heads - h + per_pass - 1) / per_pass);  // rows of this lane
   // kAhead heads' rows under way at a time; the turns of the lane's columns stay in registers.
-  LaneTurns lt = {};
-  if (A.rot > 0 && h0 < n_q + n_k && 8 * c < A.rot) lt = lane_turns(A, turns[t], c);
-  for (int p = 0; p < A.row_passes; p += kAhead) {
-    const int h = h0 + p * per_pass + (r >> A.row_tokens_shift);
-    uint4 part[kAhead];
+  uint4 part[kAhead];
+  auto load = [&](int p) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-      if (p + u < A.row_passes && h + u * per_pass < heads) part[u] = load_part(row_of(h + u * per_pass), c);
+      if (tok < end && p + u < left) part[u] = *reinterpret_cast<const uint4*>(src + (p + u) * per_pass * D);
+  };
+  load(0);
+  const int blk = is_q ? 0 : row_block<PAGED>(A.M, b, min(tok, end - 1));
+  LaneTurns lt = {};
+  if (turned) {
+    make_turns<D>(A, turns, first + j0, tokens, first, end);
+    __syncthreads();
+    lt = lane_turns(A, turns[t], c);
+  }
+  if (tok >= end) return;
+  for (int p = 0; p < left; p += kAhead) {
+    if (p > 0) load(p);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int hu = h + u * per_pass;
-      if (p + u >= A.row_passes || hu >= heads) break;
+      if (p + u >= left) break;
       float y[8];
-      if (hu < n_q) {
-        rotated<D>(A, part[u], c, true, lt, y);
-        *reinterpret_cast<uint4*>(A.out_q + (src_row * A.Hq + hu) * D + 8 * c) = packed(y);
-      } else {
-        const bool is_k = hu < n_q + n_k;
-        rotated<D>(A, part[u], c, is_k && A.rot > 0, lt, y);
-        store_row<D, FMT>(is_k ? A.k : A.v, A.scale_off, row_at<PAGED>(A.M, b, is_k ? hu - n_q : hu - n_q - n_k, tok, blk), c, y);
-      }
+      rotated<D>(A, part[u], c, turned, lt, y);
+      if (is_q) *reinterpret_cast<uint4*>(dst + (p + u) * per_pass * D) = packed(y);
+      else store_row<D, FMT>(is_v ? A.v : A.k, A.scale_off, row_at<PAGED>(A.M, b, h + (p + u) * per_pass, tok, blk), c, y);
     }
   }
 }
@@ -461,10 +478,12 @@ hipError_t launch_write(const Plan& pl, const void* q, const void* k_new, const 
     A.k_jobs = tiles * A.k_groups;
   }
   while ((1 << A.row_tokens_shift) < std::min(n_new, kRowTokens)) ++A.row_tokens_shift;
-  const int heads = (out_q ? A.Hq : 0) + (summary ? 0 : A.Hkv) + A.Hkv, per_pass = tokens >> A.row_tokens_shift;
-  const int passes = (heads + per_pass - 1) / per_pass, tiles = (n_new + (1 << A.row_tokens_shift) - 1) >> A.row_tokens_shift;
-  A.row_passes = std::max(1, std::min({8, passes, (int)((int64_t)batch * tiles * passes / (8 * pl.num_cus))}));
-  A.row_groups = (passes + A.row_passes - 1) / A.row_passes;
+  const int per_pass = tokens >> A.row_tokens_shift, tiles = (n_new + (1 << A.row_tokens_shift) - 1) >> A.row_tokens_shift;
+  const int q_passes = out_q ? (A.Hq + per_pass - 1) / per_pass : 0, kv_passes = (A.Hkv + per_pass - 1) / per_pass;
+  A.row_passes = std::max(1, std::min({8, std::max(q_passes, kv_passes), (int)((int64_t)batch * tiles * (q_passes + kv_passes) / (8 * pl.num_cus))}));
+  A.q_groups = (q_passes + A.row_passes - 1) / A.row_passes;
+  A.v_groups = (kv_passes + A.row_passes - 1) / A.row_passes;
+  A.row_groups = A.q_groups + A.v_groups + (summary ? 0 : A.v_groups);
   const dim3 grid(A.k_jobs + tiles * A.row_groups, batch);
   return with_format(pl, [&](auto d, auto fmt, auto paged) {
     hipLaunchKernelGGL((write_kernel<d(), fmt(), paged()>), grid, dim3(kWriteThreads), 0, st, A);
