@@ -503,9 +503,9 @@ __device__ __forceinline__ void attend_again(const AttendArgs& A, int64_t vb, in
 #pragma unroll
   for (int o = LPR; o < kWave; o <<= 1) all = fmaxf(all, __shfl_xor(all, o));
   const float f = m == -INFINITY ? 0.f : m == all ? 1.f : __builtin_amdgcn_exp2f(m - all);
-  l = f == 0.f ? 0.f : l * f;
+  l *= f;
 #pragma unroll
-  for (int c = 0; c < 8; ++c) acc[c] = f == 0.f ? 0.f : acc[c] * f;
+  for (int c = 0; c < 8; ++c) acc[c] *= f;
 #pragma unroll
   for (int o = LPR; o < kWave; o <<= 1) {
     l += __shfl_xor(l, o);
@@ -544,16 +544,19 @@ __global__ __launch_bounds__(kAttendThreads) void attend_merge_kernel(AttendArgs
 #pragma unroll
   for (int u = 0; u < kAhead; ++u) first[u] = p[min(part + u * PARTS, A.splits - 1) * D];
   float m = wave_max(fmaxf(x0.x, x1.x));
-  auto weight_of = [&](float x) { return x == -INFINITY ? 0.f : x == m ? 1.f : __builtin_amdgcn_exp2f(x - m); };
-  const float w0 = weight_of(x0.x), w1 = weight_of(x1.x);
-  float l = wave_sum_f32((w0 != 0.f ? x0.y * w0 : 0.f) + (w1 != 0.f ? x1.y * w1 : 0.f)), a = 0.f;
-  // (pieces without a token, whose sums nobody wrote, have weight 0)
+  // (pieces without a token, whose sums nobody wrote, do not count; one whose weight is 0 does, for the sake of an Inf or a NaN in it)
+  auto counts = [](float2 x) { return x.x > -INFINITY; };
+  auto weight_of = [&](float2 x) { return !counts(x) ? 0.f : x.x == m ? 1.f : __builtin_amdgcn_exp2f(x.x - m); };
+  const float w0 = weight_of(x0), w1 = weight_of(x1);
+  const uint64_t there0 = __ballot(counts(x0)), there1 = __ballot(counts(x1));
+  float l = wave_sum_f32((counts(x0) ? x0.y * w0 : 0.f) + (counts(x1) ? x1.y * w1 : 0.f)), a = 0.f;
   auto weight = [&](int s) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s < kWave ? w0 : w1), s & (kWave - 1))); };
+  auto there = [&](int s) { return s < A.splits && ((s < kWave ? there0 : there1) >> (s & (kWave - 1)) & 1u); };
   const int wave_part = __builtin_amdgcn_readfirstlane(part);
 #pragma unroll
   for (int u = 0; u < kAhead; ++u) {
     const int s = wave_part + u * PARTS;
-    if (s < A.splits && weight(s) != 0.f) a += first[u] * weight(s);
+    if (there(s)) a += first[u] * weight(s);
   }
   for (int s0 = wave_part + kAhead * PARTS; s0 < A.splits; s0 += kAhead * PARTS) {
     float more[kAhead];
@@ -562,7 +565,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_merge_kernel(AttendArgs
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int s = s0 + u * PARTS;
-      if (s < A.splits && weight(s) != 0.f) a += more[u] * weight(s);
+      if (there(s)) a += more[u] * weight(s);
     }
   }
   s_acc[part][c] = a;

@@ -403,14 +403,14 @@ def _check_attention(s, q, lens, lists, o, lse):
             for t in range(s.q_len):
                 toks = lists[b * s.q_len + t][h]
                 for x in range(g):
-                    with np.errstate(invalid="ignore"):
+                    with np.errstate(invalid="ignore", over="ignore"):
                         want, total = co.attend(qh[b, t, h * g + x], k[toks], v[toks], scale)
                     got, at = oh[b * s.q_len + t, h * g + x], (b, t, h * g + x)
                     ok = np.isfinite(want)
                     assert np.array_equal(got[~ok], want[~ok], equal_nan=True), at
                     size = np.linalg.norm(want[ok])
                     # 32-bit scores and weights: as vatt_dense_decode
-                    assert np.linalg.norm((got - want)[ok]) <= 2e-5 * size, at
+                    assert np.linalg.norm(got[ok] - want[ok]) <= 2e-5 * size, at
                     if math.isfinite(total):
                         assert abs(lh[b * s.q_len + t, h * g + x] - total) <= 2e-5 * max(1.0, abs(total)), at
                     else:
@@ -561,6 +561,23 @@ def test_groups_that_are_nan_reach_only_the_queries_that_see_them(fmt, q_len):
             s.set_row(s.k, 1, h, tok, scales=odd)
     q = _bf16(s.rng.normal(size=(2, q_len, 8, 128)))
     _check_attention(s, q, lens, [[np.arange(n)] * 2 for n in _seen(s, lens)], *_dense(s, q, lens))
+
+
+@pytest.mark.parametrize("q_len", [1, 6])
+def test_a_key_that_is_nan_alone_in_its_piece(q_len):
+    """The newest token behind a whole number of 128, and 128 tokens in a row: no other score stands beside theirs."""
+    odd = np.full(4, 255, dtype=np.uint8)
+    for n, toks in ((257, [256]), (600, range(256, 384)), (1, [0])):
+        s = Setup(2, 4, 2, 128, 600, 0, 1, 16, q_len, seed=7, topk_frac=1.0)
+        lens, cap = [n, 600], s.vb.vatt_block_list_capacity(s.plan)
+        for tok in toks:
+            for h in range(2):
+                s.set_row(s.k, 0, h, tok, scales=odd)
+        q = _bf16(s.rng.normal(size=(2, q_len, 4, 128)))
+        lists = [[np.arange(m)] * 2 for m in _seen(s, lens)]
+        _check_attention(s, q, lens, lists, *_dense(s, q, lens))
+        blocks = torch.arange(cap, dtype=torch.int32, device="cuda").expand(2 * q_len, 2, -1).contiguous()
+        _check_attention(s, q, lens, lists, *_block_decode(s, q, lens, blocks, s.ints([[cap] * 2] * (2 * q_len))))
 
 
 def test_scores_far_apart():
