@@ -76,15 +76,23 @@ class Setup:
 
     def rows(self, buf, b, h, tokens):
         """Values of rows, [len(tokens), d]."""
-        host = buf.cpu().numpy()
-        out = np.zeros((len(tokens), self.d))
-        for i, tok in enumerate(tokens):
-            codes, scales = self.raw(host, b, h, int(tok))
-            if self.fmt == co.BF16:
-                out[i] = torch.from_numpy(codes.copy()).view(torch.bfloat16).double().numpy()
-            else:
-                out[i] = co.decode(co.unpack(codes, self.fmt), scales, self.fmt)
-        return out
+        tokens = np.asarray(list(tokens), dtype=np.int64)
+        if self.page:
+            table = self.table.cpu().numpy().astype(np.int64)
+            at = (table[b][tokens // self.page] * self.hkv + h) * self.page + tokens % self.page
+            scale_at = at
+        else:
+            at, scale_at = (b * self.hkv + h) * self.n_max + tokens, (b * self.hkv + h) * ((self.n_max + 7) // 8 * 8) + tokens
+        host, off = buf.cpu().numpy(), self.vb.vatt_kv_scale_offset(self.plan)
+        size = {0: 2 * self.d, 1: self.d, 2: self.d // 2}[self.fmt]
+        codes = host[:off // size * size].reshape(-1, size)[at]
+        if self.fmt == co.BF16:
+            return (np.ascontiguousarray(codes).view(np.uint16).astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+        scales = host[off:].reshape(-1, self.d // 32)[scale_at].astype(np.float64)
+        if self.fmt == co.E2M1:
+            codes = np.stack([codes & 15, codes >> 4], -1).reshape(len(tokens), self.d)
+        unit = np.where(scales == 255, math.nan, 2.0 ** (scales - 127))
+        return co.code_values(self.fmt)[codes] * np.repeat(unit, 32, axis=1)
 
     def set_row(self, buf, b, h, tok, codes=None, scales=None, values=None):
         size = {0: 2 * self.d, 1: self.d, 2: self.d // 2}[self.fmt]
@@ -136,6 +144,8 @@ WRITES = [
     (4, 2, 1, 128, 60, 32, 0, 32, 3, [-1, 60, 59, 8], None, dict(theta=1e4), True),                      # sequences out of range
     (2, 4, 2, 128, 513, 0, 1, 128, 400, [100, 5], None, None, False),                                    # no rotation
     (33, 4, 2, 64, 40, 8, 1, None, 1, list(range(33)), None, dict(theta=1e4), True),
+    (1, 2, 1, 128, 170752, 0, 0, 16, 3, [170749], None, dict(theta=500000.0), False),                    # the furthest positions
+    (1, 2, 1, 64, 170752, 64, 2, 32, 40, [170730], None, dict(theta=1e4, layout=1), True),
 ]
 
 
@@ -314,6 +324,8 @@ SELECTS = [
     (2, 16, 8, 64, 5000, 0, 16, 5, [5000, 4097], dict(topk_frac=0.02)),
     (2, 4, 2, 128, 640, 16, 16, 1, [640, 639], dict(topk_frac=0.0)),
     (1, 2, 2, 64, 640, 16, 16, 1, [640], dict(topk_frac=1.0)),
+    (2, 2, 1, 64, 40000, 64, 16, 1, [40000, 39000], dict(topk_frac=0.02)),      # rows of more than 2048 blocks
+    (1, 8, 1, 128, 170752, 0, 16, 2, [170752], dict(topk_frac=0.01)),          # the largest capacity
 ]
 
 
@@ -444,7 +456,7 @@ DENSE = [
     (2, 4, 2, 128, 300, 8, 1, 17, [300, 40]), (1, 8, 1, 128, 200, 32, 2, 12, [199]), (1, 4, 1, 64, 3001, 0, 1, 1, [3001]),
     (1, 2, 1, 128, 9000, 256, 2, 1, [8999]), (2, 2, 2, 128, 150, 0, 1, 3, [150, 2]), (1, 2, 2, 64, 99, 0, 2, 5, [99]),
     (2, 4, 2, 128, 350, 16, 2, 3, [350, 64]), (1, 1, 1, 64, 300, 0, 1, 7, [300]), (2, 8, 1, 128, 290, 0, 1, 1, [290, 65]),
-    (1, 1, 1, 128, 200, 32, 2, 9, [197]), (40, 2, 1, 64, 64, 16, 1, 1, [1 + (i * 37) % 64 for i in range(40)]),
+    (1, 1, 1, 128, 200, 32, 2, 9, [197]), (1, 2, 1, 64, 170752, 0, 1, 1, [170751]), (1, 4, 1, 64, 170752, 64, 2, 1, [170752]), (40, 2, 1, 64, 64, 16, 1, 1, [1 + (i * 37) % 64 for i in range(40)]),
 ]
 
 
