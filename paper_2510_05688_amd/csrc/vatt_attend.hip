@@ -59,7 +59,9 @@ __device__ __forceinline__ int token_of(const TokenList& L, int group, int blk) 
   if (group >= L.count) return kNowhere;
   if (!L.blocks) return group * 8;
   if ((uint32_t)blk > (uint32_t)(L.n - 1) >> L.shift) return kNowhere;
-  return (blk << L.shift) + ((group << 3) & ((1 << L.shift) - 1));
+  // (nor is there a group behind the last token of the last block: a contiguous cache has no scales for it)
+  const int tok = (blk << L.shift) + ((group << 3) & ((1 << L.shift) - 1));
+  return tok < L.n ? tok : kNowhere;
 }
 
 // STREAM: read once.  All tokens' rows are, those of lists may be in the lists of several query tokens (16 x 32K tokens in e4m3 192 us

@@ -475,6 +475,8 @@ BLOCKS = [
     (2, 4, 4, 128, 640, 16, 2, 16, 2, [640, 333], {}), (1, 16, 2, 128, 2000, 0, 1, 64, 1, [1999], dict(topk_frac=1.0)),
     (2, 4, 1, 64, 1000, 0, 2, 256, 1, [1000, 255], dict(topk_frac=0.9)), (1, 4, 2, 128, 8192, 256, 0, 256, 1, [8001], dict(topk_frac=1.0)),
     (3, 2, 2, 64, 333, 0, 0, 16, 1, [333, 332, 9], dict(sm_scale=0.3)),
+    # the last block goes on behind the cache's last row, and behind its last scales
+    (1, 2, 1, 128, 33, 0, 1, 256, 1, [33], {}), (2, 4, 2, 64, 41, 0, 2, 64, 1, [41, 40], {}), (1, 8, 1, 128, 8, 0, 2, 16, 2, [8], {}),
 ]
 
 
