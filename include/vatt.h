@@ -412,8 +412,8 @@ int vatt_plan_set_rotary(vatt_plan* plan, const vatt_rotary* rotary);
  *   summary      device or NULL: the summaries of every block that gets a token become those of the sequence as it now is (whatever they
  *                were: a sequence may be cut back by writing from an earlier position)
  *   out_q        device, bf16 [B, n_new, Hq, d]; needs a rotation
- *   out_lens     device, int32 [B] or NULL: the sequences' new lengths, first[b] + tokens written; not the buffer `first`, which
- *                workgroups of the call still read
+ *   out_lens     device, int32 [B] or NULL: the sequences' new lengths, first[b] + tokens written; neither of the buffers `first` and
+ *                `new_lens`, which workgroups of the call still read
  * No output may overlap an input.  Pointers 16-byte aligned (lengths: 4).  Errors as in vatt_decode.
  */
 int vatt_write_kv(vatt_plan* plan, const void* q, const void* k_new, const void* v_new, int64_t q_stride, int64_t k_stride,

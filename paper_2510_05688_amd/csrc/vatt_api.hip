@@ -764,7 +764,7 @@ int vatt_write_kv(vatt_plan* plan, const void* q, const void* k_new, const void*
   if (!q != !out_q || (q && (pl.rotary_dim == 0 || q == out_q))) return VATT_E_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k) || !aligned16(v) || !aligned16(summary) || !aligned16(out_q))
     return VATT_E_INVALID_ARG;
-  if (n_new < 1 || n_new > pl.p.n_max || out_lens == first) return VATT_E_INVALID_ARG;
+  if (n_new < 1 || n_new > pl.p.n_max || out_lens == first || (out_lens && out_lens == new_lens)) return VATT_E_INVALID_ARG;
   const int64_t q_row = (int64_t)pl.p.n_q_heads * pl.p.head_dim, kv_row = (int64_t)pl.p.n_kv_heads * pl.p.head_dim;
   if ((q && (q_stride < q_row || q_stride % 8 != 0)) || k_stride < kv_row || k_stride % 8 != 0 || v_stride < kv_row || v_stride % 8 != 0)
     return VATT_E_INVALID_ARG;

@@ -138,7 +138,7 @@ def test_refusals_of_write():
     for over in (dict(k_new=None), dict(v_new=None), dict(first=None), dict(k=None), dict(v=None), dict(k_new=Mem(4104)), dict(v=Mem(4100)),
                  dict(n_new=0), dict(n_new=1001), dict(k_stride=248), dict(k_stride=260), dict(v_stride=255), dict(v_stride=0),
                  dict(q=Mem()), dict(out_q=Mem()), dict(q, q_stride=1016), dict(q, q_stride=1028), dict(q, out_q=q["q"]),
-                 dict(summary=Mem(4098)), dict(first=Mem(64), out_lens=Mem(64))):
+                 dict(summary=Mem(4098)), dict(first=Mem(64), out_lens=Mem(64)), dict(new_lens=Mem(64), out_lens=Mem(64))):
         assert _status(_write, plan, **over) == ARG, over
     vb.vatt_plan_set_rotary(plan, None)
     assert _status(_write, plan, **q) == ARG  # queries are only rotated
