@@ -59,6 +59,7 @@ class DecodeSession:
         self.dense_lse = torch.empty(self.B, self.Hq, dtype=torch.float32, device=dev)
         self.block_table: Optional[torch.Tensor] = None
         self.q = self.k = self.v = self.seq_lens = self.seq_seeds = None
+        self.summary = self.blocks = self.block_count = None
 
     def close(self):
         if self.plan:
@@ -80,6 +81,7 @@ class DecodeSession:
         self.seq_lens = torch.from_numpy(np.ascontiguousarray(seq_lens, dtype=np.int32)).to(dev)
         self.seq_seeds = torch.from_numpy(np.ascontiguousarray(seeds, dtype=np.uint64).view(np.int64)).to(dev)
         self.block_table = None
+        self.summary = self.blocks = self.block_count = None  # (of make_cache's cache only)
         if block_table is not None:
             self.block_table = torch.from_numpy(np.ascontiguousarray(block_table, dtype=np.int32)).to(dev)
         return self
@@ -173,7 +175,6 @@ class DecodeSession:
         if block_table is not None:
             self.block_table = torch.from_numpy(np.ascontiguousarray(block_table, dtype=np.int32)).to(dev)
         self.seq_lens = torch.zeros(self.params["batch"], dtype=torch.int32, device=dev)
-        self._next_lens = torch.zeros_like(self.seq_lens)
         self.block_capacity = vb.vatt_block_list_capacity(self.plan)
         self.summary = self.blocks = self.block_count = None
         if self.block_capacity:
@@ -184,12 +185,20 @@ class DecodeSession:
 
     def write(self, q, k_new, v_new, new_lens=None):
         """Appends the tokens k_new, v_new (bf16 [B, n_new, Hkv, d], as far as new_lens says) to every sequence; returns the
-        rotated queries (bf16 [B, n_new, Hq, d]) or None without q."""
+        rotated queries (bf16 [B, n_new, Hq, d]) or None without q.  seq_lens stays the same tensor, so that a captured write
+        goes on where the last replay ended."""
+        for x, heads in ((q, self.Hq), (k_new, self.Hkv), (v_new, self.Hkv)):
+            want = (self.params["batch"], k_new.shape[1], heads, self.d)
+            if x is not None and (x.shape != want or x.dtype != torch.bfloat16 or x.device != self.device):
+                raise ValueError(f"expected bfloat16 {want} on {self.device}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+        if new_lens is not None and (new_lens.numel() != self.params["batch"] or new_lens.dtype != torch.int32 or new_lens.device != self.device):
+            raise ValueError(f"new_lens: one int32 per sequence on {self.device}")
         out_q = None if q is None else torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
+        lens = torch.empty_like(self.seq_lens)
         vb.vatt_write_kv(self.plan, q, k_new, v_new, 0 if q is None else vb.token_stride(q), vb.token_stride(k_new),
                          vb.token_stride(v_new), k_new.shape[1], self.seq_lens, new_lens, self.k, self.v, self.block_table,
-                         self.summary, out_q, self._next_lens, self._stream())
-        self.seq_lens, self._next_lens = self._next_lens, self.seq_lens
+                         self.summary, out_q, lens, self._stream())
+        self.seq_lens.copy_(lens)
         return out_q
 
     def read_rows(self, first, n_rows: int):

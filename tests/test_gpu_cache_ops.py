@@ -778,6 +778,58 @@ def test_a_session(fmt):
     sess.close()
 
 
+def test_a_session_captured():
+    """A token's write, choice and attention through DecodeSession, captured once: every replay goes on where the last one ended."""
+    from paper_2510_05688_amd.session import DecodeSession
+    s = Setup(2, 8, 2, 128, 256, 32, 1, 32, rotary=dict(theta=10000.0), seed=21, topk_frac=0.4)
+    table = s.table.cpu().numpy()
+    one, two = (DecodeSession(s.params, kv_format=1, block_tokens=32, rotary=dict(theta=10000.0)).make_cache(table) for _ in range(2))
+    x = [_bf16(s.rng.normal(size=(2, 150, h, 128))) for h in (8, 2, 2)]
+    now = [t[:, :1].clone() for t in x]
+
+    def step(sess):
+        q = sess.write(*now)
+        sess.select_blocks(q)
+        sess.block_decode(q)
+
+    for sess in (one, two):
+        sess.write(*x, s.ints([150, 93]))
+        step(sess)
+    lens = one.seq_lens
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(one)
+    assert one.seq_lens is lens and lens.tolist() == [151, 94]
+    for i in range(4):
+        for t in now:
+            t.copy_(_bf16(s.rng.normal(size=tuple(t.shape))))
+        graph.replay()
+        step(two)
+        torch.cuda.synchronize()
+        assert lens.tolist() == two.seq_lens.tolist() == [152 + i, 95 + i]
+        for name in ("k", "v", "summary", "blocks", "block_count", "out_o", "out_lse"):
+            a, b = getattr(one, name), getattr(two, name)
+            if name == "blocks":  # (what lies behind a list is as it was)
+                there = torch.arange(a.shape[-1], device="cuda") < one.block_count[..., None]
+                a, b = a[there], b[there]
+            assert torch.equal(a, b), name
+
+
+def test_a_session_refuses_other_shapes_and_types():
+    from paper_2510_05688_amd.session import DecodeSession
+    s = Setup(2, 8, 2, 128, 64, 0, 0, 16, seed=22)
+    sess = DecodeSession(s.params, rotary=dict(theta=10000.0)).make_cache()
+    q, kv = (torch.zeros(2, 3, h, 128, dtype=torch.bfloat16, device="cuda") for h in (8, 2))
+    for bad in ((q, kv[:1], kv), (q, kv, kv[..., :64]), (q, kv, kv[:, :2]), (q[:, :2], kv, kv), (q[:, :, :4], kv, kv), (q.float(), kv, kv),
+                (q, kv.cpu(), kv)):
+        with pytest.raises(ValueError):
+            sess.write(*bad)
+    for bad in (s.ints([1]), s.ints([1, 1]).long(), s.ints([1, 1]).cpu()):
+        with pytest.raises(ValueError):
+            sess.write(q, kv, kv, bad)
+    assert sess.seq_lens.tolist() == [0, 0]
+
+
 def test_calls_for_bf16_caches_refuse_others():
     s = Setup(1, 4, 2, 128, 64, 0, 1)
     vb, x, i, z = s.vb, torch.zeros(1 << 16, device="cuda"), s.ints([1]), torch.zeros(1, dtype=torch.int64, device="cuda")
