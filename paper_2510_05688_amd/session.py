@@ -4,6 +4,7 @@ No arithmetic of the method happens here; every call goes straight to the C ABI.
 """
 from __future__ import annotations
 
+import math
 from typing import Dict, Optional
 
 import numpy as np
@@ -201,20 +202,41 @@ class DecodeSession:
         self.seq_lens.copy_(lens)
         return out_q
 
+    def _check(self, name, x, dtype, *shape):
+        """A kernel gets x as an address: x has to be a tensor of so many values, one behind the other, on this device (None is left to
+        the call)."""
+        if x is None:
+            return
+        if not isinstance(x, torch.Tensor):
+            raise ValueError(f"{name}: expected a tensor, got {type(x).__name__}")
+        if x.numel() != math.prod(shape) or x.dtype != dtype or x.device != self.device or not x.is_contiguous():
+            raise ValueError(f"{name}: expected contiguous {dtype} {shape} on {self.device}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+
+    def _query(self, q):
+        if q is None:
+            return self.q
+        self._check("q", q, torch.bfloat16, self.B, self.Hq, self.d)
+        return q
+
     def read_rows(self, first, n_rows: int):
-        """(K, V) rows first[b] .. first[b] + n_rows - 1 in bf16 [B, Hkv, n_rows, d]; zeros where a sequence has none."""
+        """(K, V) rows first[b] .. first[b] + n_rows - 1 in bf16 [B, Hkv, n_rows, d]; zeros where a sequence has none.  first: int32 [B]
+        on the device, None for 0."""
+        self._check("first", first, torch.int32, self.params["batch"])
         out = [torch.zeros(self.params["batch"], self.Hkv, n_rows, self.d, dtype=torch.bfloat16, device=self.device) for _ in range(2)]
         vb.vatt_read_kv(self.plan, self.k, self.v, self.block_table, self.seq_lens, first, n_rows, out[0], out[1], self._stream())
         return out
 
     def select_blocks(self, q=None, topk_idx=None, topk_cnt=None):
         """Fills self.blocks and self.block_count (and the token lists for decode_given_topk, if given)."""
-        vb.vatt_select_blocks(self.plan, self.q if q is None else q, self.summary, self.block_table, self.seq_lens, self.workspace,
+        k_max = self.seg[3] - self.seg[2]
+        self._check("topk_idx", topk_idx, torch.int32, self.B, self.Hq, max(k_max, 1))  # (with none an entry that nobody writes)
+        self._check("topk_cnt", topk_cnt, torch.int32, self.B, self.Hq)
+        vb.vatt_select_blocks(self.plan, self._query(q), self.summary, self.block_table, self.seq_lens, self.workspace,
                               self.blocks, self.block_count, topk_idx, topk_cnt, self._stream())
 
     def block_decode(self, q=None):
         """Attention over the chosen blocks, into out_o and out_lse."""
-        vb.vatt_block_decode(self.plan, self.q if q is None else q, self.k, self.v, self.block_table, self.seq_lens, self.blocks,
+        vb.vatt_block_decode(self.plan, self._query(q), self.k, self.v, self.block_table, self.seq_lens, self.blocks,
                              self.block_count, self.workspace, self.out_o, self.out_lse, self._stream())
 
     # ---- read-back -----------------------------------------------------------

@@ -1,0 +1,72 @@
+"""What DecodeSession checks before a call goes to the library, without a GPU: nothing here may reach a kernel."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2510_05688_amd import session as sm
+
+
+class Calls:
+    """The binding with every call that would launch something written down instead."""
+
+    def __init__(self, monkeypatch, *names):
+        self.made = []
+        for name in names:
+            monkeypatch.setattr(sm.vb, name, lambda *a, _name=name, **kw: self.made.append((_name, a)))
+
+
+def _session(q_len=1, batch=2, hq=8, hkv=2, d=64, n_max=100, k_max=30, page=0):
+    """A session as its constructor leaves it, on the CPU: no plan, no workspace."""
+    s = sm.DecodeSession.__new__(sm.DecodeSession)
+    s.plan, s.device, s.q_len = None, torch.device("cpu"), q_len
+    s.params = dict(batch=batch, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, n_max=n_max, page_size=page)
+    s.B, s.Hq, s.Hkv, s.d, s.n_max, s.paged, s.seg = batch * q_len, hq, hkv, d, n_max, page > 0, [0, 4, 8, 8 + k_max, 60]
+    s.workspace = s.out_o = s.out_lse = s.k = s.v = s.q = s.seq_seeds = s.block_table = s.summary = s.blocks = s.block_count = None
+    s.seq_lens = torch.full((batch,), 50, dtype=torch.int32)
+    s._stream = lambda: 0
+    return s
+
+
+def _ints(*x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
+def test_rows_back_are_asked_for_by_one_int32_per_sequence(monkeypatch):
+    calls, s = Calls(monkeypatch, "vatt_read_kv"), _session()
+    for bad in (5, 0, [1, 2], np.array([1, 2], dtype=np.int32), _ints(1), _ints(1, 2, 3), _ints(1, 2).long(), _ints(1, 0, 2, 0)[::2]):
+        with pytest.raises(ValueError):
+            s.read_rows(bad, 3)
+    assert not calls.made
+    s.read_rows(_ints(1, 2), 3)
+    s.read_rows(None, 3)
+    assert [name for name, _ in calls.made] == ["vatt_read_kv"] * 2
+
+
+@pytest.mark.parametrize("q_len", [1, 3])
+def test_queries_of_the_block_calls(monkeypatch, q_len):
+    calls, s = Calls(monkeypatch, "vatt_select_blocks", "vatt_block_decode"), _session(q_len)
+    q = torch.zeros(2, q_len, 8, 64, dtype=torch.bfloat16)
+    for call in (s.select_blocks, s.block_decode):
+        for bad in (4096, q[:1], q[..., :32], q[:, :, :4], q.float(), q.transpose(2, 3).contiguous().transpose(2, 3),
+                    torch.cat([q, q], 1), q.view(torch.int16), q.to("meta")):
+            with pytest.raises(ValueError):
+                call(bad)
+    assert not calls.made
+    s.select_blocks(q)
+    s.block_decode(q.view(2 * q_len, 8, 64))  # [B, Hq, d] as the plan's other calls have it
+    s.q = q
+    s.select_blocks()
+    s.block_decode()
+    assert [name for name, _ in calls.made] == ["vatt_select_blocks", "vatt_block_decode"] * 2
+
+
+def test_token_lists_of_the_choice(monkeypatch):
+    calls, s = Calls(monkeypatch, "vatt_select_blocks"), _session(2)
+    q, idx, cnt = torch.zeros(2, 2, 8, 64, dtype=torch.bfloat16), torch.zeros(4, 8, 30, dtype=torch.int32), torch.zeros(4, 8, dtype=torch.int32)
+    for a, b in ((idx[:2], cnt), (idx[..., :29], cnt), (idx.long(), cnt), (idx.to("meta"), cnt), (idx.mT.contiguous().mT, cnt),
+                 (idx, cnt[:3]), (idx, cnt.long()), (idx, cnt.to("meta")), (4096, cnt), (idx, 4096)):
+        with pytest.raises(ValueError):
+            s.select_blocks(q, a, b)
+    assert not calls.made
+    s.select_blocks(q, idx, cnt)
+    assert len(calls.made) == 1
