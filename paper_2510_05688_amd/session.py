@@ -220,7 +220,9 @@ class DecodeSession:
 
     def read_rows(self, first, n_rows: int):
         """(K, V) rows first[b] .. first[b] + n_rows - 1 in bf16 [B, Hkv, n_rows, d]; zeros where a sequence has none.  first: int32 [B]
-        on the device, None for 0."""
+        on the device, or one number for all (None: 0)."""
+        if isinstance(first, int):
+            first = torch.full((self.params["batch"],), first, dtype=torch.int32, device=self.device)
         self._check("first", first, torch.int32, self.params["batch"])
         out = [torch.zeros(self.params["batch"], self.Hkv, n_rows, self.d, dtype=torch.bfloat16, device=self.device) for _ in range(2)]
         vb.vatt_read_kv(self.plan, self.k, self.v, self.block_table, self.seq_lens, first, n_rows, out[0], out[1], self._stream())

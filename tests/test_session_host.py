@@ -33,13 +33,16 @@ def _ints(*x):
 
 def test_rows_back_are_asked_for_by_one_int32_per_sequence(monkeypatch):
     calls, s = Calls(monkeypatch, "vatt_read_kv"), _session()
-    for bad in (5, 0, [1, 2], np.array([1, 2], dtype=np.int32), _ints(1), _ints(1, 2, 3), _ints(1, 2).long(), _ints(1, 0, 2, 0)[::2]):
+    for bad in ([1, 2], 5.0, np.array([1, 2], dtype=np.int32), _ints(1), _ints(1, 2, 3), _ints(1, 2).long(), _ints(1, 0, 2, 0)[::2]):
         with pytest.raises(ValueError):
             s.read_rows(bad, 3)
     assert not calls.made
     s.read_rows(_ints(1, 2), 3)
     s.read_rows(None, 3)
-    assert [name for name, _ in calls.made] == ["vatt_read_kv"] * 2
+    for number in (0, 5):  # the same first row for all, never an address
+        s.read_rows(number, 3)
+    assert [name for name, _ in calls.made] == ["vatt_read_kv"] * 4
+    assert calls.made[1][1][5] is None and [calls.made[i][1][5].tolist() for i in (0, 2, 3)] == [[1, 2], [0, 0], [5, 5]]
 
 
 @pytest.mark.parametrize("q_len", [1, 3])
