@@ -34,7 +34,8 @@ class DecodeSession:
         self.q_len = int(q_len)
         self.plan = (vb.vatt_plan_create(self.params, device) if self.q_len == 1
                      else vb.vatt_plan_create_chunk(self.params, self.q_len, device))
-        vb.vatt_plan_set_option(self.plan, vb.VATT_OPT_KV_FORMAT, int(kv_format))
+        self.kv_format = int(kv_format)
+        vb.vatt_plan_set_option(self.plan, vb.VATT_OPT_KV_FORMAT, self.kv_format)
         if block_tokens is not None:
             vb.vatt_plan_set_option(self.plan, vb.VATT_OPT_BLOCK_TOKENS, int(block_tokens))
         if rotary is not None:
@@ -75,7 +76,12 @@ class DecodeSession:
 
     # ---- uploads -----------------------------------------------------------
     def upload(self, q_bits, k_bits, v_bits, seq_lens, seeds, block_table=None):
+        """k_bits, v_bits: bf16 rows in the plan's layout; on a quantised plan codes and scales, vatt_kv_cache_bytes in all."""
         dev = self.device
+        if self.kv_format != vb.VATT_KV_BF16:
+            want = vb.vatt_kv_cache_bytes(self.plan)
+            if np.asarray(k_bits).nbytes != want or np.asarray(v_bits).nbytes != want:
+                raise ValueError(f"K and V of this plan's format have {want} bytes each, got {np.asarray(k_bits).nbytes} and {np.asarray(v_bits).nbytes}")
         self.q = _bf16_from_bits(q_bits, dev)
         self.k = _bf16_from_bits(k_bits, dev)
         self.v = _bf16_from_bits(v_bits, dev)

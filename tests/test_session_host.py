@@ -73,3 +73,27 @@ def test_token_lists_of_the_choice(monkeypatch):
     assert not calls.made
     s.select_blocks(q, idx, cnt)
     assert len(calls.made) == 1
+
+
+def test_an_upload_into_a_quantised_plan_has_its_bytes(monkeypatch):
+    """bf16 rows for a plan whose kernels read codes and scales would be taken for those, and can be shorter than the cache."""
+    p = dict(batch=1, n_q_heads=2, n_kv_heads=1, head_dim=64, n_max=1, kv_layout=0, page_size=0, num_blocks=0, sink=4, window=4, topk_abs=0,
+             topk_frac=0.1, base_abs=0, base_frac=0.1, epsilon=0.1, delta=0.1, target=0, sm_scale=0.0, budget_cap_frac=1.0)
+    for fmt, n_max in ((1, 1), (2, 1), (1, 50), (2, 77)):
+        s = _session(batch=1, hq=2, hkv=1, n_max=n_max)
+        s.plan, s.kv_format = sm.vb.vatt_plan_create(dict(p, n_max=n_max), -1), fmt
+        sm.vb.vatt_plan_set_option(s.plan, sm.vb.VATT_OPT_KV_FORMAT, fmt)
+        q, rows, size = np.zeros((1, 2, 64), np.uint16), np.zeros((1, 1, n_max, 64), np.uint16), sm.vb.vatt_kv_cache_bytes(s.plan)
+        whole = np.arange(size // 2, dtype=np.uint16)
+        for k, v in ((rows, rows), (whole, rows), (rows, whole), (whole[:-1], whole[:-1])):
+            with pytest.raises(ValueError):
+                s.upload(q, k, v, [1], [0])
+        assert s.q is None and s.k is None
+        s.upload(q, whole, whole, [1], [0])  # a cache that was written somewhere else
+        assert s.k.view(torch.int16).numpy().view(np.uint16).tolist() == whole.tolist()
+        s.close()
+    s = _session(batch=1, hq=2, hkv=1, n_max=50)
+    s.plan, s.kv_format = sm.vb.vatt_plan_create(dict(p, n_max=50), -1), 0
+    s.upload(np.zeros((1, 2, 64), np.uint16), *[np.zeros((1, 1, 50, 64), np.uint16)] * 2, [50], [0])
+    assert s.k.shape == (1, 1, 50, 64)
+    s.close()
