@@ -97,3 +97,31 @@ def test_an_upload_into_a_quantised_plan_has_its_bytes(monkeypatch):
     s.upload(np.zeros((1, 2, 64), np.uint16), *[np.zeros((1, 1, 50, 64), np.uint16)] * 2, [50], [0])
     assert s.k.shape == (1, 1, 50, 64)
     s.close()
+
+
+def _host_session(page=0, block=16, **over):
+    """A session with a plan that is of no device."""
+    p = dict(batch=2, n_q_heads=8, n_kv_heads=2, head_dim=64, n_max=100, kv_layout=1 if page else 0, page_size=page, num_blocks=30 if page else 0,
+             sink=4, window=4, topk_abs=0, topk_frac=0.3, base_abs=0, base_frac=0.1, epsilon=0.1, delta=0.1, target=0, sm_scale=0.0,
+             budget_cap_frac=1.0)
+    p.update(over)
+    s = _session(page=page)
+    s.plan, s.kv_format, s.params = sm.vb.vatt_plan_create(p, -1), 0, p
+    if block:
+        sm.vb.vatt_plan_set_option(s.plan, sm.vb.VATT_OPT_BLOCK_TOKENS, block)
+    return s
+
+
+def test_a_cache_on_pages_needs_its_whole_block_table():
+    s = _host_session(page=16)
+    table = np.arange(14, dtype=np.int32).reshape(2, 7)
+    for bad in (None, table[:1], table[:, :6], np.arange(13)):
+        with pytest.raises(ValueError):
+            s.make_cache(bad)
+    assert s.k is None and s.block_table is None
+    s.make_cache(table)
+    assert s.block_table.tolist() == table.tolist()
+    s.close()
+    s = _host_session().make_cache()
+    assert s.block_table is None
+    s.close()
