@@ -178,10 +178,10 @@ class DecodeSession:
         """Allocates an empty cache in the plan's format, summaries of its blocks and lists for the chosen ones.
         block_table: [B, ceil(n_max / page_size)] on a paged plan."""
         dev, rows = self.device, self.B
-        if self.paged:
+        if self.paged and block_table is not None:
             want = self.params["batch"] * -(-self.n_max // self.params["page_size"])
-            if block_table is None or np.size(block_table) != want:
-                raise ValueError(f"block_table: a paged plan's has {want} entries, got {None if block_table is None else np.shape(block_table)}")
+            if np.size(block_table) != want:
+                raise ValueError(f"block_table: a paged plan's has {want} entries, got {np.shape(block_table)}")
         self.k, self.v = (torch.zeros(vb.vatt_kv_cache_bytes(self.plan), dtype=torch.uint8, device=dev) for _ in range(2))
         self.block_table = None
         if block_table is not None:
