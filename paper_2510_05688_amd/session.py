@@ -60,7 +60,7 @@ class DecodeSession:
         self.dense_o = torch.empty(self.B, self.Hq, self.d, dtype=torch.float32, device=dev)
         self.dense_lse = torch.empty(self.B, self.Hq, dtype=torch.float32, device=dev)
         self.block_table: Optional[torch.Tensor] = None
-        self.q = self.k = self.v = self.seq_lens = self.seq_seeds = None
+        self.q = self.k = self.v = self.seq_lens = self.seq_seeds = self.rcache = self.cache_seeds = None
         self.summary = self.blocks = self.block_count = None
 
     def close(self):
@@ -182,6 +182,7 @@ class DecodeSession:
             want = self.params["batch"] * -(-self.n_max // self.params["page_size"])
             if np.size(block_table) != want:
                 raise ValueError(f"block_table: a paged plan's has {want} entries, got {np.shape(block_table)}")
+        self.q = self.seq_seeds = self.rcache = self.cache_seeds = None  # (of other sequences)
         self.k, self.v = (torch.zeros(vb.vatt_kv_cache_bytes(self.plan), dtype=torch.uint8, device=dev) for _ in range(2))
         self.block_table = None
         if block_table is not None:

@@ -115,7 +115,7 @@ def _host_session(page=0, block=16, **over):
 def test_a_cache_on_pages_needs_its_whole_block_table():
     s = _host_session(page=16)
     table = np.arange(14, dtype=np.int32).reshape(2, 7)
-    for bad in (None, table[:1], table[:, :6], np.arange(13)):
+    for bad in (table[:1], table[:, :6], np.arange(13)):
         with pytest.raises(ValueError):
             s.make_cache(bad)
     assert s.k is None and s.block_table is None
@@ -124,4 +124,15 @@ def test_a_cache_on_pages_needs_its_whole_block_table():
     s.close()
     s = _host_session().make_cache()
     assert s.block_table is None
+    s.close()
+
+
+def test_a_new_cache_leaves_nothing_of_the_last_one():
+    """Queries, seeds and the random cache of other sequences would be used without a word."""
+    s = _host_session()
+    s.upload(np.zeros((2, 8, 64), np.uint16), *[np.zeros((2, 2, 100, 64), np.uint16)] * 2, [5, 5], [1, 2])
+    s.rcache = s.cache_seeds = torch.zeros(1)
+    s.make_cache()
+    assert s.q is None and s.seq_seeds is None and s.rcache is None and s.cache_seeds is None
+    assert s.seq_lens.tolist() == [0, 0]
     s.close()
