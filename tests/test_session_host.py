@@ -136,3 +136,19 @@ def test_a_new_cache_leaves_nothing_of_the_last_one():
     assert s.q is None and s.seq_seeds is None and s.rcache is None and s.cache_seeds is None
     assert s.seq_lens.tolist() == [0, 0]
     s.close()
+
+
+def test_queries_of_tokens_that_are_not_written(monkeypatch):
+    """Padding, and tokens of a full sequence, which the call leaves as they were: zeros, not what lay in the memory."""
+    s, calls = _host_session(), []
+    s.make_cache()
+    monkeypatch.setattr(sm.vb, "vatt_write_kv", lambda *a: calls.append(a))
+    q, kv = torch.ones(2, 3, 8, 64, dtype=torch.bfloat16), torch.ones(2, 3, 2, 64, dtype=torch.bfloat16)
+    was = torch.are_deterministic_algorithms_enabled()
+    torch.use_deterministic_algorithms(True)  # (memory nobody has written is then NaN)
+    try:
+        out = s.write(q, kv, kv, _ints(1, 0))
+    finally:
+        torch.use_deterministic_algorithms(was)
+    assert calls and not out.any()
+    s.close()
