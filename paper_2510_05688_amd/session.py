@@ -198,14 +198,13 @@ class DecodeSession:
 
     def write(self, q, k_new, v_new, new_lens=None):
         """Appends the tokens k_new, v_new (bf16 [B, n_new, Hkv, d], as far as new_lens says) to every sequence; returns the
-        rotated queries (bf16 [B, n_new, Hq, d], zeros for tokens that are not written) or None without q.  seq_lens stays the same tensor, so that a captured write
-        goes on where the last replay ended."""
+        rotated queries (bf16 [B, n_new, Hq, d], zeros for tokens that are not written) or None without q.  seq_lens stays the
+        same tensor, so that a captured write goes on where the last replay ended."""
         for x, heads in ((q, self.Hq), (k_new, self.Hkv), (v_new, self.Hkv)):
             want = (self.params["batch"], k_new.shape[1], heads, self.d)
             if x is not None and (x.shape != want or x.dtype != torch.bfloat16 or x.device != self.device):
                 raise ValueError(f"expected bfloat16 {want} on {self.device}, got {x.dtype} {tuple(x.shape)} on {x.device}")
-        if new_lens is not None and (new_lens.numel() != self.params["batch"] or new_lens.dtype != torch.int32 or new_lens.device != self.device):
-            raise ValueError(f"new_lens: one int32 per sequence on {self.device}")
+        self._check("new_lens", new_lens, torch.int32, self.params["batch"])
         out_q = None if q is None else torch.zeros(q.shape, dtype=torch.bfloat16, device=self.device)
         lens = torch.empty_like(self.seq_lens)
         vb.vatt_write_kv(self.plan, q, k_new, v_new, 0 if q is None else vb.token_stride(q), vb.token_stride(k_new),

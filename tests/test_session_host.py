@@ -152,3 +152,15 @@ def test_queries_of_tokens_that_are_not_written(monkeypatch):
         torch.use_deterministic_algorithms(was)
     assert calls and not out.any()
     s.close()
+
+
+def test_lengths_of_new_tokens_lie_one_behind_the_other(monkeypatch):
+    s, calls = _host_session(), Calls(monkeypatch, "vatt_write_kv")
+    s.make_cache()
+    kv = torch.ones(2, 3, 2, 64, dtype=torch.bfloat16)
+    for bad in (_ints(1, 9, 2, 9)[::2], _ints(1).expand(2), _ints(1), _ints(1, 2).long(), 2):
+        with pytest.raises(ValueError):
+            s.write(None, kv, kv, bad)
+    assert not calls.made
+    s.write(None, kv, kv, _ints(1, 2))
+    s.close()
