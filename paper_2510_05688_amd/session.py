@@ -147,6 +147,7 @@ class DecodeSession:
     def append_device_cached(self, k_new, v_new):
         vb.vatt_append_kv_cached(self.plan, k_new, v_new, self.k, self.v, self.block_table, self.seq_lens,
                                  self.cache_seeds, self.rcache, self._stream())
+        self._renew_summary()
 
     def decode_given_topk_cached(self, topk_idx, topk_cnt, k=None, v=None):
         vb.vatt_decode_given_topk_cached(self.plan, self.q, self.k if k is None else k,
@@ -170,14 +171,16 @@ class DecodeSession:
         self.append_device(kn, vn)
 
     def append_device(self, k_new, v_new):
-        """Append one token per sequence from tensors that are already on the device (bf16 [B, Hkv, d])."""
+        """Append one token per sequence from tensors that are already on the device (bf16 [B, Hkv, d]).  Summaries, if there are any,
+        are made anew from the whole of K: write() renews only the blocks that get a token."""
         vb.vatt_append_kv(self.plan, k_new, v_new, self.k, self.v, self.block_table, self.seq_lens, self._stream())
+        self._renew_summary()
 
     # ---- the cache from the projections' outputs to attention over blocks -----
     def make_cache(self, block_table=None):
         """Allocates an empty cache in the plan's format, summaries of its blocks and lists for the chosen ones.
         block_table: [B, ceil(n_max / page_size)] on a paged plan."""
-        dev, rows = self.device, self.B
+        dev = self.device
         if self.paged and block_table is not None:
             want = self.params["batch"] * -(-self.n_max // self.params["page_size"])
             if np.size(block_table) != want:
@@ -188,13 +191,29 @@ class DecodeSession:
         if block_table is not None:
             self.block_table = torch.from_numpy(np.ascontiguousarray(block_table, dtype=np.int32)).to(dev)
         self.seq_lens = torch.zeros(self.params["batch"], dtype=torch.int32, device=dev)
+        self._make_summary()
+        return self
+
+    def _make_summary(self):
         self.block_capacity = vb.vatt_block_list_capacity(self.plan)
         self.summary = self.blocks = self.block_count = None
         if self.block_capacity:
+            dev = self.device
             self.summary = torch.zeros(vb.vatt_block_summary_bytes(self.plan) // 2, dtype=torch.bfloat16, device=dev)
-            self.blocks = torch.zeros(rows, self.Hkv, self.block_capacity, dtype=torch.int32, device=dev)
-            self.block_count = torch.zeros(rows, self.Hkv, dtype=torch.int32, device=dev)
+            self.blocks = torch.zeros(self.B, self.Hkv, self.block_capacity, dtype=torch.int32, device=dev)
+            self.block_count = torch.zeros(self.B, self.Hkv, dtype=torch.int32, device=dev)
+
+    def fill_summary(self):
+        """Summaries of all blocks of the cache as it is, from one pass over K: what select_blocks needs of an uploaded cache, or of one
+        that was written to without write() or append_device()."""
+        if self.summary is None:
+            self._make_summary()
+        vb.vatt_block_summary_fill(self.plan, self.k, self.block_table, self.seq_lens, self.summary, self._stream())
         return self
+
+    def _renew_summary(self):
+        if self.summary is not None:
+            self.fill_summary()
 
     def write(self, q, k_new, v_new, new_lens=None):
         """Appends the tokens k_new, v_new (bf16 [B, n_new, Hkv, d], as far as new_lens says) to every sequence; returns the

@@ -164,3 +164,27 @@ def test_lengths_of_new_tokens_lie_one_behind_the_other(monkeypatch):
     assert not calls.made
     s.write(None, kv, kv, _ints(1, 2))
     s.close()
+
+
+def test_appended_tokens_reach_the_summaries(monkeypatch):
+    calls, s = Calls(monkeypatch, "vatt_append_kv", "vatt_append_kv_cached", "vatt_block_summary_fill"), _host_session()
+    x = torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    s.rcache = s.cache_seeds = None
+    s.append_device(x, x)
+    s.append_device_cached(x, x)
+    assert [name for name, _ in calls.made] == ["vatt_append_kv", "vatt_append_kv_cached"]  # there are none
+    s.make_cache()
+    calls.made.clear()
+    s.append_device(x, x)
+    s.append_device_cached(x, x)
+    assert [name for name, _ in calls.made] == ["vatt_append_kv", "vatt_block_summary_fill", "vatt_append_kv_cached", "vatt_block_summary_fill"]
+    s.close()
+
+
+def test_summaries_of_an_uploaded_cache(monkeypatch):
+    calls, s = Calls(monkeypatch, "vatt_block_summary_fill"), _host_session()
+    s.upload(np.zeros((2, 8, 64), np.uint16), *[np.zeros((2, 2, 100, 64), np.uint16)] * 2, [5, 5], [1, 2])
+    s.fill_summary()
+    assert calls.made[0][1][1:5] == (s.k, None, s.seq_lens, s.summary) and s.summary.numel() == 2 * 2 * 7 * 2 * 64
+    assert s.blocks.shape == (2, 2, s.block_capacity) and s.block_count.shape == (2, 2)
+    s.close()
