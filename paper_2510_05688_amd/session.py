@@ -116,9 +116,10 @@ class DecodeSession:
                        self.workspace, self.out_o, self.out_lse, self.out_idx, self.out_counts,
                        self.out_budget_raw, self.out_stats, self._stream())
 
-    def decode_given_topk(self, topk_idx, topk_cnt, k=None, v=None):
-        """vatt_decode_given_topk with int32 device tensors topk_idx [B, Hq, k_max], topk_cnt [B, Hq]."""
-        vb.vatt_decode_given_topk(self.plan, self.q, self.k if k is None else k, self.v if v is None else v,
+    def decode_given_topk(self, topk_idx, topk_cnt, k=None, v=None, q=None):
+        """vatt_decode_given_topk with int32 device tensors topk_idx [B, Hq, k_max], topk_cnt [B, Hq].  After make_cache() its seeds
+        come from set_seeds()."""
+        vb.vatt_decode_given_topk(self.plan, self._query(q), self.k if k is None else k, self.v if v is None else v,
                                   self.block_table, self.seq_lens, self.seq_seeds, topk_idx, topk_cnt,
                                   self.workspace, self.out_o, self.out_lse, self.out_idx, self.out_counts,
                                   self.out_budget_raw, self.out_stats, self._stream())
@@ -149,8 +150,8 @@ class DecodeSession:
                                  self.cache_seeds, self.rcache, self._stream())
         self._renew_summary()
 
-    def decode_given_topk_cached(self, topk_idx, topk_cnt, k=None, v=None):
-        vb.vatt_decode_given_topk_cached(self.plan, self.q, self.k if k is None else k,
+    def decode_given_topk_cached(self, topk_idx, topk_cnt, k=None, v=None, q=None):
+        vb.vatt_decode_given_topk_cached(self.plan, self._query(q), self.k if k is None else k,
                                          self.v if v is None else v, self.block_table, self.seq_lens,
                                          self.seq_seeds, topk_idx, topk_cnt, self.rcache, self.workspace,
                                          self.out_o, self.out_lse, self.out_idx, self.out_counts,

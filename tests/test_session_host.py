@@ -188,3 +188,18 @@ def test_summaries_of_an_uploaded_cache(monkeypatch):
     assert calls.made[0][1][1:5] == (s.k, None, s.seq_lens, s.summary) and s.summary.numel() == 2 * 2 * 7 * 2 * 64
     assert s.blocks.shape == (2, 2, s.block_capacity) and s.block_count.shape == (2, 2)
     s.close()
+
+
+def test_the_verified_step_takes_queries(monkeypatch):
+    """What write() returns goes into the step with a supplied top-k set as it goes into the others."""
+    calls, s = Calls(monkeypatch, "vatt_decode_given_topk", "vatt_decode_given_topk_cached"), _host_session()
+    s.make_cache()
+    s.out_idx = s.out_counts = s.out_budget_raw = s.out_stats = None
+    q, idx, cnt = torch.zeros(2, 1, 8, 64, dtype=torch.bfloat16), torch.zeros(2, 8, 30, dtype=torch.int32), torch.zeros(2, 8, dtype=torch.int32)
+    s.decode_given_topk(idx, cnt, q=q)
+    s.decode_given_topk_cached(idx, cnt, q=q)
+    assert [a[1] is q for _, a in calls.made] == [True, True]
+    for call in (s.decode_given_topk, s.decode_given_topk_cached):
+        with pytest.raises(ValueError):
+            call(idx, cnt, q=q[:1])
+    s.close()
