@@ -93,7 +93,8 @@ __device__ __forceinline__ uint4 other_half(const WriteArgs& A, const uint4& own
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-// A lane's share of a token's turns: column i becomes own_i cos_i + partner_i sin_i, the sign of the sine included.
+// A lane's share of a token's turns: column i becomes own_i cos_i + partner_i sin_i, the sign of the sine included.  Columns that are not
+// rotated have cos 1, partner 0 and sin -0, whose product -0 leaves every value as it is, -0 too.
 struct LaneTurns {
   float cos[8], sin[8];
 };
@@ -105,7 +106,7 @@ __device__ __forceinline__ LaneTurns lane_turns(const WriteArgs& A, const float2
   for (int i = 0; i < 8; ++i) {
     const float2 x = !turned ? make_float2(1.f, 0.f) : turns[A.pairs ? 4 * c + i / 2 : (lower ? 8 * c : 8 * c - A.rot / 2) + i];
     t.cos[i] = x.x;
-    t.sin[i] = (A.pairs ? (i & 1) == 0 : lower) ? -x.y : x.y;
+    t.sin[i] = !turned || (A.pairs ? (i & 1) == 0 : lower) ? -x.y : x.y;
   }
   return t;
 }
@@ -128,7 +129,7 @@ __device__ __forceinline__ void rotated(const WriteArgs& A, const uint4& own, in
     const uint4 other = other_half<D>(A, own, c);
     o[0] = other.x; o[1] = other.y; o[2] = other.z; o[3] = other.w;
   }
-  const uint32_t turned = 8 * c < A.rot ? 0xffffffffu : 0u;  // (else cos 1 and sin 0, and nothing that 0 could make a NaN of)
+  const uint32_t turned = 8 * c < A.rot ? 0xffffffffu : 0u;  // (else nothing that 0 could make a NaN of)
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t x = o[i] & turned;

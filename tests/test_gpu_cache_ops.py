@@ -842,3 +842,28 @@ def test_calls_for_bf16_caches_refuse_others():
         with pytest.raises(vb.VattError) as e:
             call()
         assert e.value.status == vb.VATT_E_UNSUPPORTED_SHAPE
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("fmt", [0, 1, 2])
+def test_columns_that_are_not_rotated_stay_as_they_are(fmt, layout):
+    """To the bit: negative zeros, subnormals and infinities too."""
+    s = Setup(1, 4, 2, 128, 64, 0, fmt, 16, rotary=dict(theta=10000.0, rotary_dim=48, layout=layout), seed=23)
+    x = [s.rng.normal(size=(1, 20, h, 128)) for h in (4, 2, 2)]
+    x = [_bf16(np.where(s.rng.uniform(size=t.shape) < 0.3, -0.0, t)) for t in x]
+    x[0][0, :, :, 70], x[0][0, :, :, 71] = math.inf, 2.0 ** -133
+    if fmt == 0:
+        x[1][0, :, :, 70], x[1][0, :, :, 71] = -math.inf, -2.0 ** -133
+    out_q = torch.zeros_like(x[0])
+    s.write(*x, s.ints([3]), out_q=out_q)
+    torch.cuda.synchronize()
+    assert torch.equal(out_q[..., 48:].view(torch.int16), x[0][..., 48:].view(torch.int16))
+    host, vals = s.k.cpu().numpy(), _np(x[1])
+    for j in range(20):
+        for h in range(2):
+            codes, scales = s.raw(host, 0, h, 3 + j)
+            if fmt == 0:
+                assert np.array_equal(codes[96:], x[1][0, j, h].view(torch.uint8).cpu().numpy()[96:]), (j, h)
+                continue
+            c, e = co.encode(vals[0, j, h], fmt)  # (the last two groups of 32 columns hold no rotated one)
+            assert np.array_equal(co.unpack(codes, fmt)[64:], c[64:]) and np.array_equal(scales[2:], e[2:]), (j, h)
