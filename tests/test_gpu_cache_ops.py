@@ -867,3 +867,9 @@ def test_columns_that_are_not_rotated_stay_as_they_are(fmt, layout):
                 continue
             c, e = co.encode(vals[0, j, h], fmt)  # (the last two groups of 32 columns hold no rotated one)
             assert np.array_equal(co.unpack(codes, fmt)[64:], c[64:]) and np.array_equal(scales[2:], e[2:]), (j, h)
+
+
+@pytest.mark.parametrize("rotary", [dict(theta=1e4, attention=1.75), dict(YARN, attention=0.8), dict(WAVES, attention=1.0, layout=1)],
+                         ids=["plain", "yarn", "wavelength"])
+def test_rotations_with_a_factor_of_their_own(rotary):
+    test_write((2, 4, 2, 128, 96, 0, 0, 16, 40, [0, 13], None, rotary, False))

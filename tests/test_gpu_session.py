@@ -62,3 +62,21 @@ def test_blocks_of_tokens_appended_beside_a_random_cache():
     for i in range(20):
         sess.append_device_cached(_bf16(s.rng.normal(size=(2, 2, 128)) * (9 if i == 3 else 1)), _bf16(s.rng.normal(size=(2, 2, 128))))
     _chosen(s, sess, _bf16(s.rng.normal(size=(2, 8, 128))), [470, 220])
+
+
+@pytest.mark.parametrize("page", [0, 32])
+def test_chosen_tokens_through_the_verified_step(page):
+    """Choice -> step with that top-k set: with an epsilon that asks for every token the estimate is dense attention."""
+    from paper_2510_05688_amd.session import DecodeSession
+    s = Setup(2, 8, 2, 128, 700, page, 0, 32, seed=33, topk_frac=0.2, epsilon=1e-4)
+    sess = DecodeSession(s.params, block_tokens=32, rotary=dict(theta=10000.0)).make_cache(s.table.cpu().numpy() if page else None)
+    x = [_bf16(s.rng.normal(size=(2, 691, h, 128))) for h in (8, 2, 2)]
+    sess.write(*[t[:, :690].contiguous() for t in x], s.ints([690, 333]))
+    q, lens = sess.write(*[t[:, 690:].contiguous() for t in x]), [691, 334]
+    topk, cnt = _chosen(s, sess, q, lens)
+    sess.set_seeds([7, 8])
+    sess.decode_given_topk(topk, cnt, q=q)
+    torch.cuda.synchronize()
+    counts = sess.out_counts.cpu().numpy()
+    assert (counts[..., 2] == cnt.cpu().numpy()).all() and (counts[..., 4] == counts[..., 5]).all()  # the budget is the whole residual
+    _check_attention(s, q, lens, [[np.arange(n)] * 2 for n in lens], sess.out_o, sess.out_lse)
