@@ -39,8 +39,10 @@ struct WriteArgs {
   double freq[64];
 };
 
-// sin and cos of a >= 0 in 64 bits, rounded to 32 with a factor: a minus the nearest multiple of pi / 2 (pi / 2 in two parts, so that the
-// difference is right to 2^-60 of a), then the Taylor series to x^13 and x^12, whose next terms are below 2^-36 for |x| <= pi / 4.
+// sin and cos of a >= 0 in 64 bits, rounded to 32 with a factor: a minus the nearest multiple of pi / 2 (pi / 2 in two parts, whose own
+// error is below 2^-100 of a; the two differences round by 2^-54 each), then the Taylor series to x^13 and x^12, whose next terms are
+// below 2^-41 for |x| <= pi / 4.  a itself, a rounded product of position and frequency, is off by up to 2^-53 of it: 2^-35 at the
+// furthest positions.
 __device__ __forceinline__ float2 turn(double a, double factor) {
   const double k = rint(a * 0.63661977236758134308);
   const double x = fma(-k, 6.123233995736766036e-17, fma(-k, 1.57079632679489661923, a));
