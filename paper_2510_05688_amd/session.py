@@ -24,20 +24,17 @@ class DecodeSession:
     def __init__(self, params: Dict, device: int = 0, q_len: int = 1, kv_format: int = vb.VATT_KV_BF16,
                  block_tokens: Optional[int] = None, rotary: Optional[Dict] = None):
         """kv_format, block_tokens, rotary: the cache's format (VATT_KV_*), the tokens per block and the rotation
-        (fields of vatt_rotary) of the cache calls below.  q_len > 1: a plan for multi-query steps; q is then [B, q_len, Hq, d] and every output has one row per
-        (sequence, query token) pair, b * q_len + t, where the single-token shapes have one per sequence."""
+        (fields of vatt_rotary) of the cache calls below.  q_len > 1: a plan for multi-query steps; q is then
+        [B, q_len, Hq, d] and every output has one row per (sequence, query token) pair, b * q_len + t, where the
+        single-token shapes have one per sequence."""
         if not torch.cuda.is_available():
             raise RuntimeError("DecodeSession needs a GPU; there is no CPU path")
         self.device = torch.device("cuda", device)
         torch.cuda.set_device(self.device)
         self.params = dict(params)
         self.q_len = int(q_len)
-        self.plan = (vb.vatt_plan_create(self.params, device) if self.q_len == 1
-                     else vb.vatt_plan_create_chunk(self.params, self.q_len, device))
-        self.kv_format = int(kv_format)
-        vb.vatt_plan_set_option(self.plan, vb.VATT_OPT_KV_FORMAT, self.kv_format)
-        if block_tokens is not None:
-            vb.vatt_plan_set_option(self.plan, vb.VATT_OPT_BLOCK_TOKENS, int(block_tokens))
+        self.kv_format, self.block_tokens, self.plain = int(kv_format), block_tokens, None
+        self.plan = self._new_plan()
         if rotary is not None:
             vb.vatt_plan_set_rotary(self.plan, rotary)
         p = self.params
@@ -63,10 +60,20 @@ class DecodeSession:
         self.q = self.k = self.v = self.seq_lens = self.seq_seeds = self.rcache = self.cache_seeds = None
         self.summary = self.blocks = self.block_count = None
 
+    def _new_plan(self):
+        device = -1 if self.device.type == "cpu" else self.device.index
+        plan = (vb.vatt_plan_create(self.params, device) if self.q_len == 1
+                else vb.vatt_plan_create_chunk(self.params, self.q_len, device))
+        vb.vatt_plan_set_option(plan, vb.VATT_OPT_KV_FORMAT, self.kv_format)
+        if self.block_tokens is not None:
+            vb.vatt_plan_set_option(plan, vb.VATT_OPT_BLOCK_TOKENS, int(self.block_tokens))
+        return plan
+
     def close(self):
-        if self.plan:
-            vb.vatt_plan_destroy(self.plan)
-            self.plan = None
+        for plan in (self.plan, self.plain):
+            if plan:
+                vb.vatt_plan_destroy(plan)
+        self.plan = self.plain = None
 
     def __del__(self):
         try:
@@ -146,9 +153,9 @@ class DecodeSession:
         return tok.cpu().numpy(), cnt.cpu().numpy()
 
     def append_device_cached(self, k_new, v_new):
+        self._renew_summary(k_new, v_new)
         vb.vatt_append_kv_cached(self.plan, k_new, v_new, self.k, self.v, self.block_table, self.seq_lens,
                                  self.cache_seeds, self.rcache, self._stream())
-        self._renew_summary()
 
     def decode_given_topk_cached(self, topk_idx, topk_cnt, k=None, v=None, q=None):
         vb.vatt_decode_given_topk_cached(self.plan, self._query(q), self.k if k is None else k,
@@ -172,10 +179,10 @@ class DecodeSession:
         self.append_device(kn, vn)
 
     def append_device(self, k_new, v_new):
-        """Append one token per sequence from tensors that are already on the device (bf16 [B, Hkv, d]).  Summaries, if there are any,
-        are made anew from the whole of K: write() renews only the blocks that get a token."""
+        """Append one token per sequence from tensors that are already on the device (bf16 [B, Hkv, d]).  The summaries
+        of their blocks follow, if there are any."""
+        self._renew_summary(k_new, v_new)
         vb.vatt_append_kv(self.plan, k_new, v_new, self.k, self.v, self.block_table, self.seq_lens, self._stream())
-        self._renew_summary()
 
     # ---- the cache from the projections' outputs to attention over blocks -----
     def make_cache(self, block_table=None):
@@ -203,6 +210,7 @@ class DecodeSession:
             self.summary = torch.zeros(vb.vatt_block_summary_bytes(self.plan) // 2, dtype=torch.bfloat16, device=dev)
             self.blocks = torch.zeros(self.B, self.Hkv, self.block_capacity, dtype=torch.int32, device=dev)
             self.block_count = torch.zeros(self.B, self.Hkv, dtype=torch.int32, device=dev)
+            self.plain = self.plain or self._new_plan()  # (without a rotation: appended rows are the caller's as they are)
 
     def fill_summary(self):
         """Summaries of all blocks of the cache as it is, from one pass over K: what select_blocks needs of an uploaded cache, or of one
@@ -212,9 +220,12 @@ class DecodeSession:
         vb.vatt_block_summary_fill(self.plan, self.k, self.block_table, self.seq_lens, self.summary, self._stream())
         return self
 
-    def _renew_summary(self):
-        if self.summary is not None:
-            self.fill_summary()
+    def _renew_summary(self, k_new, v_new):
+        """The row that an append is about to write, written with the summary of its block."""
+        if self.summary is not None and self.kv_format == vb.VATT_KV_BF16:  # (the others do not append)
+            row = self.Hkv * self.d
+            vb.vatt_write_kv(self.plain, None, k_new, v_new, 0, row, row, 1, self.seq_lens, None, self.k, self.v, self.block_table,
+                             self.summary, None, None, self._stream())
 
     def write(self, q, k_new, v_new, new_lens=None):
         """Appends the tokens k_new, v_new (bf16 [B, n_new, Hkv, d], as far as new_lens says) to every sequence; returns the

@@ -55,13 +55,18 @@ def test_blocks_of_an_uploaded_cache_and_of_appended_tokens(page):
 def test_blocks_of_tokens_appended_beside_a_random_cache():
     from paper_2510_05688_amd.session import DecodeSession
     s = Setup(2, 8, 2, 128, 500, 0, 0, 16, seed=32, topk_frac=0.2)
-    sess = DecodeSession(s.params, block_tokens=16).make_cache()
-    x = _bf16(s.rng.normal(size=(2, 450, 2, 128)))
-    sess.write(None, x, x, s.ints([450, 200]))
+    sess = DecodeSession(s.params, block_tokens=16, rotary=dict(theta=10000.0)).make_cache()
+    x = _bf16(s.rng.normal(size=(2, 490, 2, 128)))
+    sess.write(None, x, x, s.ints([490, 200]))
     sess.make_random_cache([5, 6])
-    for i in range(20):
-        sess.append_device_cached(_bf16(s.rng.normal(size=(2, 2, 128)) * (9 if i == 3 else 1)), _bf16(s.rng.normal(size=(2, 2, 128))))
-    _chosen(s, sess, _bf16(s.rng.normal(size=(2, 8, 128))), [470, 220])
+    rows = [_bf16(s.rng.normal(size=(2, 2, 128)) * (9 if i == 3 else 1)) for i in range(20)]
+    for r in rows:  # (the first sequence is full after ten)
+        sess.append_device_cached(r, r)
+    assert sess.seq_lens.tolist() == [500, 220]
+    _chosen(s, sess, _bf16(s.rng.normal(size=(2, 8, 128))), [500, 220])
+    for b, n in ((0, 490), (1, 200)):  # as they are, whatever the plan's rotation
+        for i, r in enumerate(rows[:10]):
+            assert np.array_equal(s.rows(s.k, b, 1, [n + i])[0], _np(r[b, 1])) and np.array_equal(s.rows(s.v, b, 1, [n + i])[0], _np(r[b, 1]))
 
 
 @pytest.mark.parametrize("page", [0, 32])

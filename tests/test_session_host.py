@@ -18,10 +18,10 @@ class Calls:
 def _session(q_len=1, batch=2, hq=8, hkv=2, d=64, n_max=100, k_max=30, page=0):
     """A session as its constructor leaves it, on the CPU: no plan, no workspace."""
     s = sm.DecodeSession.__new__(sm.DecodeSession)
-    s.plan, s.device, s.q_len = None, torch.device("cpu"), q_len
+    s.plan, s.plain, s.device, s.q_len, s.kv_format, s.block_tokens = None, None, torch.device("cpu"), q_len, 0, None
     s.params = dict(batch=batch, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, n_max=n_max, page_size=page)
     s.B, s.Hq, s.Hkv, s.d, s.n_max, s.paged, s.seg = batch * q_len, hq, hkv, d, n_max, page > 0, [0, 4, 8, 8 + k_max, 60]
-    s.workspace = s.out_o = s.out_lse = s.k = s.v = s.q = s.seq_seeds = s.block_table = s.summary = s.blocks = s.block_count = None
+    s.workspace = s.out_o = s.out_lse = s.k = s.v = s.q = s.seq_seeds = s.block_table = s.summary = s.blocks = s.block_count = s.rcache = s.cache_seeds = None
     s.seq_lens = torch.full((batch,), 50, dtype=torch.int32)
     s._stream = lambda: 0
     return s
@@ -106,9 +106,8 @@ def _host_session(page=0, block=16, **over):
              budget_cap_frac=1.0)
     p.update(over)
     s = _session(page=page)
-    s.plan, s.kv_format, s.params = sm.vb.vatt_plan_create(p, -1), 0, p
-    if block:
-        sm.vb.vatt_plan_set_option(s.plan, sm.vb.VATT_OPT_BLOCK_TOKENS, block)
+    s.params, s.block_tokens = p, block
+    s.plan = s._new_plan()
     return s
 
 
@@ -167,9 +166,8 @@ def test_lengths_of_new_tokens_lie_one_behind_the_other(monkeypatch):
 
 
 def test_appended_tokens_reach_the_summaries(monkeypatch):
-    calls, s = Calls(monkeypatch, "vatt_append_kv", "vatt_append_kv_cached", "vatt_block_summary_fill"), _host_session()
+    calls, s = Calls(monkeypatch, "vatt_append_kv", "vatt_append_kv_cached", "vatt_write_kv"), _host_session()
     x = torch.zeros(2, 2, 64, dtype=torch.bfloat16)
-    s.rcache = s.cache_seeds = None
     s.append_device(x, x)
     s.append_device_cached(x, x)
     assert [name for name, _ in calls.made] == ["vatt_append_kv", "vatt_append_kv_cached"]  # there are none
@@ -177,7 +175,12 @@ def test_appended_tokens_reach_the_summaries(monkeypatch):
     calls.made.clear()
     s.append_device(x, x)
     s.append_device_cached(x, x)
-    assert [name for name, _ in calls.made] == ["vatt_append_kv", "vatt_block_summary_fill", "vatt_append_kv_cached", "vatt_block_summary_fill"]
+    assert [name for name, _ in calls.made] == ["vatt_write_kv", "vatt_append_kv", "vatt_write_kv", "vatt_append_kv_cached"]
+    assert all(a[0] is s.plain is not s.plan for name, a in calls.made if name == "vatt_write_kv")  # nothing is rotated
+    s.kv_format = 1  # the append is refused: nothing may be written before
+    calls.made.clear()
+    s.append_device(x, x)
+    assert [name for name, _ in calls.made] == ["vatt_append_kv"]
     s.close()
 
 
