@@ -379,7 +379,7 @@ size_t vatt_block_list_capacity(const vatt_plan* plan);   /* entries of one list
 
 /*
  * Rotary positions.  The first rotary_dim columns of a row are rotary_dim / 2 pairs; pair i of the token at position p is turned by the
- * angle p f_i (in 64 bits) and multiplied by `attention`:
+ * angle p f_i (in 64 bits) and multiplied by `attention`, the columns behind them stay as they are:
  *   layout  VATT_ROTARY_HALF: columns i and i + rotary_dim / 2;  VATT_ROTARY_PAIRS: columns 2 i and 2 i + 1
  *   f_i = theta^(-2 i / rotary_dim), for contexts longer than the trained original_len scaled by
  *   VATT_ROTARY_LINEAR      f_i / factor

@@ -64,8 +64,9 @@ __device__ __forceinline__ int token_of(const TokenList& L, int group, int blk) 
   return tok < L.n ? tok : kNowhere;
 }
 
-// STREAM: read once.  All tokens' rows are, those of lists may be in the lists of several query tokens (16 x 32K tokens in e4m3 192 us
-// without the hint, 181 with it; lists of two query tokens, 12 x 4K - 64K, 29.0 without, 31.1 with).
+// STREAM: read once.  All tokens' rows are with up to 32 query vectors per KV head (with more, every round of 32 reads them again, with the
+// hint too: 4 x 32K in e4m3 with 32 vectors 70 us, with 64 111); those of lists may be in the lists of several query tokens (16 x 32K
+// tokens in e4m3 192 us without the hint, 181 with it; lists of two query tokens, 12 x 4K - 64K, 29.0 without, 31.1 with).
 template <bool STREAM>
 __device__ __forceinline__ uint4 load_16(const unsigned char* p) {
   return STREAM ? load_stream_16(reinterpret_cast<const uint16_t*>(p)) : *reinterpret_cast<const uint4*>(p);
@@ -97,8 +98,8 @@ __device__ __forceinline__ uint32_t row_scales(const unsigned char* p) {
 //   * P goes in as three bf16 terms that add up to the fp32 value, so that the sums keep fp32 accuracy.  Where the vectors fill five columns at
 //     most, their three terms are columns of one product (PACK 3); with up to eight, two of them are (PACK 2).
 // The running maximum of a column moves only when a score passes it by more than kLazy.
-// What bounds it: the rows' bytes.  All tokens of 16 x 32K in e4m3 (1.1 GB) take 176 us = 6.3 TB/s where the same loads without the
-// products and exponentials take 164; lists of 12 x 4K - 64K tokens with two queries each (98 MB in pieces of 2 KB, with scales of 64
+// What bounds it: the rows' bytes.  All tokens of 16 x 32K in e4m3 (1.1 GB) take 170 to 180 us, by the clock (6.2 - 6.5 TB/s), where the
+// same loads without the products and exponentials take 164; lists of 12 x 4K - 64K tokens with two queries each (98 MB in pieces of 2 KB, with scales of 64
 // bytes apart from them) 28 us, loads alone 22.  Half or twice as many workgroups, three of them on a CU instead of two, and a least
 // number of chunks for each made no difference or were slower.
 template <int D, int FMT, bool PAGED, bool LIST, int NQT, int PACK>
@@ -650,7 +651,9 @@ hipError_t launch_attend(const Plan& pl, const void* q, const void* k, const voi
   A.log2_scale = (float)((double)pl.sm_scale * 1.4426950408889634);
   const int vectors = blocks ? pl.group : pl.group * pl.q_len;
   A.rounds = vectors <= 16 ? 1 : (vectors + 31) / 32;
-  // Four workgroups per CU in all, none with less than a unit of keys per wave at the longest; the partial sums fit the workspace.
+  // Four workgroups per CU in all, none with less than a unit of keys per wave at the longest; the partial sums fit the workspace.  Every
+  // row gets as many, however long it is: with one long sequence among short ones a few workgroups have nearly all the work (one of 128K
+  // tokens among 47 of 1000 in e4m3, 376 MB, 468 us; 2K to 32K evenly, 588 MB, 110).
   const int64_t rows = (int64_t)pl.vbatch * A.Hq, jobs = (int64_t)(blocks ? pl.vbatch : pl.p.batch) * A.Hkv * A.rounds;
   const int64_t longest = blocks ? (int64_t)A.capacity * pl.block_tokens : pl.p.n_max;
   int64_t splits = std::min<int64_t>((4 * pl.num_cus + jobs - 1) / jobs, (longest + kUnit * kAttendWaves - 1) / (kUnit * kAttendWaves));

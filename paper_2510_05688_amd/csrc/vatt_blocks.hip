@@ -69,8 +69,9 @@ __device__ __forceinline__ uint4 magnitudes(const uint4& w) {
 // at a time (operand lane l: row or column l % 16, eight columns of the head); the same with magnitudes bounds the error.  A sum of 2 d
 // products in any order, every addition off by at most 2^-23 of the magnitudes so far, is off by at most 2 d 2^-23 of the sum of all
 // magnitudes; 2^-23 more covers the rounding of the exact sum to 32 bits.  (2^-100: products below the normal range.)
-// What bounds it: the summaries' bytes.  12 sequences of 8K - 128K tokens on pages, 213 MB of summaries, 39 us = 5.4 TB/s; all scores in 64 bits
-// on the vector units took 58 (they were busy 85 % of the time).
+// What bounds it: the summaries' bytes, which are read again for every 16 query vectors of a KV head.  12 sequences of 8K - 128K tokens on pages,
+// 213 MB of summaries, 39 us = 5.4 TB/s; all scores in 64 bits on the vector units took 58 (they were busy 85 % of the time).  Whole
+// call on 8 x 64K, 134 MB: up to 16 vectors 32 - 34 us, 20 vectors 56, 40 vectors 77.
 template <int D, bool PAGED>
 __global__ __launch_bounds__(kScoreThreads) void block_score_kernel(SelectBlocksArgs A) {
   constexpr int S = D / 32, TILE = kScoreTile;

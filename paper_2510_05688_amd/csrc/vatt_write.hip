@@ -371,6 +371,9 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(WriteArgs A) {
   }
 }
 
+// A tile of one KV head per workgroup, a pass over it at a time.  What bounds it: with blocks of 16 and 128 columns a thread has one row part
+// under way (8 x 32K tokens, bf16, 604 MB, 155 us = 3.9 TB/s; blocks of 64, whose next pass is under way, 108 us = 5.1 TB/s; e4m3 on
+// pages, 344 MB, 188 us).
 template <int D, int FMT, bool PAGED>
 __global__ __launch_bounds__(kWriteThreads) void summary_kernel(WriteArgs A) {
   constexpr int TT = kWriteThreads / (D / 8);
