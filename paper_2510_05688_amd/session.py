@@ -118,7 +118,7 @@ class DecodeSession:
 
     # ---- calls ---------------------------------------------------------------
     def decode(self, q=None, k=None, v=None):
-        vb.vatt_decode(self.plan, self.q if q is None else q, self.k if k is None else k,
+        vb.vatt_decode(self.plan, self._query(q), self.k if k is None else k,
                        self.v if v is None else v, self.block_table, self.seq_lens, self.seq_seeds,
                        self.workspace, self.out_o, self.out_lse, self.out_idx, self.out_counts,
                        self.out_budget_raw, self.out_stats, self._stream())
@@ -165,12 +165,12 @@ class DecodeSession:
                                          self.out_budget_raw, self.out_stats, self._stream())
 
     def dense(self, q=None, k=None, v=None):
-        vb.vatt_dense_decode(self.plan, self.q if q is None else q, self.k if k is None else k,
+        vb.vatt_dense_decode(self.plan, self._query(q), self.k if k is None else k,
                              self.v if v is None else v, self.block_table, self.seq_lens, self.workspace,
                              self.dense_o, self.dense_lse, self._stream())
 
     def score(self, q=None, k=None):
-        vb.vatt_score(self.plan, self.q if q is None else q, self.k if k is None else k, self.block_table,
+        vb.vatt_score(self.plan, self._query(q), self.k if k is None else k, self.block_table,
                       self.seq_lens, self.workspace, self._stream())
 
     def append(self, k_new_bits, v_new_bits):

@@ -206,3 +206,20 @@ def test_the_verified_step_takes_queries(monkeypatch):
         with pytest.raises(ValueError):
             call(idx, cnt, q=q[:1])
     s.close()
+
+
+@pytest.mark.parametrize("q_len", [1, 4])
+def test_queries_of_the_steps_over_all_tokens(monkeypatch, q_len):
+    """write() returns as many queries as it was given tokens; a plan takes q_len of them."""
+    calls, s = Calls(monkeypatch, "vatt_dense_decode", "vatt_decode", "vatt_score"), _session(q_len)
+    s.dense_o = s.dense_lse = s.out_idx = s.out_counts = s.out_budget_raw = s.out_stats = None
+    for call in (s.dense, s.decode, s.score):
+        for tokens in (1, 2, 4, 5):
+            q = torch.zeros(2, tokens, 8, 64, dtype=torch.bfloat16)
+            if tokens == q_len:
+                call(q)
+                assert calls.made.pop()[1][1] is q
+                continue
+            with pytest.raises(ValueError):
+                call(q)
+    assert not calls.made
