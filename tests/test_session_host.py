@@ -223,3 +223,19 @@ def test_queries_of_the_steps_over_all_tokens(monkeypatch, q_len):
             with pytest.raises(ValueError):
                 call(q)
     assert not calls.made
+
+
+def test_queries_into_a_buffer_of_the_callers(monkeypatch):
+    """It is handed on as it is: nothing is cleared, nothing allocated."""
+    calls, s = Calls(monkeypatch, "vatt_write_kv"), _host_session()
+    s.make_cache()
+    q, kv = torch.ones(2, 3, 8, 64, dtype=torch.bfloat16), torch.ones(2, 3, 2, 64, dtype=torch.bfloat16)
+    out = torch.full_like(q, 7.0)
+    for bad in (out[:1], out[:, :2], out.float(), out.to("meta"), out.transpose(0, 1), 4096):
+        with pytest.raises(ValueError):
+            s.write(q, kv, kv, out_q=bad)
+    with pytest.raises(ValueError):
+        s.write(None, kv, kv, out_q=out)
+    assert not calls.made
+    assert s.write(q, kv, kv, out_q=out) is out and calls.made[0][1][14] is out and (out == 7.0).all()
+    s.close()
