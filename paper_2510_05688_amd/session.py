@@ -85,8 +85,8 @@ class DecodeSession:
     def upload(self, q_bits, k_bits, v_bits, seq_lens, seeds, block_table=None):
         """k_bits, v_bits: bf16 rows in the plan's layout; on a quantised plan codes and scales, vatt_kv_cache_bytes in all."""
         dev = self.device
-        if self.kv_format != vb.VATT_KV_BF16:
-            want = vb.vatt_kv_cache_bytes(self.plan)
+        want = vb.vatt_kv_cache_bytes(self.plan)
+        if vb.vatt_kv_scale_offset(self.plan) < want:  # (there are scales)
             if np.asarray(k_bits).nbytes != want or np.asarray(v_bits).nbytes != want:
                 raise ValueError(f"K and V of this plan's format have {want} bytes each, got {np.asarray(k_bits).nbytes} and {np.asarray(v_bits).nbytes}")
         self.q = _bf16_from_bits(q_bits, dev)
@@ -210,7 +210,16 @@ class DecodeSession:
             self.summary = torch.zeros(vb.vatt_block_summary_bytes(self.plan) // 2, dtype=torch.bfloat16, device=dev)
             self.blocks = torch.zeros(self.B, self.Hkv, self.block_capacity, dtype=torch.int32, device=dev)
             self.block_count = torch.zeros(self.B, self.Hkv, dtype=torch.int32, device=dev)
-            self.plain = self.plain or self._new_plan()  # (without a rotation: appended rows are the caller's as they are)
+            self._make_plain()
+
+    def _make_plain(self):
+        """A plan like the session's without a rotation: appended rows are the caller's as they are, and bf16."""
+        self.plain = self.plain or self._new_plan()
+        vb.vatt_plan_set_option(self.plain, vb.VATT_OPT_KV_FORMAT, vb.VATT_KV_BF16)
+        for tokens in (16, 32, 64, 128, 256):  # (the number may have been set on the plan itself; the size says which)
+            if vb.vatt_block_summary_bytes(self.plain) == vb.vatt_block_summary_bytes(self.plan):
+                break
+            vb.vatt_plan_set_option(self.plain, vb.VATT_OPT_BLOCK_TOKENS, tokens)
 
     def fill_summary(self):
         """Summaries of all blocks of the cache as it is, from one pass over K: what select_blocks needs of an uploaded cache, or of one
@@ -222,7 +231,7 @@ class DecodeSession:
 
     def _renew_summary(self, k_new, v_new):
         """The row that an append is about to write, written with the summary of its block."""
-        if self.summary is not None and self.kv_format == vb.VATT_KV_BF16:  # (the others do not append)
+        if self.summary is not None and vb.vatt_kv_scale_offset(self.plan) == vb.vatt_kv_cache_bytes(self.plan):  # (quantised plans do not append)
             row = self.Hkv * self.d
             vb.vatt_write_kv(self.plain, None, k_new, v_new, 0, row, row, 1, self.seq_lens, None, self.k, self.v, self.block_table,
                              self.summary, None, None, self._stream())

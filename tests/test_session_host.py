@@ -177,7 +177,7 @@ def test_appended_tokens_reach_the_summaries(monkeypatch):
     s.append_device_cached(x, x)
     assert [name for name, _ in calls.made] == ["vatt_write_kv", "vatt_append_kv", "vatt_write_kv", "vatt_append_kv_cached"]
     assert all(a[0] is s.plain is not s.plan for name, a in calls.made if name == "vatt_write_kv")  # nothing is rotated
-    s.kv_format = 1  # the append is refused: nothing may be written before
+    sm.vb.vatt_plan_set_option(s.plan, sm.vb.VATT_OPT_KV_FORMAT, 1)  # the append is refused: nothing may be written before
     calls.made.clear()
     s.append_device(x, x)
     assert [name for name, _ in calls.made] == ["vatt_append_kv"]
@@ -238,4 +238,19 @@ def test_queries_into_a_buffer_of_the_callers(monkeypatch):
         s.write(None, kv, kv, out_q=out)
     assert not calls.made
     assert s.write(q, kv, kv, out_q=out) is out and calls.made[0][1][14] is out and (out == 7.0).all()
+    s.close()
+
+
+@pytest.mark.parametrize("block", [16, 32, 64])
+def test_options_set_on_the_plan_itself(monkeypatch, block):
+    """Blocks and formats that the constructor was not told of: appended rows go into summaries of that layout, uploads are still checked."""
+    calls, s, x = Calls(monkeypatch, "vatt_append_kv", "vatt_write_kv"), _host_session(block=None), torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    sm.vb.vatt_plan_set_option(s.plan, sm.vb.VATT_OPT_BLOCK_TOKENS, block)
+    s.make_cache()
+    s.append_device(x, x)
+    used = [a[0] for name, a in calls.made if name == "vatt_write_kv"]
+    assert len(used) == 1 and sm.vb.vatt_block_summary_bytes(used[0]) == sm.vb.vatt_block_summary_bytes(s.plan) == 2 * s.summary.numel()
+    sm.vb.vatt_plan_set_option(s.plan, sm.vb.VATT_OPT_KV_FORMAT, 2)
+    with pytest.raises(ValueError):
+        s.upload(np.zeros((2, 8, 64), np.uint16), *[np.zeros((2, 2, 100, 64), np.uint16)] * 2, [5, 5], [1, 2])
     s.close()
