@@ -359,8 +359,8 @@ int vatt_append_kv(vatt_plan* plan, const void* k_new, const void* v_new, void* 
  * NaN).  In the contiguous layout the scales are [batch, n_kv_heads, n_max rounded up to a multiple of 8, head_dim / 32], in the
  * paged one [num_blocks, n_kv_heads, page_size, head_dim / 32].  The scale of 32 values is the smallest power of two at which none
  * is above the format's largest value; values are rounded to the nearest, ties to even; magnitudes above 1.5 * 2^127 count as that.
- * On a quantised plan vatt_write_kv, vatt_read_kv, vatt_block_summary_fill, vatt_block_decode and vatt_dense_decode work; the others
- * that take K or V return VATT_E_UNSUPPORTED_SHAPE.
+ * On a quantised plan vatt_write_kv, vatt_read_kv, vatt_block_summary_fill, vatt_block_decode, vatt_dense_decode, vatt_chunk_attend and
+ * vatt_window_decode work; the others that take K or V return VATT_E_UNSUPPORTED_SHAPE.
  *
  * Blocks.  VATT_OPT_BLOCK_TOKENS = c (a power of two in 16 .. 256, in the paged layout at most page_size; default 16): block j of a
  * sequence is its tokens j c .. j c + c - 1.  A block's summary is, for every column, the largest and the smallest value that its
@@ -459,6 +459,44 @@ int vatt_select_blocks(vatt_plan* plan, const void* q, const void* summary, cons
 int vatt_block_decode(vatt_plan* plan, const void* q, const void* k, const void* v, const int32_t* block_table,
                       const int32_t* seq_lens, const int32_t* blocks, const int32_t* block_count, void* workspace,
                       size_t workspace_bytes, float* out_o, float* out_lse, void* stream);
+
+/*
+ * Attention of the new tokens of every sequence over the cache that already holds their rows (vatt_write_kv with the same first and
+ * new_lens): whole prompts, which the paper processes densely, pieces of them, drafted tokens, single ones.  Query token j of sequence b
+ * is at position p = first[b] + j and sees token i of the sequence when
+ *     i <= p  and  (window == 0  or  i < sink  or  i > p - window):
+ * all tokens up to itself, or the first `sink` and the last `window` of them.  Its output is the softmax attention (Eq. 1) over these.
+ *   q            device, bf16, token j of sequence b at q + (b n_new + j) q_stride, its heads [Hq, d] packed
+ *   q_stride     elements between tokens, a multiple of 8, at least Hq d
+ *   n_new        1 .. n_max; need not be the plan's q_len
+ *   first        device, int32 [B]; a sequence with first[b] outside [0, n_max) has no new tokens
+ *   new_lens     device, int32 [B] or NULL: only the first new_lens[b] tokens of sequence b count (clamped to [0, n_new]; NULL: all), and
+ *                none at n_max or beyond
+ *   k, v         device, the cache in the plan's format
+ *   sink         >= 0; without a meaning when window is 0
+ *   window       >= 0
+ *   workspace    device, 256-byte aligned, vatt_chunk_workspace_bytes(plan, n_new) bytes; NULL where that is 0
+ *   out_type     VATT_OUT_F32 or VATT_OUT_BF16: the type of out_o.  With the latter the softmax weights are rounded to bf16 too before
+ *                they meet V (sums in 32 bits), which halves the work; with the former they keep 24 bits
+ *   out_o        device [B, n_new, Hq, d]; rows of tokens that do not count are left as they were
+ *   out_lse      device, float [B, n_new, Hq] or NULL: ln of the sum of exponentials; likewise
+ * Rows of the cache that a query does not see have no say, whatever they hold.  No output may overlap an input.  Pointers 16-byte
+ * aligned (lengths, out_lse: 4).  Errors as in vatt_decode.
+ */
+enum { VATT_OUT_F32 = 0, VATT_OUT_BF16 = 1 };
+size_t vatt_chunk_workspace_bytes(const vatt_plan* plan, int n_new); /* 0 also for an n_new that the call refuses */
+int vatt_chunk_attend(vatt_plan* plan, const void* q, int64_t q_stride, int n_new, const int32_t* first, const int32_t* new_lens,
+                      const void* k, const void* v, const int32_t* block_table, int sink, int window, void* workspace,
+                      size_t workspace_bytes, int out_type, void* out_o, float* out_lse, void* stream);
+
+/*
+ * A decode step over the first `sink` (>= 0) and the last `window` (>= 1) tokens that each query sees, its own among them: the
+ * deterministic set of Algorithm 1 without top-k and samples, for layers that attend to a window.  The sizes are the call's, not
+ * those of the plan.  K and V in the plan's format; other arguments as in vatt_dense_decode.
+ */
+int vatt_window_decode(vatt_plan* plan, const void* q, const void* k, const void* v, const int32_t* block_table,
+                       const int32_t* seq_lens, int sink, int window, void* workspace, size_t workspace_bytes, float* out_o,
+                       float* out_lse, void* stream);
 
 /*
  * KV cache in host memory (the paper's efficiency experiment hosts the KV cache on the CPU and finds the time

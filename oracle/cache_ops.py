@@ -182,3 +182,18 @@ def attend(q, k, v, scale):
             return np.full(len(q), math.nan), -math.inf
         p = np.exp(s - m)
         return (p[:, None] * v).sum(0) / p.sum(), m + math.log(p.sum()) if not math.isnan(p.sum()) else math.nan
+
+
+# ---- new tokens ------------------------------------------------------------------------------------------------------------
+
+def visible(p, sink, window):
+    """Tokens that a query at position p sees: all up to its own, or (window > 0) the first `sink` and the last `window` of them."""
+    i = np.arange(p + 1)
+    return i if window == 0 else i[(i < sink) | (i > p - window)]
+
+
+def new_tokens(first, want, n_new, n_max):
+    """How many of a sequence's new tokens count: none where the first one's position is outside the cache, none behind its end."""
+    if first < 0 or first >= n_max:
+        return 0
+    return min(max(0, min(want, n_new)), n_max - first)

@@ -42,6 +42,7 @@ VATT_OPT_GIVEN_FUSED = 16
 VATT_OPT_KV_FORMAT = 17
 VATT_OPT_BLOCK_TOKENS = 18
 VATT_KV_BF16, VATT_KV_E4M3, VATT_KV_E2M1 = 0, 1, 2
+VATT_OUT_F32, VATT_OUT_BF16 = 0, 1
 VATT_ROTARY_HALF, VATT_ROTARY_PAIRS = 0, 1
 VATT_ROTARY_NONE, VATT_ROTARY_LINEAR, VATT_ROTARY_WAVELENGTH, VATT_ROTARY_YARN = 0, 1, 2, 3
 VATT_BOUND_CLT = 0
@@ -56,6 +57,7 @@ EXPORTS = [
     "vatt_decode_given_topk_cached", "vatt_random_cache_read",
     "vatt_kv_cache_bytes", "vatt_kv_scale_offset", "vatt_block_summary_bytes", "vatt_block_list_capacity", "vatt_plan_set_rotary",
     "vatt_write_kv", "vatt_read_kv", "vatt_block_summary_fill", "vatt_select_blocks", "vatt_block_decode",
+    "vatt_chunk_workspace_bytes", "vatt_chunk_attend", "vatt_window_decode",
     "vatt_host_kv_device_pointer", "vatt_status_string",
 ]
 
@@ -161,6 +163,12 @@ def _load():
     lib.vatt_select_blocks.restype = ctypes.c_int
     lib.vatt_block_decode.argtypes = [vp] * 9 + [sz] + [vp] * 3
     lib.vatt_block_decode.restype = ctypes.c_int
+    lib.vatt_chunk_workspace_bytes.argtypes = [vp, ctypes.c_int]
+    lib.vatt_chunk_workspace_bytes.restype = sz
+    lib.vatt_chunk_attend.argtypes = [vp, vp, i64, ctypes.c_int] + [vp] * 5 + [ctypes.c_int] * 2 + [vp, sz, ctypes.c_int] + [vp] * 3
+    lib.vatt_chunk_attend.restype = ctypes.c_int
+    lib.vatt_window_decode.argtypes = [vp] * 6 + [ctypes.c_int] * 2 + [vp, sz] + [vp] * 3
+    lib.vatt_window_decode.restype = ctypes.c_int
     lib.vatt_status_string.argtypes = [ctypes.c_int]
     lib.vatt_status_string.restype = ctypes.c_char_p
     return lib
@@ -413,6 +421,27 @@ def vatt_block_decode(plan, q, k, v, block_table, seq_lens, blocks, block_count,
                                 _ptr(stream))
     if rc != VATT_OK:
         raise VattError(rc, "vatt_block_decode")
+
+
+def vatt_chunk_workspace_bytes(plan, n_new: int) -> int:
+    return int(_lib.vatt_chunk_workspace_bytes(plan, n_new))
+
+
+def vatt_chunk_attend(plan, q, q_stride, n_new, first, new_lens, k, v, block_table, sink, window, workspace, out_type, out_o, out_lse,
+                      stream=None) -> None:
+    """The stride is elements between tokens: see token_stride.  `workspace` may be None where the call needs none."""
+    rc = _lib.vatt_chunk_attend(plan, _ptr(q), q_stride, n_new, _ptr(first), _ptr(new_lens), _ptr(k), _ptr(v), _ptr(block_table), sink,
+                                window, _ptr(workspace), 0 if workspace is None else _nbytes(workspace), out_type, _ptr(out_o),
+                                _ptr(out_lse), _ptr(stream))
+    if rc != VATT_OK:
+        raise VattError(rc, "vatt_chunk_attend")
+
+
+def vatt_window_decode(plan, q, k, v, block_table, seq_lens, sink, window, workspace, out_o, out_lse, stream=None) -> None:
+    rc = _lib.vatt_window_decode(plan, _ptr(q), _ptr(k), _ptr(v), _ptr(block_table), _ptr(seq_lens), sink, window, _ptr(workspace),
+                                 _nbytes(workspace), _ptr(out_o), _ptr(out_lse), _ptr(stream))
+    if rc != VATT_OK:
+        raise VattError(rc, "vatt_window_decode")
 
 
 def vatt_row_read(src, rows_total: int, rows, count: int, sink, stream=None) -> None:

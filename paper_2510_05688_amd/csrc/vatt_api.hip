@@ -826,6 +826,45 @@ int vatt_block_decode(vatt_plan* plan, const void* q, const void* k, const void*
   return VATT_OK;
 }
 
+size_t vatt_chunk_workspace_bytes(const vatt_plan* plan, int n_new) {
+  if (!plan || n_new < 1 || n_new > plan->pl.p.n_max) return 0;
+  return chunk_workspace_bytes(plan->pl, n_new);
+}
+
+int vatt_chunk_attend(vatt_plan* plan, const void* q, int64_t q_stride, int n_new, const int32_t* first, const int32_t* new_lens,
+                      const void* k, const void* v, const int32_t* block_table, int sink, int window, void* workspace,
+                      size_t workspace_bytes, int out_type, void* out_o, float* out_lse, void* stream) {
+  if (!plan) return VATT_E_INVALID_ARG;
+  const Plan& pl = plan->pl;
+  if (!q || !first || !k || !v || !out_o || q == out_o) return VATT_E_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out_o)) return VATT_E_INVALID_ARG;
+  if (n_new < 1 || n_new > pl.p.n_max || q_stride < (int64_t)pl.p.n_q_heads * pl.p.head_dim || q_stride % 8 != 0) return VATT_E_INVALID_ARG;
+  if (sink < 0 || window < 0 || (out_type != VATT_OUT_F32 && out_type != VATT_OUT_BF16)) return VATT_E_INVALID_ARG;
+  if (!chunk_fits(pl, n_new)) return VATT_E_UNSUPPORTED_SHAPE;
+  const int rc = check_cache(plan, block_table);
+  if (rc != VATT_OK) return rc;
+  const size_t need = chunk_workspace_bytes(pl, n_new);
+  if (need > 0 && !workspace) return VATT_E_INVALID_ARG;
+  if (workspace_bytes < need) return VATT_E_WORKSPACE_TOO_SMALL;
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return VATT_E_INVALID_ARG;
+  VATT_LAUNCH(launch_chunk(pl, q, q_stride, n_new, first, new_lens, k, v, block_table, sink, window, workspace, out_type == VATT_OUT_BF16,
+                           out_o, out_lse, static_cast<hipStream_t>(stream)));
+  return VATT_OK;
+}
+
+int vatt_window_decode(vatt_plan* plan, const void* q, const void* k, const void* v, const int32_t* block_table,
+                       const int32_t* seq_lens, int sink, int window, void* workspace, size_t workspace_bytes, float* out_o,
+                       float* out_lse, void* stream) {
+  if (!plan) return VATT_E_INVALID_ARG;
+  if (!q || !k || !v || !seq_lens || !out_o || sink < 0 || window < 1) return VATT_E_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return VATT_E_INVALID_ARG;
+  const int rc = check_common(plan, workspace, workspace_bytes, block_table);
+  if (rc != VATT_OK) return rc;
+  VATT_LAUNCH(launch_window(plan->pl, q, k, v, block_table, seq_lens, sink, window, workspace, out_o, out_lse,
+                            static_cast<hipStream_t>(stream)));
+  return VATT_OK;
+}
+
 const char* vatt_status_string(int status) {
   switch (status) {
     case VATT_OK: return "ok";

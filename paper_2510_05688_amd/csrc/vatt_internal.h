@@ -262,6 +262,14 @@ hipError_t launch_select_blocks(const Plan& pl, const void* q, const void* summa
 hipError_t launch_attend(const Plan& pl, const void* q, const void* k, const void* v, const int32_t* block_table,
                          const int32_t* seq_lens, const int32_t* blocks, const int32_t* block_count, void* ws, float* out_o,
                          float* out_lse, hipStream_t st);
+// Attention of new tokens over the cache (vatt_chunk_attend) and of a decode step over the first tokens and a window.
+bool chunk_fits(const Plan& pl, int n_new);  // whether the launch has room for so many tiles
+size_t chunk_workspace_bytes(const Plan& pl, int n_new);
+hipError_t launch_chunk(const Plan& pl, const void* q, int64_t q_stride, int n_new, const int32_t* first, const int32_t* new_lens, const void* k,
+                        const void* v, const int32_t* block_table, int sink, int window, void* ws, bool bf16, void* out_o, float* out_lse,
+                        hipStream_t st);
+hipError_t launch_window(const Plan& pl, const void* q, const void* k, const void* v, const int32_t* block_table, const int32_t* seq_lens,
+                         int sink, int window, void* ws, float* out_o, float* out_lse, hipStream_t st);
 hipError_t set_kernel_attributes(const Plan& pl);        // every selection kernel: dynamic LDS limit
 hipError_t set_budget_kernel_attributes();
 hipError_t set_given_kernel_attributes(const Plan& pl);  // (its part for the caller-supplied-top-k kernels)

@@ -21,6 +21,10 @@ def _bf16_from_bits(bits: np.ndarray, device) -> torch.Tensor:
 class DecodeSession:
     """Owns a plan, its workspace and output buffers on one GPU."""
 
+    # where the tokens of the last write() begin, and whether that still holds (the buffer stays, for captured writes)
+    first: Optional[torch.Tensor] = None
+    written = False
+
     def __init__(self, params: Dict, device: int = 0, q_len: int = 1, kv_format: int = vb.VATT_KV_BF16,
                  block_tokens: Optional[int] = None, rotary: Optional[Dict] = None):
         """kv_format, block_tokens, rotary: the cache's format (VATT_KV_*), the tokens per block and the rotation
@@ -59,6 +63,7 @@ class DecodeSession:
         self.block_table: Optional[torch.Tensor] = None
         self.q = self.k = self.v = self.seq_lens = self.seq_seeds = self.rcache = self.cache_seeds = None
         self.summary = self.blocks = self.block_count = None
+        self.first = torch.zeros(p["batch"], dtype=torch.int32, device=dev)
 
     def _new_plan(self):
         device = -1 if self.device.type == "cpu" else self.device.index
@@ -96,6 +101,7 @@ class DecodeSession:
         self.seq_seeds = torch.from_numpy(np.ascontiguousarray(seeds, dtype=np.uint64).view(np.int64)).to(dev)
         self.block_table = None
         self.summary = self.blocks = self.block_count = None  # (of make_cache's cache only)
+        self.written = False
         if block_table is not None:
             self.block_table = torch.from_numpy(np.ascontiguousarray(block_table, dtype=np.int32)).to(dev)
         return self
@@ -153,6 +159,7 @@ class DecodeSession:
         return tok.cpu().numpy(), cnt.cpu().numpy()
 
     def append_device_cached(self, k_new, v_new):
+        self.written = False
         self._renew_summary(k_new, v_new)
         vb.vatt_append_kv_cached(self.plan, k_new, v_new, self.k, self.v, self.block_table, self.seq_lens,
                                  self.cache_seeds, self.rcache, self._stream())
@@ -181,6 +188,7 @@ class DecodeSession:
     def append_device(self, k_new, v_new):
         """Append one token per sequence from tensors that are already on the device (bf16 [B, Hkv, d]).  The summaries
         of their blocks follow, if there are any."""
+        self.written = False
         self._renew_summary(k_new, v_new)
         vb.vatt_append_kv(self.plan, k_new, v_new, self.k, self.v, self.block_table, self.seq_lens, self._stream())
 
@@ -194,6 +202,7 @@ class DecodeSession:
             if np.size(block_table) != want:
                 raise ValueError(f"block_table: a paged plan's has {want} entries, got {np.shape(block_table)}")
         self.q = self.seq_seeds = self.rcache = self.cache_seeds = None  # (of other sequences)
+        self.written = False
         self.k, self.v = (torch.zeros(vb.vatt_kv_cache_bytes(self.plan), dtype=torch.uint8, device=dev) for _ in range(2))
         self.block_table = None
         if block_table is not None:
@@ -252,12 +261,47 @@ class DecodeSession:
             self._check("out_q", out_q, torch.bfloat16, *q.shape)
         elif q is not None:
             out_q = torch.zeros(q.shape, dtype=torch.bfloat16, device=self.device)
-        lens = torch.empty_like(self.seq_lens)
-        vb.vatt_write_kv(self.plan, q, k_new, v_new, 0 if q is None else vb.token_stride(q), vb.token_stride(k_new),
-                         vb.token_stride(v_new), k_new.shape[1], self.seq_lens, new_lens, self.k, self.v, self.block_table,
-                         self.summary, out_q, lens, self._stream())
-        self.seq_lens.copy_(lens)
+        strides = [0 if x is None else vb.token_stride(x) for x in (q, k_new, v_new)]
+        self.written = False
+        if self.first is None:
+            self.first = torch.empty_like(self.seq_lens)
+        self.first.copy_(self.seq_lens)
+        vb.vatt_write_kv(self.plan, q, k_new, v_new, *strides, k_new.shape[1], self.first, new_lens, self.k, self.v, self.block_table,
+                         self.summary, out_q, self.seq_lens, self._stream())
+        self.written = True
         return out_q
+
+    def attend(self, q, new_lens=None, sink=0, window=0, dtype=torch.bfloat16, out=None, lse=None, first=None):
+        """Attention of the tokens of the last write() over the cache, each over all tokens up to itself or (window > 0) over the first
+        `sink` and the last `window` of them.  q: their rotated queries, bf16 [B, n_new, Hq, d]; new_lens: as in that write.  Returns
+        (output in `dtype`, bfloat16 or float32, [B, n_new, Hq, d]; ln of the sums, float32 [B, n_new, Hq]), zeros for tokens that do
+        not count; with `out` (its type counts) or `lse` they go there, and such rows stay as they are.  first: int32 [B], where the
+        tokens begin, if they are not those of the last write()."""
+        want = (self.params["batch"], q.shape[1] if q.dim() == 4 else 0, self.Hq, self.d)
+        if q.shape != want or q.dtype != torch.bfloat16 or q.device != self.device:
+            raise ValueError(f"expected bfloat16 [{want[0]}, n_new, {want[2]}, {want[3]}] on {self.device}, got {q.dtype} {tuple(q.shape)} on {q.device}")
+        if first is None and not self.written:
+            raise ValueError("no write() to go by: give the tokens' first positions")
+        self._check("new_lens", new_lens, torch.int32, want[0])
+        self._check("first", first, torch.int32, want[0])
+        dtype = dtype if out is None else out.dtype
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"output in bfloat16 or float32, not {dtype}")
+        self._check("out", out, dtype, *want)
+        self._check("lse", lse, torch.float32, *want[:3])
+        out = torch.zeros(want, dtype=dtype, device=self.device) if out is None else out
+        lse = torch.zeros(want[:3], dtype=torch.float32, device=self.device) if lse is None else lse
+        need = vb.vatt_chunk_workspace_bytes(self.plan, want[1])
+        workspace = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        vb.vatt_chunk_attend(self.plan, q, vb.token_stride(q), want[1], self.first if first is None else first, new_lens, self.k, self.v,
+                             self.block_table, sink, window, workspace, vb.VATT_OUT_BF16 if dtype == torch.bfloat16 else vb.VATT_OUT_F32,
+                             out, lse, self._stream())
+        return out, lse
+
+    def window_decode(self, sink: int, window: int, q=None):
+        """A decode step over the first `sink` and the last `window` tokens, into out_o and out_lse."""
+        vb.vatt_window_decode(self.plan, self._query(q), self.k, self.v, self.block_table, self.seq_lens, sink, window, self.workspace,
+                              self.out_o, self.out_lse, self._stream())
 
     def _check(self, name, x, dtype, *shape):
         """A kernel gets x as an address: x has to be a tensor of so many values, one behind the other, on this device (None is left to

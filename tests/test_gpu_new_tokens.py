@@ -1,0 +1,444 @@
+"""Attention of new tokens over the cache (vatt_chunk_attend) and decode steps over a window and the first tokens
+(vatt_window_decode) against the 64-bit oracle."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_ops as co
+from test_gpu_cache_ops import HALF_BF16, Setup, _bf16, _np
+
+pytestmark = pytest.mark.gpu
+
+FILL = 7.5  # what output rows hold that nobody writes
+INF, NAN = math.inf, math.nan
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _chunk(s, q, first, new, sink, window, bf16, stride=None, lse=True):
+    batch, n_new = q.shape[:2]
+    o = torch.full((batch, n_new, s.hq, s.d), FILL, dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda")
+    out_lse = torch.full((batch, n_new, s.hq), FILL, device="cuda") if lse else None
+    need = s.vb.vatt_chunk_workspace_bytes(s.plan, n_new)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    s.vb.vatt_chunk_attend(s.plan, q, stride or s.vb.token_stride(q), n_new, s.ints(first), None if new is None else s.ints(new), s.k, s.v, s.table,
+                           sink, window, ws, s.vb.VATT_OUT_BF16 if bf16 else s.vb.VATT_OUT_F32, o, out_lse, _stream())
+    torch.cuda.synchronize()
+    return o, out_lse
+
+
+def _close(got, want, size, bf16, at):
+    """got against want for one row; size: the weighted mean of |V| per column.  32 bits: scores and weights as in vatt_dense_decode.  bf16:
+    every weight off by half a step of bf16, then the result by half a step, with what 32 bits leave in between."""
+    ok = np.isfinite(want)
+    assert np.array_equal(got[~ok], want[~ok], equal_nan=True), at
+    norm = np.linalg.norm(want[ok])
+    if not bf16:
+        assert np.linalg.norm(got[ok] - want[ok]) <= 2e-5 * norm, at
+        return
+    weights = HALF_BF16 * size[ok] + 2e-5 * norm
+    assert (np.abs(got[ok] - want[ok]) <= weights + HALF_BF16 * (np.abs(want[ok]) + weights)).all(), at
+
+
+def _check_rows(s, q, places, sink, window, o, lse, bf16, finite=True):
+    """places[b]: positions of the query tokens of sequence b that count; q, o, lse [B, n_new, Hq, ..]."""
+    qh, oh, lh = _np(q), _np(o), None if lse is None else _np(lse)
+    g, scale = s.hq // s.hkv, s.params["sm_scale"] or 1 / math.sqrt(s.d)
+    for b, ps in enumerate(places):
+        rest = oh[b, len(ps):]
+        assert (rest == FILL).all() and (lh is None or (lh[b, len(ps):] == FILL).all()), ("rows that do not count", b)
+        for h in range(s.hkv if len(ps) else 0):
+            n = max(ps) + 1
+            k, v = s.rows(s.k, b, h, range(n)), s.rows(s.v, b, h, range(n))
+            heads = slice(h * g, (h + 1) * g)
+            if finite:  # all rows at once
+                there = np.zeros((len(ps), n), dtype=bool)
+                for t, p in enumerate(ps):
+                    there[t, co.visible(p, sink, window)] = True
+                x = scale * np.einsum("tgd,nd->tgn", qh[b, :len(ps), heads], k)
+                x = np.where(there[:, None], x, -INF)
+                m = x.max(-1, keepdims=True)
+                w = np.exp(x - m)
+                total = w.sum(-1, keepdims=True)
+                want, size, ln = (w @ v) / total, (w @ np.abs(v)) / total, (m + np.log(total))[..., 0]
+            for t, p in enumerate(ps):
+                for j in range(g):
+                    if finite:
+                        a, z, e = want[t, j], size[t, j], ln[t, j]
+                    else:
+                        at = co.visible(p, sink, window)
+                        with np.errstate(invalid="ignore", over="ignore"):
+                            a, e = co.attend(qh[b, t, h * g + j], k[at], v[at], scale)
+                            z = co.attend(qh[b, t, h * g + j], k[at], np.abs(v[at]), scale)[0]
+                    where = (b, t, h * g + j)
+                    _close(oh[b, t, h * g + j], a, z, bf16, where)
+                    if lh is not None:
+                        got = lh[b, t, h * g + j]
+                        if math.isfinite(e):
+                            assert abs(got - e) <= 2e-5 * max(1.0, abs(e)), where
+                        else:
+                            assert np.array_equal(got, e, equal_nan=True), where
+
+
+def _places(s, first, new, n_new):
+    new = [n_new] * s.batch if new is None else new
+    return [list(range(f, f + co.new_tokens(f, m, n_new, s.n_max))) for f, m in zip(first, new)]
+
+
+# ---- chunks --------------------------------------------------------------------------------------------------------------------
+
+CHUNKS = [
+    # (batch, hq, hkv, d, n_max, page, fmt, n_new, first, new_lens, sink, window)
+    (1, 1, 1, 64, 1, 0, 0, 1, [0], None, 0, 0),                                    # one token, the first one
+    (1, 1, 1, 128, 1, 8, 1, 1, [0], [1], 3, 1),
+    (2, 4, 2, 128, 100, 0, 0, 1, [99, 0], None, 0, 0),
+    (2, 4, 1, 128, 65, 0, 0, 65, [0, 0], [65, 64], 0, 0),                          # one key behind a tile's end
+    (1, 8, 1, 64, 300, 16, 0, 300, [0], None, 0, 0),
+    (3, 8, 2, 128, 333, 0, 0, 100, [233, 0, 97], [100, 0, 31], 0, 0),              # one without new tokens
+    (4, 2, 2, 64, 200, 0, 0, 70, [150, -1, 200, 5], [70, 70, 70, -4], 0, 0),        # the end of the cache, firsts outside it
+    (2, 16, 2, 128, 520, 64, 0, 33, [487, 200], None, 0, 0),                       # groups of 8
+    (2, 4, 4, 64, 257, 0, 0, 257, [0, 0], [257, 129], 0, 0),                       # groups of 1
+    (1, 4, 1, 128, 1000, 8, 0, 37, [963], None, 0, 0),                             # pages of 8
+    (2, 4, 2, 128, 390, 16, 1, 190, [200, 3], None, 0, 0),
+    (1, 8, 2, 64, 501, 0, 1, 501, [0], None, 0, 0),                                # scales of a contiguous cache
+    (2, 4, 2, 128, 301, 0, 2, 150, [151, 20], [150, 77], 0, 0),
+    (2, 8, 1, 64, 320, 256, 2, 20, [300, 17], None, 0, 0),
+    (1, 4, 2, 128, 700, 0, 0, 700, [0], None, 4, 100),                             # windows: with first tokens, ...
+    (2, 4, 2, 128, 640, 16, 0, 300, [340, 0], [300, 211], 130, 64),                # ... more than the window, beyond a tile
+    (1, 8, 1, 64, 500, 0, 0, 200, [300], None, 0, 1),                              # ... each its own token only
+    (1, 2, 2, 128, 500, 64, 1, 200, [300], None, 1, 1),
+    (2, 4, 1, 128, 400, 0, 2, 130, [270, 0], None, 37, 65),
+    (1, 4, 1, 64, 300, 0, 0, 300, [0], None, 0, 300),                              # as wide as the cache
+    (1, 4, 1, 64, 300, 0, 0, 300, [0], None, 1 << 30, 5),                          # every token is a first one
+    (1, 4, 1, 128, 300, 0, 0, 77, [200], None, 100, 1 << 30),
+    (1, 2, 1, 128, 2000, 0, 0, 3, [1990], None, 0, 0),                             # few rows, many splits
+    (1, 8, 1, 128, 3001, 32, 1, 5, [2996], None, 70, 1500),
+    (1, 1, 1, 128, 130, 0, 0, 129, [1], None, 0, 0),                               # one row behind a tile of rows
+    (40, 8, 8, 64, 64, 16, 0, 9, [(i * 37) % 64 for i in range(40)], [i % 10 for i in range(40)], 0, 0),
+]
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("case", CHUNKS, ids=lambda c: "-".join(str(x) for x in c[:8]) + f"-{c[10]}-{c[11]}")
+def test_chunk(case, bf16):
+    batch, hq, hkv, d, n_max, page, fmt, n_new, first, new, sink, window = case
+    s = Setup(batch, hq, hkv, d, n_max, page, fmt, None, seed=n_max + n_new)
+    q = _bf16(s.rng.normal(size=(batch, n_new, hq, d)))
+    o, lse = _chunk(s, q, first, new, sink, window, bf16)
+    _check_rows(s, q, _places(s, first, new, n_new), sink, window, o, lse, bf16)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_queries_of_a_fused_projection_and_no_lse(bf16):
+    s = Setup(2, 4, 2, 128, 260, 0, 0, None, seed=1)
+    x = _bf16(s.rng.normal(size=(2, 130, (4 + 2 + 2) * 128)))
+    q = x[..., :4 * 128].unflatten(-1, (4, 128))
+    o, _ = _chunk(s, q, [0, 130], None, 0, 0, bf16, lse=False)
+    _check_rows(s, q, _places(s, [0, 130], None, 130), 0, 0, o, None, bf16)
+
+
+@pytest.mark.parametrize("scale", [0.01, 3.0])
+@pytest.mark.parametrize("fmt", [0, 2])
+def test_chunk_with_another_scale(scale, fmt):
+    """Nearly uniform weights, and ones that the largest score has nearly alone (scores of some 100)."""
+    s = Setup(1, 4, 2, 128, 400, 0, fmt, None, seed=2, sm_scale=scale)
+    q = _bf16(s.rng.normal(size=(1, 200, 4, 128)))
+    for bf16 in (False, True):
+        o, lse = _chunk(s, q, [200], None, 3, 90, bf16)
+        _check_rows(s, q, _places(s, [200], None, 200), 3, 90, o, lse, bf16)
+
+
+def test_chunk_scores_far_apart():
+    """Weights over the whole range of exp; the largest score first, last and in the middle, so that the running maximum moves often."""
+    s = Setup(3, 2, 1, 64, 700, 0, 0, None, sm_scale=1.0)
+    for b, at in enumerate((0, 350, 699)):
+        for tok in range(700):
+            s.set_row(s.k, b, 0, tok, values=np.full(64, -abs(tok - at) / 64.0 / 4.0))
+    q = _bf16(np.ones((3, 100, 2, 64)) * np.array([1.0, 8.0])[:, None])
+    for bf16 in (False, True):
+        o, lse = _chunk(s, q, [600] * 3, None, 0, 0, bf16)
+        _check_rows(s, q, _places(s, [600] * 3, None, 100), 0, 0, o, lse, bf16)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("sink,window", [(0, 0), (5, 40)])
+@pytest.mark.parametrize("page,n_new", [(0, 150), (16, 150), (0, 3)])
+def test_infinity_and_nan_reach_only_the_queries_that_see_them(page, n_new, sink, window, bf16):
+    s = Setup(2, 4, 2, 128, 336, page, 0, None, seed=5)
+    n = [333, 190]
+    first = [x - n_new for x in n]
+    for b in range(2):
+        for h in range(2):
+            for tok, value in ((n[b] - 1, [INF, 1.0, NAN]), (n[b] - 2, [INF, -INF, 1.0]), (first[b] + 1, [-INF, 1.0, 1.0]), (3, [1.0, NAN, 1.0]),
+                               (n[b] // 3, [1.0, 1.0, INF])):
+                row = s.rng.normal(size=128)
+                row[3:6] = value
+                s.set_row(s.v, b, h, tok, values=row)
+            for tok in range(n[b], min(n[b] + 70, 336)):  # behind the sequence
+                s.set_row(s.v, b, h, tok, values=np.full(128, NAN))
+                s.set_row(s.k, b, h, tok, values=np.full(128, INF))
+            low = s.rng.normal(size=128)
+            low[0] = -INF
+            s.set_row(s.k, b, h, n[b] - n_new // 2, values=low)  # a score of -Inf
+    q = s.rng.normal(size=(2, n_new, 4, 128))
+    q[..., 0] = np.abs(q[..., 0]) + 0.1
+    q = _bf16(q)
+    o, lse = _chunk(s, q, first, None, sink, window, bf16)
+    _check_rows(s, q, _places(s, first, None, n_new), sink, window, o, lse, bf16, finite=False)
+
+
+@pytest.mark.parametrize("fmt", [1, 2])
+def test_groups_that_are_nan_reach_only_the_queries_that_see_them(fmt):
+    s = Setup(1, 4, 1, 128, 203, 0, fmt, None, seed=6)
+    odd = np.array([120, 255, 120, 120], dtype=np.uint8)
+    s.set_row(s.v, 0, 0, 150, scales=odd)
+    s.set_row(s.v, 0, 0, 202, scales=odd)
+    s.set_row(s.k, 0, 0, 180, scales=odd)
+    q = _bf16(s.rng.normal(size=(1, 100, 4, 128)))
+    for window in (0, 12):
+        for bf16 in (False, True):
+            o, lse = _chunk(s, q, [100], [90], 0, window, bf16)
+            _check_rows(s, q, _places(s, [100], [90], 100), 0, window, o, lse, bf16, finite=False)
+
+
+def test_first_scores_all_minus_infinity():
+    """A query all of whose scores are -Inf has no softmax (NaN); one that sees a finite score as well has its value."""
+    s = Setup(1, 2, 1, 64, 200, 0, 0, None, seed=7)
+    for tok in range(0, 130):
+        row = s.rng.normal(size=64)
+        row[0] = -INF
+        s.set_row(s.k, 0, 0, tok, values=row)
+    q = s.rng.normal(size=(1, 140, 2, 64))
+    q[..., 0] = np.abs(q[..., 0]) + 0.1
+    q = _bf16(q)
+    for bf16 in (False, True):
+        o, lse = _chunk(s, q, [60], None, 0, 0, bf16)
+        _check_rows(s, q, _places(s, [60], None, 140), 0, 0, o, lse, bf16, finite=False)
+
+
+# ---- decode steps over a window --------------------------------------------------------------------------------------------------
+
+WINDOWS = [
+    # (batch, hq, hkv, d, n_max, page, fmt, q_len, lens, sink, window)
+    (1, 1, 1, 64, 1, 0, 0, 1, [1], 0, 1), (2, 4, 2, 128, 100, 0, 0, 1, [100, 3], 4, 10), (2, 8, 2, 128, 600, 16, 0, 1, [600, 77], 128, 128),
+    (3, 8, 1, 64, 700, 0, 0, 1, [700, 129, 9], 0, 200), (2, 4, 4, 128, 640, 64, 1, 1, [640, 333], 7, 1), (2, 4, 1, 64, 500, 0, 2, 1, [499, 500], 9, 255),
+    (2, 8, 2, 128, 401, 0, 0, 4, [401, 3], 5, 30), (1, 8, 1, 128, 300, 8, 0, 5, [299], 16, 17), (2, 4, 2, 64, 350, 16, 1, 17, [350, 40], 3, 33),
+    (1, 8, 1, 128, 900, 0, 2, 12, [899], 70, 500), (1, 2, 1, 128, 1000, 256, 0, 40, [998], 1, 300), (2, 2, 2, 64, 150, 0, 1, 3, [150, 2], 200, 4),
+    (1, 4, 1, 128, 9000, 0, 0, 1, [8999], 4, 4096), (1, 4, 1, 64, 170752, 64, 1, 1, [170752], 128, 128), (2, 2, 1, 64, 300, 0, 0, 2, [300, 299], 0, 1 << 30),
+    (40, 2, 1, 64, 64, 16, 1, 1, [1 + (i * 37) % 64 for i in range(40)], 2, 7), (1, 4, 4, 128, 64, 0, 0, 1, [64], 1 << 30, 1),
+]
+
+
+def _window(s, q, lens, sink, window, lse=True):
+    o = torch.full((s.batch, s.q_len, s.hq, s.d), FILL, device="cuda")
+    out_lse = torch.full((s.batch, s.q_len, s.hq), FILL, device="cuda") if lse else None
+    s.vb.vatt_window_decode(s.plan, q, s.k, s.v, s.table, s.ints(lens), sink, window, s.ws, o, out_lse, _stream())
+    torch.cuda.synchronize()
+    return o, out_lse
+
+
+def _decode_places(s, lens):
+    return [[max(n - s.q_len + t, 0) for t in range(s.q_len)] for n in lens]
+
+
+@pytest.mark.parametrize("case", WINDOWS, ids=lambda c: "-".join(str(x) for x in c[:8]) + f"-{c[9]}-{c[10]}")
+def test_window_decode(case):
+    batch, hq, hkv, d, n_max, page, fmt, q_len, lens, sink, window = case
+    s = Setup(batch, hq, hkv, d, n_max, page, fmt, None, q_len, seed=n_max + q_len)
+    q = _bf16(s.rng.normal(size=(batch, q_len, hq, d)))
+    o, lse = _window(s, q, lens, sink, window)
+    _check_rows(s, q, _decode_places(s, lens), sink, window, o, lse, False)
+
+
+@pytest.mark.parametrize("q_len", [1, 6])
+@pytest.mark.parametrize("page", [0, 16])
+def test_window_decode_infinity_and_nan(page, q_len):
+    s = Setup(2, 4, 2, 128, 336, page, 0, None, q_len, seed=8)
+    lens = [333, 90]
+    for b, n in enumerate(lens):
+        for h in range(2):
+            for tok, value in ((n - 1, [INF, 1.0, NAN]), (n - 30, [INF, -INF, 1.0]), (n - 31, [1.0, NAN, 1.0]), (3, [-INF, 1.0, 1.0]), (12, [NAN, NAN, NAN])):
+                row = s.rng.normal(size=128)
+                row[3:6] = value
+                s.set_row(s.v, b, h, tok, values=row)
+            for tok in range(n, min(n + 16, 336)):
+                s.set_row(s.v, b, h, tok, values=np.full(128, NAN))
+                s.set_row(s.k, b, h, tok, values=np.full(128, INF))
+            s.set_row(s.k, b, h, 13, values=np.full(128, NAN))  # between the first tokens and the window
+    q = _bf16(s.rng.normal(size=(2, q_len, 4, 128)))
+    for sink, window in ((4, 30), (11, 25), (0, 1), (0, 29)):
+        o, lse = _window(s, q, lens, sink, window)
+        _check_rows(s, q, _decode_places(s, lens), sink, window, o, lse, False, finite=False)
+
+
+def test_windows_as_wide_as_the_sequence_are_dense_attention():
+    s = Setup(2, 8, 2, 128, 512, 16, 0, None, 3, seed=9)
+    q, lens = _bf16(s.rng.normal(size=(2, 3, 8, 128))), [500, 77]
+    o, lse = _window(s, q, lens, 0, 512)
+    do, dlse = torch.empty_like(o), torch.empty_like(lse)
+    s.vb.vatt_dense_decode(s.plan, q, s.k, s.v, s.table, s.ints(lens), s.ws, do, dlse, _stream())
+    co_, clse = _chunk(s, q, [497, 74], None, 0, 0, False)
+    torch.cuda.synchronize()
+    for a, b in ((o, do), (lse, dlse), (co_, do), (clse, dlse)):
+        assert float((a - b).norm() / b.norm()) < 1e-5
+
+
+# ---- together ------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt,page", [(0, 0), (0, 64), (1, 16), (2, 0)])
+def test_a_prompt_in_pieces_then_tokens(fmt, page):
+    """A ragged prompt written and attended to in two pieces gives what it gives whole; single tokens follow, windowed and not."""
+    rot = dict(theta=10000.0)
+    s, whole = (Setup(2, 8, 2, 128, 640, page, fmt, None, rotary=rot, seed=10) for _ in range(2))
+    x = [_bf16(s.rng.normal(size=(2, 400, h, 128))) for h in (8, 2, 2)]
+    lens, got = [370, 201], []
+
+    def piece(c, t0, t1, first, new, sink, window):
+        part = [t[:, t0:t1].contiguous() for t in x]
+        out_q = torch.zeros_like(part[0])
+        c.write(*part, c.ints(first), c.ints(new), None, out_q, None)
+        return out_q, [_chunk(c, out_q, first, new, sink, w, False) for w in (0, window)]
+
+    q, all_at_once = piece(whole, 0, 400, [0, 0], lens, 4, 90)
+    for t0, t1 in ((0, 150), (150, 400)):
+        got.append(piece(s, t0, t1, [t0, t0], [max(min(n, t1) - t0, 0) for n in lens], 4, 90)[1])
+    for w in range(2):
+        for b, n in enumerate(lens):
+            for y in range(2):
+                one, two = all_at_once[w][y][b, :n], torch.cat([g[w][y][b] for g in got])[:n]
+                assert float((one - two).norm() / one.norm()) < 1e-5
+    _check_rows(whole, q, _places(whole, [0, 0], lens, 400), 4, 90, *all_at_once[1], False)
+    for t in range(2):
+        first = [n + t for n in lens]
+        out_q, (dense, windowed) = piece(s, t, t + 1, first, [1, 1], 4, 90)
+        o, lse = _window(s, out_q, [f + 1 for f in first], 4, 90)
+        for a, b in ((o, windowed[0]), (lse, windowed[1])):
+            assert float((a - b).norm() / b.norm()) < 1e-5
+        _check_rows(s, out_q, [[f] for f in first], 0, 0, *dense, False)
+
+
+@pytest.mark.parametrize("fmt,page,n_new", [(1, 16, 40), (0, 0, 1), (0, 0, 150)])
+def test_captured(fmt, page, n_new):
+    """Write, chunk and windowed step captured once and replayed with other inputs in the same buffers, the program's own work between."""
+    s = Setup(3, 8, 2, 128, 512, page, fmt, None, rotary=dict(theta=10000.0), seed=11)
+    x = [_bf16(s.rng.normal(size=(3, n_new, h, 128))) for h in (8, 2, 2)]
+    first, new, after = s.ints([300, 17, 255]), s.ints([n_new, n_new // 2, n_new]), s.ints([0, 0, 0])
+    out_q = torch.zeros_like(x[0])
+    last = torch.zeros((3, 8, 128), dtype=torch.bfloat16, device="cuda")
+    need = s.vb.vatt_chunk_workspace_bytes(s.plan, n_new)
+    ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
+    o, lse = torch.zeros((3, n_new, 8, 128), device="cuda"), torch.zeros((3, n_new, 8), device="cuda")
+    wo, wlse = torch.zeros((3, 8, 128), device="cuda"), torch.zeros((3, 8), device="cuda")
+
+    def step():
+        st = _stream()
+        s.write(*x, first, new, None, out_q, after)
+        s.vb.vatt_chunk_attend(s.plan, out_q, 8 * 128, n_new, first, new, s.k, s.v, s.table, 4, 100, ws, s.vb.VATT_OUT_F32, o, lse, st)
+        last.copy_(out_q[:, 0])
+        s.vb.vatt_window_decode(s.plan, last, s.k, s.v, s.table, after, 4, 33, s.ws, wo, wlse, st)
+
+    outs = (out_q, after, o, lse, wo, wlse)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        for t in x:
+            t.copy_(_bf16(s.rng.normal(size=tuple(t.shape))))
+        first.copy_(s.ints([300 + i, 17 + 3 * i, 255 + 30 * i]))
+        for t in (o, lse, wo, wlse):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        for t in (o, lse, wo, wlse):
+            t.zero_()
+        step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, outs):
+            assert torch.equal(a, b)
+
+
+def test_another_stream():
+    s = Setup(2, 8, 2, 128, 512, 0, 1, None, seed=12)
+    q = _bf16(s.rng.normal(size=(2, 70, 8, 128)))
+    one = _bf16(s.rng.normal(size=(2, 1, 8, 128)))
+    side, res = torch.cuda.Stream(), []
+    for stream in (torch.cuda.current_stream(), side):
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            res.append([*_chunk(s, q, [400, 3], [70, 50], 0, 0, True), *_window(s, one, [470, 53], 4, 50)])
+        stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_a_session(fmt):
+    """As a program does it through DecodeSession: a ragged prompt, a second piece, then tokens over all rows and over a window."""
+    from paper_2510_05688_amd.session import DecodeSession
+    s = Setup(2, 8, 2, 128, 256, 32, fmt, None, rotary=dict(theta=10000.0), seed=13)
+    sess = DecodeSession(s.params, kv_format=fmt, rotary=dict(theta=10000.0)).make_cache(s.table.cpu().numpy())
+    s.k, s.v = sess.k, sess.v
+    x = [_bf16(s.rng.normal(size=(2, 210, h, 128))) for h in (8, 2, 2)]
+
+    def check(q, places, sink, window, o, lse):
+        whole = [t.float().clone() for t in (o, lse)]
+        for b, ps in enumerate(places):
+            assert not o[b, len(ps):].any() and not lse[b, len(ps):].any()
+            for t in whole:
+                t[b, len(ps):] = FILL
+        _check_rows(s, q, places, sink, window, *whole, o.dtype == torch.bfloat16)
+
+    new = s.ints([130, 77])
+    q = sess.write(*[t[:, :130].contiguous() for t in x], new)
+    check(q, [range(130), range(77)], 0, 0, *sess.attend(q, new))
+    check(q, [range(130), range(77)], 4, 50, *sess.attend(q, new, 4, 50, torch.float32))
+    q = sess.write(*[t[:, 130:190].contiguous() for t in x])
+    assert sess.seq_lens.tolist() == [190, 137] and sess.first.tolist() == [130, 77]
+    check(q, [range(130, 190), range(77, 137)], 0, 0, *sess.attend(q))
+    for t in range(190, 193):
+        q = sess.write(*[y[:, t:t + 1].contiguous() for y in x])
+        o, lse = sess.attend(q, dtype=torch.float32)
+        sess.dense(q)
+        assert float((o.view(2, 8, 128) - sess.dense_o).norm() / sess.dense_o.norm()) < 1e-5
+        sess.window_decode(4, 50, q)
+    check(q, [[192], [139]], 4, 50, sess.out_o[:, None], sess.out_lse[:, None])
+    sess.close()
+
+
+def test_a_session_captured():
+    """A token's write, attention over all rows and over a window through DecodeSession, captured once: every replay goes on where the last
+    one ended."""
+    from paper_2510_05688_amd.session import DecodeSession
+    s = Setup(2, 8, 2, 128, 256, 32, 1, None, rotary=dict(theta=10000.0), seed=21)
+    table = s.table.cpu().numpy()
+    one, two = (DecodeSession(s.params, kv_format=1, rotary=dict(theta=10000.0)).make_cache(table) for _ in range(2))
+    x = [_bf16(s.rng.normal(size=(2, 150, h, 128))) for h in (8, 2, 2)]
+    now = [t[:, :3].clone() for t in x]
+    outs = [[torch.zeros(2, 3, 8, 128, device="cuda"), torch.zeros(2, 3, 8, device="cuda")] for _ in range(2)]
+
+    def step(sess, out):
+        q = sess.write(*now)
+        sess.attend(q, out=out[0], lse=out[1])
+        sess.window_decode(2, 40, q[:, 2].contiguous())
+
+    for sess, out in zip((one, two), outs):
+        sess.write(*x, s.ints([150, 93]))
+        step(sess, out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(one, outs[0])
+    for i in range(4):
+        for t in now:
+            t.copy_(_bf16(s.rng.normal(size=tuple(t.shape))))
+        graph.replay()
+        step(two, outs[1])
+        torch.cuda.synchronize()
+        assert one.seq_lens.tolist() == two.seq_lens.tolist() == [156 + 3 * i, 99 + 3 * i]
+        for a, b in zip((*outs[0], one.out_o, one.out_lse, one.k), (*outs[1], two.out_o, two.out_lse, two.k)):
+            assert torch.equal(a, b)
