@@ -1,5 +1,6 @@
 // Attention of the new tokens of every sequence (a prompt, a piece of one, drafted tokens) over the cache that holds their rows.
 #include <algorithm>
+#include <type_traits>
 
 #include "vatt_format.h"
 
@@ -14,7 +15,9 @@ constexpr int kChunkThreads = 256, kChunkWaves = kChunkThreads / kWave;
 constexpr int kWaveRows = 32;                         // rows (query vectors) of a wave
 constexpr int kTileRows = kWaveRows * kChunkWaves;    // ... of a workgroup
 constexpr int kTileKeys = 64;
-constexpr int kChunkSplitsMax = 64;
+constexpr int kPiecesMax = 64;      // pieces that a tile's keys are cut into at most
+constexpr int kPieceLeast = 4;      // key tiles of a piece at least
+constexpr int kSeqsPerLane = 4, kSeqsMax = kSeqsPerLane * kWave;  // sequences that a wave looks through for its work
 
 struct ChunkArgs {
   const uint16_t* q;
@@ -24,12 +27,14 @@ struct ChunkArgs {
   int64_t scale_off;
   const int32_t* first;
   const int32_t* new_lens;
-  float* part;      // [B * n_new * Hq][splits][d]: sums of the weighted V rows
-  float2* part_ml;  // [B * n_new * Hq][splits]: (max in units of log 2, sum of the weights); max -Inf: no token seen
+  float* part;      // [pieces][kTileRows][d]: sums of the weighted V rows
+  float2* part_ml;  // [pieces][kTileRows]: (max in units of log 2, sum of the weights); max -Inf: no token seen
   void* out_o;
   float* out_lse;
   RowMap M;
-  int batch, Hq, Hkv, n_new, splits, sink, window;
+  int batch, Hq, Hkv, n_new, sink, window;
+  int slots;  // workgroups that run at a time
+  int room;   // pieces of one KV head that the workspace holds
   float log2_scale;  // softmax scale / ln 2
 };
 
@@ -60,17 +65,168 @@ __device__ __forceinline__ KeyTiles key_tiles(const ChunkArgs& A, int p_lo, int 
   return T;
 }
 
-// Where 16-byte chunk c of row `row` lies in a tile in LDS.
-template <int D>
-__device__ __forceinline__ int k_place(int row, int c) {
-  if constexpr (D == 128) return row * 256 + ((c ^ (row & 15)) << 4);
-  else return row * 128 + ((c ^ ((row >> 1) & 7)) << 4);
+__device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane((int)wave_inclusive_scan_u32((uint32_t)v), kWave - 1); }
+
+// What a workgroup does: a tile of rows of one sequence and KV head, over one of `pieces` parts of its keys.
+struct Work {
+  int b, kvh, tile, piece, pieces, slot;  // slot: the piece's place in the workspace
+};
+
+// Pieces that the tiles of sequences are cut into.  total: key tiles of all tiles of one KV head, most: if each had as many as its sequence's last one.
+// Tiles that are long beside what all work comes to per workgroup slot are cut into pieces of about that length, all tiles of a sequence into
+// equally many; their sums are joined by the merge.  (32-bit values, rounded the same way wherever this is worked out.)
+struct Cut {
+  float piece;  // key tiles; 0: nothing is cut
+  __device__ __forceinline__ Cut(const ChunkArgs& A, float total, float most, int longest) {
+#pragma clang fp contract(off)
+    const float share = total * A.Hkv / A.slots;
+    piece = A.room > 0 && longest > 1.25f * share + 12.f ? fmaxf(most * A.Hkv / A.slots, (float)kPieceLeast) : 0.f;
+  }
+  __device__ __forceinline__ int pieces(int last) const { return piece == 0.f || last == 0 ? 1 : min((int)ceilf(last / piece), kPiecesMax); }
+};
+
+// A sequence's tiles: how many, and the key tiles of the first and the last one.
+struct SeqTiles {
+  int tiles, first, last;
+  __device__ __forceinline__ SeqTiles(const ChunkArgs& A, int g_shift, const NewTokens& n) : tiles(0), first(0), last(0) {
+    if (n.count == 0) return;
+    const int tokens = kTileRows >> g_shift, end = n.first + n.count - 1;
+    tiles = ((n.count << g_shift) + kTileRows - 1) / kTileRows;
+    first = key_tiles(A, n.first, min(n.first + tokens - 1, end)).count;
+    last = key_tiles(A, n.first + (tiles - 1) * tokens, end).count;
+  }
+};
+
+// Which of `count` tiles, the longest first, item y is.  Where all run at once, two to a compute unit, a long one shares its unit with a short one.
+__device__ __forceinline__ int order(const ChunkArgs& A, int y, int count) {
+  const int half = A.slots / 2 / A.Hkv;
+  return count * A.Hkv <= A.slots && y >= half && y < count ? count - 1 - (y - half) : y;
 }
+
+// The batch's work, as every wave sees it: lane l has sequences l, l + 64, ...  Pieces come first, then the tiles that are not cut, the longest
+// first: what a tile costs goes by its place in the sequence, counted in tiles (its level).
+struct Batch {
+  int tiles[kSeqsPerLane], pieces[kSeqsPerLane], level[kSeqsPerLane];
+  int cut;  // pieces of one KV head in all
+
+  __device__ __forceinline__ void read(const ChunkArgs& A, int g_shift) {
+    const int lane = threadIdx.x & 63;
+    int last[kSeqsPerLane];
+    float total = 0.f, most = 0.f;
+    int longest = 0;
+#pragma unroll
+    for (int i = 0; i < kSeqsPerLane; ++i) {
+      const int b = lane + i * kWave;
+      tiles[i] = level[i] = last[i] = 0;
+      pieces[i] = 1;
+      if (i * kWave < A.batch && b < A.batch) {
+        const NewTokens n = new_tokens(A, b);
+        const SeqTiles t(A, g_shift, n);
+        tiles[i] = t.tiles;
+        level[i] = n.first / (kTileRows >> g_shift);
+        last[i] = t.last;
+        total += 0.5f * (float)(t.tiles * (t.first + t.last));
+        most += (float)(t.tiles * t.last);
+        longest = max(longest, t.last);
+      }
+    }
+    cut = 0;
+    if (A.room == 0) return;
+    const Cut c(A, wave_sum_f32(total), wave_sum_f32(most), (int)wave_max((float)longest));
+    if (c.piece == 0.f) return;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kSeqsPerLane; ++i) {
+      pieces[i] = c.pieces(last[i]);
+      if (pieces[i] > 1) n += tiles[i] * pieces[i];
+    }
+    cut = wave_total(n);
+    if (cut > A.room) {  // (not reached: see chunk_pieces)
+      cut = 0;
+#pragma unroll
+      for (int i = 0; i < kSeqsPerLane; ++i) pieces[i] = 1;
+    }
+  }
+  // Tiles of whole sequences at a level or above it.
+  __device__ __forceinline__ int above(int l) const {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kSeqsPerLane; ++i) n += pieces[i] == 1 ? max(level[i] + tiles[i] - max(level[i], l), 0) : 0;
+    return wave_total(n);
+  }
+  // Item y of one KV head; false where there is none.
+  __device__ __forceinline__ bool find(const ChunkArgs& A, int y, Work& w) const {
+    const int lane = threadIdx.x & 63;
+    if (y < cut) {
+      int before = 0;
+#pragma unroll
+      for (int i = 0; i < kSeqsPerLane; ++i) {
+        const int mine = pieces[i] > 1 ? tiles[i] * pieces[i] : 0, upto = before + (int)wave_inclusive_scan_u32((uint32_t)mine);
+        const uint64_t hit = __ballot(y >= upto - mine && y < upto);
+        if (hit) {
+          const int l = __builtin_ctzll(hit), from = __builtin_amdgcn_readlane(upto - mine, l);
+          w.pieces = __builtin_amdgcn_readlane(pieces[i], l);
+          w.b = l + i * kWave;
+          w.tile = (y - from) / w.pieces;
+          w.piece = y - from - w.tile * w.pieces;
+          return true;
+        }
+        before = __builtin_amdgcn_readlane(upto, kWave - 1);
+      }
+      return false;
+    }
+    y -= cut;
+    int top = 0;
+#pragma unroll
+    for (int i = 0; i < kSeqsPerLane; ++i) top = max(top, level[i] + tiles[i]);
+    int lo = 0, hi = (int)wave_max((float)top);  // above(lo) > y >= above(hi)
+    const int count = above(0);
+    if (count <= y) return false;
+    y = order(A, y, count);
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (above(mid) > y) lo = mid; else hi = mid;
+    }
+    y -= above(lo + 1);
+    w.piece = 0;
+    w.pieces = 1;
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < kSeqsPerLane; ++i) {
+      const uint64_t there = __ballot(pieces[i] == 1 && level[i] <= lo && lo < level[i] + tiles[i]);
+      const int rank = before + __popcll(there & ((1ull << lane) - 1));
+      const uint64_t hit = __ballot((there >> lane & 1) && rank == y);
+      if (hit) {
+        const int l = __builtin_ctzll(hit);
+        w.b = l + i * kWave;
+        w.tile = lo - __builtin_amdgcn_readlane(level[i], l);
+        return true;
+      }
+      before += __popcll(there);
+    }
+    return false;
+  }
+};
+
+// Which 16-byte chunk of row `row` lies at place `pos` of the row in LDS, and where chunk c lies in a tile (the same exchange): 16 rows' chunks of
+// one column, as K is read, lie in different banks, and so do the four rows by four chunks of V that are read transposed.
 template <int D>
-__device__ __forceinline__ int v_place(int row, int c) {
-  if constexpr (D == 128) return row * 256 + ((c ^ ((row & 3) << 2)) << 4);
-  else return row * 128 + ((c ^ ((row & 2) << 1)) << 4);
+__device__ __forceinline__ int k_chunk(int row, int pos) { return D == 128 ? pos ^ (row & 15) : pos ^ ((row >> 1) & 7); }
+template <int D>
+__device__ __forceinline__ int v_chunk(int row, int pos) { return D == 128 ? pos ^ ((row & 3) << 2) : pos ^ ((row & 2) << 1); }
+template <int D>
+__device__ __forceinline__ int k_place(int row, int c) { return row * (2 * D) + (k_chunk<D>(row, c) << 4); }
+template <int D>
+__device__ __forceinline__ int v_place(int row, int c) { return row * (2 * D) + (v_chunk<D>(row, c) << 4); }
+
+// 16 bytes per lane from global memory into LDS, the lanes' one behind the other from a uniform place on.
+__device__ __forceinline__ void load_lds_16(const unsigned char* src, unsigned char* dst) {
+  typedef const __attribute__((address_space(1))) uint32_t* Global;
+  typedef __attribute__((address_space(3))) uint32_t* Lds;
+  __builtin_amdgcn_global_load_lds((Global)src, (Lds)dst, 16, 0, 0);
 }
+// Until this wave's loads into LDS are there (a barrier waits for the other waves').
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
 
 template <bool BF16>
 __device__ __forceinline__ void store_4(void* out, int64_t at, float a, float b, float c, float d) {
@@ -136,6 +292,37 @@ __device__ __forceinline__ void row_again(const ChunkArgs& A, int b, int kvh, in
   m = all;
 }
 
+// This workgroup's work; false where there is none.  Neighbours have the same tile of all KV heads (workgroups go to the XCDs in turn: with a
+// multiple of 8 KV heads a KV head's rows stay in one L2).
+__device__ __forceinline__ bool find_work(const ChunkArgs& A, int g_shift, Work& w) {
+  const int x = blockIdx.x, y = x / A.Hkv;
+  w.kvh = x - y * A.Hkv;
+  w.slot = x;
+  if (A.batch == 1) {
+    const NewTokens n = new_tokens(A, 0);
+    const SeqTiles t(A, g_shift, n);
+    w.b = 0;
+    w.pieces = Cut(A, 0.5f * (float)(t.tiles * (t.first + t.last)), (float)(t.tiles * t.last), t.last).pieces(t.last);
+    if (w.pieces * t.tiles > A.room) w.pieces = 1;
+    w.tile = w.pieces > 1 ? y / w.pieces : t.tiles - 1 - order(A, y, t.tiles);
+    w.piece = w.pieces > 1 ? y - w.tile * w.pieces : 0;
+    return w.tile >= 0 && w.tile < t.tiles;
+  }
+  if (A.batch <= kSeqsMax) {
+    Batch all;
+    all.read(A, g_shift);
+    return all.find(A, y, w);
+  }
+  // too many sequences to look through: tile by tile from the end, beginning with another sequence each time (short sequences leave workgroups
+  // without work, and those with work should not all be on the same units)
+  const int rank = y / A.batch;
+  w.b = (y - rank * A.batch + rank) % A.batch;
+  w.tile = ((new_tokens(A, w.b).count << g_shift) + kTileRows - 1) / kTileRows - 1 - rank;
+  w.piece = 0;
+  w.pieces = 1;
+  return w.tile >= 0;
+}
+
 // Rows of a KV head: row r is query token r / G, head r % G of the group.  A workgroup takes 128 of them, a wave 32, over the key tiles
 // of its split; the tiles go through LDS in bf16, the next one on its way in registers.
 //   S^T [keys x rows] = K Q^T   and   O^T [d x rows] += V^T P^T,   P = exp(S - m),
@@ -149,26 +336,28 @@ template <int D, int FMT, bool PAGED, int TERMS>
 __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   constexpr int S = D / 16;                        // steps of the first product
   constexpr int E = D / 32;                        // tiles over the head dimension
-  constexpr int LPR = D / 8;                       // 16-byte chunks of a row in LDS
-  constexpr int PASS = kChunkThreads / LPR;        // rows that the workgroup loads at a time
-  constexpr int N = kTileKeys / PASS;
+  constexpr bool QUANT = FMT != VATT_KV_BF16;
   constexpr int TILE = kTileKeys * D * 2;          // bytes
   constexpr float kLazy = 8.0f;
   constexpr bool BF16 = TERMS == 1;
-  __shared__ __align__(256) unsigned char s_kv[2][2][TILE];
+  constexpr int CARRY = BF16 ? 1 : 2;
+  // (objects of their own: what is on its way into one need not be awaited before another is read)
+  __shared__ __align__(256) unsigned char s_k0[TILE], s_k1[TILE], s_v0[TILE], s_v1[TILE];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
-  const int pairs = A.batch * A.Hkv, rank = (int)blockIdx.x / pairs, pair = (int)blockIdx.x - rank * pairs;
-  const int b = pair / A.Hkv, kvh = pair - b * A.Hkv, split = blockIdx.y;
   const int g_shift = 31 - __builtin_clz(A.Hq / A.Hkv), G = 1 << g_shift;
+  Work W;
+  if (!find_work(A, g_shift, W)) return;
+  // (uniform values, as the compiler has to know)
+  const int b = __builtin_amdgcn_readfirstlane(W.b), kvh = W.kvh, tile = __builtin_amdgcn_readfirstlane(W.tile);
+  const int piece = __builtin_amdgcn_readfirstlane(W.piece), pieces = __builtin_amdgcn_readfirstlane(W.pieces);
   const NewTokens New = new_tokens(A, b);
-  const int rows = New.count << g_shift, tile = (rows + kTileRows - 1) / kTileRows - 1 - rank;  // (the longest first)
-  if (tile < 0) return;
+  const int rows = New.count << g_shift;
 
   const int r0 = tile * kTileRows;
   const int p_lo = New.first + (r0 >> g_shift), p_hi = New.first + ((min(r0 + kTileRows, rows) - 1) >> g_shift);
   const KeyTiles T = key_tiles(A, p_lo, p_hi);
-  const int i0 = (int)((int64_t)T.count * split / A.splits), i1 = (int)((int64_t)T.count * (split + 1) / A.splits);
+  const int i0 = T.count * piece / pieces, i1 = T.count * (piece + 1) / pieces;
 
   // the wave's rows
   const int w0 = r0 + wave * kWaveRows;
@@ -182,39 +371,89 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
 #pragma unroll
   for (int s = 0; s < S; ++s) bq[s] = *reinterpret_cast<const uint4*>(A.q + q_at + s * 16 + half * 8);
 
-  // loads: thread tid has chunk tid % LPR of rows tid / LPR + PASS * n
-  const int my_row = tid / LPR, my_chunk = tid % LPR;
-  Chunk<FMT> rk[N], rv[N];
-  uint32_t sk[N], sv[N];
-  auto load = [&](int i) {
+  // The next rows of K and V on their way: bf16 straight into LDS, a 1 KB piece of whole rows per wave and instruction, the lanes' chunks of a
+  // row in the order in which they lie there; codes through registers, 16 columns per lane.  A wave has rows 16 wave .. + 15 of a tile, in
+  // two groups of 8 (of one page each).  Rows behind the last one that anybody sees are that one again.
+  constexpr int ROW = kRowBytes<FMT, D>, LPR = D / 8, RPI = kWave / LPR, LPQ = D / 16, NQ = 16 * LPQ / kWave, QB = ROW / LPQ;
+  uint32_t codes[2][NQ][QUANT ? QB / 4 : 1], scales[2][NQ];
+  const int last_group = p_hi & ~7;
+  struct Rows {
+    RowAt at[2];
+    int left[2];
+  };
+  auto block_of = [&](int i, int g) __attribute__((always_inline)) {
+    return row_block<PAGED>(A.M, b, min(T.at(min(i, i1 - 1)) * kTileKeys + 16 * wave + 8 * g, last_group));
+  };
+  auto rows_of = [&](int i, const int (&blk)[2]) __attribute__((always_inline)) {
+    Rows r;
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const int tok = min(T.at(i) * kTileKeys + my_row + PASS * n, p_hi);
-      const RowAt at = row_at<PAGED>(A.M, b, kvh, tok, row_block<PAGED>(A.M, b, tok));
-      const int64_t off = at.row * kRowBytes<FMT, D> + my_chunk * (kRowBytes<FMT, D> / LPR);
-      rk[n] = load_chunk<FMT>(A.k + off);
-      rv[n] = load_chunk<FMT>(A.v + off);
-      sk[n] = sv[n] = 0;
-      if constexpr (FMT != VATT_KV_BF16) {
-        const int64_t so = A.scale_off + at.scales * (D / 32) + my_chunk / 4;
-        sk[n] = A.k[so];
-        sv[n] = A.v[so];
+    for (int g = 0; g < 2; ++g) {
+      const int tok = min(T.at(i) * kTileKeys + 16 * wave + 8 * g, last_group);
+      r.at[g] = row_at<PAGED>(A.M, b, kvh, tok, blk[g]);
+      r.left[g] = p_hi - tok;
+    }
+    return r;
+  };
+  constexpr std::integral_constant<int, 0> K = {};
+  constexpr std::integral_constant<int, 1> V = {};
+  auto buffer = [&](auto kv, auto parity) __attribute__((always_inline)) {
+    constexpr int I = 2 * decltype(kv)::value + decltype(parity)::value;
+    if constexpr (I == 0) return &s_k0[0];
+    else if constexpr (I == 1) return &s_k1[0];
+    else if constexpr (I == 2) return &s_v0[0];
+    else return &s_v1[0];
+  };
+  auto load = [&](auto which, const Rows& R, auto parity) __attribute__((always_inline)) {
+    constexpr int KV = decltype(which)::value;
+    const unsigned char* src = KV ? A.v : A.k;
+    if constexpr (!QUANT) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const unsigned char* base = src + R.at[g].row * ROW;
+#pragma unroll
+        for (int x = 0; x < 8 / RPI; ++x) {
+          const int r = x * RPI + lane / LPR, row = 8 * g + r, pos = lane % LPR;
+          const int c = KV ? v_chunk<D>(row, pos) : k_chunk<D>(row, pos);
+          const uint32_t off = (uint32_t)(min(r, R.left[g]) * ROW + c * 16);
+          load_lds_16(base + off, buffer(which, parity) + (16 * wave + 8 * g + x * RPI) * 2 * D);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const int row = n * (kWave / LPQ) + lane / LPQ, g = row >> 3, c = lane % LPQ;
+        const int r = min(row & 7, g ? R.left[1] : R.left[0]);
+        const unsigned char* p = src + (g ? R.at[1].row : R.at[0].row) * ROW + (r * ROW + c * QB);
+        if constexpr (QB == 16) {
+          const uint4 x = *reinterpret_cast<const uint4*>(p);
+          codes[KV][n][0] = x.x; codes[KV][n][1] = x.y; codes[KV][n][2] = x.z; codes[KV][n][3] = x.w;
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(p);
+          codes[KV][n][0] = x.x; codes[KV][n][1] = x.y;
+        }
+        scales[KV][n] = src[A.scale_off + (g ? R.at[1].scales : R.at[0].scales) * (D / 32) + (r * (D / 32) + c / 2)];
       }
     }
   };
-  auto store = [&](int i, int buf) {
+  auto store = [&](auto which, auto parity) __attribute__((always_inline)) {
+    constexpr int KV = decltype(which)::value;
+    if constexpr (QUANT) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const int r = my_row + PASS * n;
-      const bool there = T.at(i) * kTileKeys + r <= p_hi;
-      *reinterpret_cast<uint4*>(&s_kv[buf][0][k_place<D>(r, my_chunk)]) = chunk_bf16<FMT>(rk[n], sk[n]);
-      // (rows that nobody sees: whatever lies there has no say)
-      const uint4 v = chunk_bf16<FMT>(rv[n], sv[n]);
-      *reinterpret_cast<uint4*>(&s_kv[buf][1][v_place<D>(r, my_chunk)]) = there ? v : make_uint4(0, 0, 0, 0);
+      for (int n = 0; n < NQ; ++n) {
+        const int row = 16 * wave + n * (kWave / LPQ) + lane / LPQ, c = lane % LPQ;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          Chunk<FMT> x;
+#pragma unroll
+          for (int y = 0; y < QB / 8; ++y) x.w[y] = codes[KV][n][h * (QB / 8) + y];
+          *reinterpret_cast<uint4*>(buffer(which, parity) + (KV ? v_place<D>(row, 2 * c + h) : k_place<D>(row, 2 * c + h))) = chunk_bf16<FMT>(x, scales[KV][n]);
+        }
+      }
     }
   };
 
-  f32x16_t acc[E];
+  f32x16_t acc[E], sc[2];
+  uint4 pb[4][CARRY];  // the weights, in bf16 or in 32 bits, from one step to the next
 #pragma unroll
   for (int e = 0; e < E; ++e)
 #pragma unroll
@@ -222,105 +461,156 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   float mrun = -INFINITY, lrun = 0.f;
   bool any = false;
 
-  if (i0 < i1) {
-    load(i0);
-    store(i0, 0);
-  }
-  __syncthreads();
-  for (int i = i0; i < i1; ++i) {
-    const int buf = (i - i0) & 1, k0 = T.at(i) * kTileKeys;
-    if (i + 1 < i1) load(i + 1);
-    const bool skip = !active || k0 > wp_hi || (A.window > 0 && k0 + kTileKeys - 1 <= wp_lo - A.window && k0 >= A.sink);
-    if (!skip) {
-      f32x16_t sc[2];
+  auto first_product = [&](auto parity) __attribute__((always_inline)) {
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+    for (int s = 0; s < S; ++s) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) sc[x][j] = 0.f;
+      for (int y = 0; y < 2; ++y) {
+        const uint4 a = *reinterpret_cast<const uint4*>(buffer(K, parity) + k_place<D>(col, 2 * s + half) + y * 32 * D * 2);
+        f32x16_t zero;
 #pragma unroll
-      for (int s = 0; s < S; ++s) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const uint4 a = *reinterpret_cast<const uint4*>(&s_kv[buf][0][k_place<D>(col, 2 * s + half) + x * 32 * D * 2]);
-          sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, bq[s]), sc[x], 0, 0, 0);
-        }
-      }
-      const bool edge = k0 + kTileKeys - 1 > wp_lo || (A.window > 0 && k0 <= wp_hi - A.window && k0 + kTileKeys > A.sink);
-      if (edge) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int tok = k0 + x * 32 + 8 * (j / 4) + 4 * half + j % 4;
-            const bool ok = tok <= p && (tok > low || tok < A.sink);
-            sc[x][j] = ok ? sc[x][j] : -INFINITY;
-            any |= ok;
-          }
-      } else {
-        any = true;
-      }
-      float top = sc[0][0];
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) top = fmaxf(top, sc[x][j]);
-      top *= A.log2_scale;
-      if (__ballot(top > mrun + kLazy)) {
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float mnew = fmaxf(mrun, top);
-        const float alpha = mrun == mnew ? 1.f : __builtin_amdgcn_exp2f(mrun - mnew);
-        mrun = mnew;
-        lrun *= alpha;
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] *= alpha;
-      }
-      const float m = mrun == -INFINITY ? 0.f : mrun;  // (so far every score is -Inf: weights 0)
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          sc[x][j] = __builtin_amdgcn_exp2f(fmaf(sc[x][j], A.log2_scale, -m));
-          lrun += sc[x][j];
-        }
-      uint4 pb[4][TERMS];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        float y[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = sc[u / 2][8 * (u % 2) + j];
-#pragma unroll
-        for (int z = 0; z < TERMS; ++z) {
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w[j] = pack_bf16(y[2 * j], y[2 * j + 1]);
-          pb[u][z] = make_uint4(w[0], w[1], w[2], w[3]);
-          if (z + 1 < TERMS) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              y[2 * j] -= bf16_lo(w[j]);
-              y[2 * j + 1] -= bf16_hi(w[j]);
-            }
-          }
-        }
-      }
-      typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
-      const int l16 = lane & 15, c_half = (lane >> 4) & 1;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int r = 16 * u + 4 * half + (l16 >> 2), c = 4 * e + 2 * c_half + ((l16 & 3) >> 1);
-          const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)&s_kv[buf][1][v_place<D>(r, c) + (l16 & 1) * 8]);
-          const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)&s_kv[buf][1][v_place<D>(r + 8, c) + (l16 & 1) * 8]);
-          const bf16x8_t va = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-          for (int z = TERMS - 1; z >= 0; --z)
-            acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, __builtin_bit_cast(bf16x8_t, pb[u][z]), acc[e], 0, 0, 0);
-        }
+        for (int j = 0; j < 16; ++j) zero[j] = 0.f;
+        sc[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, bq[s]), s == 0 ? zero : sc[y], 0, 0, 0);
       }
     }
-    if (i + 1 < i1) store(i + 1, buf ^ 1);
+  };
+  // Masks the scores, and moves the running maximum where one passes it by more than kLazy: true (for the wave) if so, and the factor that
+  // the sums so far take.
+  auto maximum = [&](int k0, float& alpha) __attribute__((always_inline)) {
+    const bool edge = k0 + kTileKeys - 1 > wp_lo || (A.window > 0 && k0 <= wp_hi - A.window && k0 + kTileKeys > A.sink);
+    if (edge) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int tok = k0 + y * 32 + 8 * (j / 4) + 4 * half + j % 4;
+          const bool ok = tok <= p && (tok > low || tok < A.sink);
+          sc[y][j] = ok ? sc[y][j] : -INFINITY;
+          any |= ok;
+        }
+    } else {
+      any = true;
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) top = fmaxf(top, sc[y][j]);
+    top *= A.log2_scale;
+    alpha = 1.f;
+    if (!__ballot(top > mrun + kLazy)) return false;
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float mnew = fmaxf(mrun, top);
+    alpha = mrun == mnew ? 1.f : __builtin_amdgcn_exp2f(mrun - mnew);
+    mrun = mnew;
+    lrun *= alpha;
+    return true;
+  };
+  auto weights = [&](int u, float m) __attribute__((always_inline)) {  // of the keys of step u of the second product
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      y[j] = __builtin_amdgcn_exp2f(fmaf(sc[u / 2][8 * (u % 2) + j], A.log2_scale, -m));
+      lrun += y[j];
+    }
+    if constexpr (BF16) {
+      pb[u][0] = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        pb[u][h] = make_uint4(__float_as_uint(y[4 * h]), __float_as_uint(y[4 * h + 1]), __float_as_uint(y[4 * h + 2]), __float_as_uint(y[4 * h + 3]));
+    }
+  };
+  auto second_product = [&](int u, auto parity) __attribute__((always_inline)) {
+    typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
+    const int l16 = lane & 15, c_half = (lane >> 4) & 1;
+    uint4 term[TERMS];
+    if constexpr (BF16) {
+      term[0] = pb[u][0];
+    } else {
+      float y[8] = {__uint_as_float(pb[u][0].x), __uint_as_float(pb[u][0].y), __uint_as_float(pb[u][0].z), __uint_as_float(pb[u][0].w),
+                    __uint_as_float(pb[u][1].x), __uint_as_float(pb[u][1].y), __uint_as_float(pb[u][1].z), __uint_as_float(pb[u][1].w)};
+#pragma unroll
+      for (int z = 0; z < TERMS; ++z) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          w[j] = pack_bf16(y[2 * j], y[2 * j + 1]);
+          y[2 * j] -= bf16_lo(w[j]);
+          y[2 * j + 1] -= bf16_hi(w[j]);
+        }
+        term[z] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int r = 16 * u + 4 * half + (l16 >> 2), c = 4 * e + 2 * c_half + ((l16 & 3) >> 1);
+      const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(buffer(V, parity) + v_place<D>(r, c) + (l16 & 1) * 8));
+      const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(buffer(V, parity) + v_place<D>(r + 8, c) + (l16 & 1) * 8));
+      const bf16x8_t va = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int z = TERMS - 1; z >= 0; --z)
+        acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, __builtin_bit_cast(bf16x8_t, term[z]), acc[e], 0, 0, 0);
+    }
+  };
+
+  // V is one tile behind K: the second product of tile i - 1 is made while the weights of tile i are, on the matrix cores and beside them.
+  if (i0 < i1) {
+    int blk[2] = {block_of(i0, 0), block_of(i0, 1)};
+    Rows now = rows_of(i0, blk);
+    load(K, now, K);
+    blk[0] = block_of(i0 + 1, 0);
+    blk[1] = block_of(i0 + 1, 1);
+    store(K, K);
+    wait_loads();
     __syncthreads();
+    auto step = [&](int i, auto parity, auto begin) __attribute__((always_inline)) {
+      constexpr std::integral_constant<int, decltype(parity)::value ^ 1> other = {};
+      constexpr bool FIRST = decltype(begin)::value == 1;
+      load(V, now, parity);
+      if (i + 1 < i1) {
+        now = rows_of(i + 1, blk);
+        load(K, now, other);
+      }
+      blk[0] = block_of(i + 2, 0);
+      blk[1] = block_of(i + 2, 1);
+      if (active) {
+        first_product(parity);
+        float alpha;
+        const bool moved = maximum(T.at(i) * kTileKeys, alpha);
+        const float m = mrun == -INFINITY ? 0.f : mrun;  // (so far every score is -Inf: weights 0)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if constexpr (!FIRST) second_product(u, other);
+          weights(u, m);
+        }
+        // (made here, beside the products, not after the branch)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int z = 0; z < CARRY; ++z) asm volatile("" : "+v"(pb[u][z].x), "+v"(pb[u][z].y), "+v"(pb[u][z].z), "+v"(pb[u][z].w));
+        if (!FIRST && moved) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[e] *= alpha;
+        }
+      }
+      store(V, parity);
+      if (i + 1 < i1) store(K, other);
+      wait_loads();
+      __syncthreads();
+    };
+    step(i0, K, V);
+    for (int i = i0 + 1; i < i1; i += 2) {
+      step(i, V, K);
+      if (i + 1 < i1) step(i + 1, K, K);
+    }
+    if (active) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if ((i1 - i0) & 1) second_product(u, K);
+        else second_product(u, V);
+      }
+    }
   }
   if (!active) return;
 
@@ -338,7 +628,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   const int64_t out_row = ((int64_t)b * A.n_new + t) * A.Hq + head;
   const float m_own = saw && mrun == -INFINITY ? -3.0e38f : mrun;
   if (row < rows && !(again >> col & 1)) {
-    if (A.splits == 1) {
+    if (pieces == 1) {
       const float inv = 1.f / l;
 #pragma unroll
       for (int e = 0; e < E; ++e)
@@ -348,7 +638,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
                         acc[e][4 * x + 3] * inv);
       if (A.out_lse && half == 0) A.out_lse[out_row] = m_own * 0.69314718055994530942f + logf(l);
     } else {
-      const int64_t place = out_row * A.splits + split;
+      const int64_t place = (int64_t)W.slot * kTileRows + wave * kWaveRows + col;
 #pragma unroll
       for (int e = 0; e < E; ++e)
 #pragma unroll
@@ -366,13 +656,13 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
     float m, ls, a[8];
     row_again<D, FMT, PAGED>(A, b, kvh, q_c, New.first + ((w0 + c) >> g_shift), T, i0, i1, m, ls, a);
     if (lane >= LPR) continue;
-    if (A.splits == 1) {
+    if (pieces == 1) {
       const float inv = 1.f / ls;
       store_4<BF16>(A.out_o, out_c * D + lane * 8, a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
       store_4<BF16>(A.out_o, out_c * D + lane * 8 + 4, a[4] * inv, a[5] * inv, a[6] * inv, a[7] * inv);
       if (A.out_lse && lane == 0) A.out_lse[out_c] = m * 0.69314718055994530942f + logf(ls);
     } else {
-      const int64_t place = out_c * A.splits + split;
+      const int64_t place = (int64_t)W.slot * kTileRows + wave * kWaveRows + c;
       store_4<false>(A.part, place * D + lane * 8, a[0], a[1], a[2], a[3]);
       store_4<false>(A.part, place * D + lane * 8 + 4, a[4], a[5], a[6], a[7]);
       if (lane == 0) A.part_ml[place] = make_float2(m, ls);
@@ -380,47 +670,88 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   }
 }
 
-// The splits' partial sums together: a wave per row.
+// The pieces' partial sums together: a wave per row, and every fourth row of a tile that was cut.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kChunkThreads) void chunk_merge_kernel(ChunkArgs A) {
-  constexpr int C = D / kWave;
-  static_assert(kChunkSplitsMax <= kWave, "a pair per lane");
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = blockIdx.y;
-  const int row = blockIdx.x * kChunkWaves + wave, t = row / A.Hq;
-  if (t >= new_tokens(A, b).count) return;
-  const int64_t out_row = (int64_t)b * A.n_new * A.Hq + row;
-  const float2 ml = lane < A.splits ? A.part_ml[out_row * A.splits + lane] : make_float2(-INFINITY, 0.f);
-  const float m = wave_max(ml.x);
-  const bool counts = ml.x > -INFINITY;  // (a piece without a token, whose sums nobody wrote, does not)
-  const float w = !counts ? 0.f : ml.x == m ? 1.f : __builtin_amdgcn_exp2f(ml.x - m);
-  const float l = wave_sum_f32(counts ? ml.y * w : 0.f);
-  const uint64_t there = __ballot(counts);
-  float a[C];
+  constexpr int C = D / kWave, kAhead = 8;
+  static_assert(kPiecesMax <= kWave, "a pair per lane");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kvh = blockIdx.x % A.Hkv;
+  const int g_shift = 31 - __builtin_clz(A.Hq / A.Hkv);
+  Batch all;
+  all.read(A, g_shift);
+  for (int y = blockIdx.x / A.Hkv; y < all.cut; y += gridDim.x / A.Hkv) {
+    Work w;
+    if (!all.find(A, y, w)) return;
+    const NewTokens New = new_tokens(A, w.b);
+    // (every piece of a tile takes its share of the tile's rows)
+    const int n = min((New.count << g_shift) - w.tile * kTileRows, kTileRows);
+    for (int r = w.piece * kChunkWaves + wave; r < n; r += w.pieces * kChunkWaves) {
+      const int row = w.tile * kTileRows + r;
+      const int64_t out_row = ((int64_t)w.b * A.n_new + (row >> g_shift)) * A.Hq + ((int64_t)kvh << g_shift) + (row & ((1 << g_shift) - 1));
+      const int slot0 = (y - w.piece) * A.Hkv + kvh;
+      auto place = [&](int s) { return (int64_t)(slot0 + s * A.Hkv) * kTileRows + r; };
+      const float2 ml = lane < w.pieces ? A.part_ml[place(lane)] : make_float2(-INFINITY, 0.f);
+      const float m = wave_max(ml.x);
+      const bool counts = ml.x > -INFINITY;  // (a piece without a token, whose sums nobody wrote, does not)
+      const float f = !counts ? 0.f : ml.x == m ? 1.f : __builtin_amdgcn_exp2f(ml.x - m);
+      const float l = wave_sum_f32(counts ? ml.y * f : 0.f);
+      const uint64_t there = __ballot(counts);
+      float a[C];
 #pragma unroll
-  for (int c = 0; c < C; ++c) a[c] = 0.f;
-  for (int s = 0; s < A.splits; ++s) {
-    if (!(there >> s & 1)) continue;
-    const float f = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s));
+      for (int c = 0; c < C; ++c) a[c] = 0.f;
+      for (int s0 = 0; s0 < w.pieces; s0 += kAhead) {
+        float x[kAhead][C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) a[c] += f * A.part[(out_row * A.splits + s) * D + lane * C + c];
+        for (int u = 0; u < kAhead; ++u) {
+#pragma unroll
+          for (int c = 0; c < C; ++c) x[u][c] = A.part[place(min(s0 + u, w.pieces - 1)) * D + lane * C + c];
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          if (s0 + u >= w.pieces || !(there >> (s0 + u) & 1)) continue;
+          const float g = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), s0 + u));
+#pragma unroll
+          for (int c = 0; c < C; ++c) a[c] += g * x[u][c];
+        }
+      }
+      const float inv = 1.f / l;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const float o = a[c] * inv;
+        if constexpr (BF16) static_cast<uint16_t*>(A.out_o)[out_row * D + lane * C + c] = (uint16_t)pack_bf16(o, o);
+        else static_cast<float*>(A.out_o)[out_row * D + lane * C + c] = o;
+      }
+      if (A.out_lse && lane == 0) A.out_lse[out_row] = m * 0.69314718055994530942f + logf(l);
+    }
   }
-  const float inv = 1.f / l;
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const float o = a[c] * inv;
-    if constexpr (BF16) static_cast<uint16_t*>(A.out_o)[out_row * D + lane * C + c] = (uint16_t)pack_bf16(o, o);
-    else static_cast<float*>(A.out_o)[out_row * D + lane * C + c] = o;
-  }
-  if (A.out_lse && lane == 0) A.out_lse[out_row] = m * 0.69314718055994530942f + logf(l);
+}
+
+// Tiles of all sequences if every new token counts, and pieces of tiles at most: a sequence's tiles are cut where they are longer than the piece,
+// of which all tiles at their longest have no more than there are slots, so that the rounding up at most doubles that.
+int64_t chunk_tiles(const Plan& pl, int n_new) {
+  return (int64_t)pl.p.batch * pl.p.n_kv_heads * (((int64_t)n_new * pl.group + kTileRows - 1) / kTileRows);
+}
+int chunk_slots(const Plan& pl) { return 2 * pl.num_cus; }
+// Whether pieces can be wanted at all: one sequence whose new tokens all count is as long as the capacity at most.
+bool chunk_may_cut(const Plan& pl, int n_new, bool all_count) {
+  const int64_t longest = (pl.p.n_max + kTileKeys - 1) / kTileKeys;
+  if (pl.p.batch > 1 || !all_count) return longest > 12;
+  return longest > 12 && chunk_tiles(pl, n_new) < chunk_slots(pl);
+}
+int64_t chunk_pieces(const Plan& pl, int n_new) {
+  const int64_t longest = (pl.p.n_max + kTileKeys - 1) / kTileKeys, each = std::min<int64_t>((longest + kPieceLeast - 1) / kPieceLeast, kPiecesMax);
+  if (pl.p.batch > kSeqsMax || longest <= 12) return 0;
+  return std::min<int64_t>(2 * chunk_slots(pl), chunk_tiles(pl, n_new) * each);
 }
 
 template <int D, int FMT, bool PAGED, int TERMS>
 hipError_t launch_chunk_t(const Plan& pl, const ChunkArgs& A, hipStream_t st) {
-  const int ranks = (A.n_new * pl.group + kTileRows - 1) / kTileRows;
-  hipLaunchKernelGGL((chunk_kernel<D, FMT, PAGED, TERMS>), dim3(ranks * A.batch * A.Hkv, A.splits), dim3(kChunkThreads), 0, st, A);
+  const int64_t tiles = chunk_tiles(pl, A.n_new), pieces = (int64_t)A.room * A.Hkv;
+  hipLaunchKernelGGL((chunk_kernel<D, FMT, PAGED, TERMS>), dim3((uint32_t)(tiles + pieces)), dim3(kChunkThreads), 0, st, A);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || A.splits == 1) return e;
-  hipLaunchKernelGGL((chunk_merge_kernel<D, TERMS == 1>), dim3((A.n_new * A.Hq + kChunkWaves - 1) / kChunkWaves, A.batch), dim3(kChunkThreads), 0, st, A);
+  if (e != hipSuccess || A.room == 0) return e;
+  const int64_t wgs = std::min<int64_t>(A.room, (4 * pl.num_cus + A.Hkv - 1) / A.Hkv);
+  hipLaunchKernelGGL((chunk_merge_kernel<D, TERMS == 1>), dim3((uint32_t)(wgs * A.Hkv)), dim3(kChunkThreads), 0, st, A);
   return hipGetLastError();
 }
 template <int D, int FMT>
@@ -436,28 +767,27 @@ hipError_t launch_chunk_d(const Plan& pl, const ChunkArgs& A, bool bf16, hipStre
   return launch_chunk_f<D, VATT_KV_BF16>(pl, A, bf16, st);
 }
 
-// Workgroups that share out a tile's keys: two per CU in all, none for less than four tiles of the capacity.
-int chunk_splits(const Plan& pl, int n_new) {
-  const int64_t tiles = (int64_t)pl.p.batch * pl.p.n_kv_heads * (((int64_t)n_new * pl.group + kTileRows - 1) / kTileRows);
-  if (tiles >= pl.num_cus) return 1;
-  const int64_t splits = (2 * pl.num_cus + tiles - 1) / tiles, most = (pl.p.n_max + 4 * kTileKeys - 1) / (4 * kTileKeys);
-  return (int)std::min<int64_t>({splits, most, kChunkSplitsMax});
-}
+// Few query vectors per KV head go to the kernel of the decode steps, which reads the keys once for 32 of them.  Whole call, us, this kernel / that
+// one: 28 vectors on 1K tokens 16.1 / 11.4, 16 on 16 x 16K 196 / 177 (e4m3 161 / 112), 32 on 16 x 16K 196 / 191 (e4m3 164 / 126), but 64 205 /
+// 326 (e4m3 185 / 219).
+bool chunk_is_few(const Plan& pl, int n_new) { return n_new * pl.group <= 32; }
 
 }  // namespace
 
 bool chunk_fits(const Plan& pl, int n_new) {
-  return (int64_t)pl.p.batch * pl.p.n_kv_heads * (((int64_t)n_new * pl.group + kTileRows - 1) / kTileRows) <= INT32_MAX / kChunkThreads;
+  return chunk_tiles(pl, n_new) + 2 * chunk_slots(pl) <= INT32_MAX / kChunkThreads;
 }
 
 size_t chunk_workspace_bytes(const Plan& pl, int n_new) {
-  const int splits = chunk_splits(pl, n_new);
-  return splits == 1 ? 0 : (size_t)pl.p.batch * n_new * pl.p.n_q_heads * splits * (pl.p.head_dim + 2) * sizeof(float);
+  if (chunk_is_few(pl, n_new)) return few_workspace_bytes(pl, n_new);
+  return (size_t)chunk_pieces(pl, n_new) * kTileRows * (pl.p.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_chunk(const Plan& pl, const void* q, int64_t q_stride, int n_new, const int32_t* first, const int32_t* new_lens, const void* k,
                         const void* v, const int32_t* block_table, int sink, int window, void* ws, bool bf16, void* out_o, float* out_lse,
                         hipStream_t st) {
+  if (chunk_is_few(pl, n_new))
+    return launch_few(pl, q, q_stride, n_new, first, new_lens, k, v, block_table, sink, window, ws, bf16, out_o, out_lse, st);
   ChunkArgs A = {};
   A.q = static_cast<const uint16_t*>(q);
   A.q_stride = q_stride;
@@ -473,12 +803,13 @@ hipError_t launch_chunk(const Plan& pl, const void* q, int64_t q_stride, int n_n
   A.Hq = pl.p.n_q_heads;
   A.Hkv = pl.p.n_kv_heads;
   A.n_new = n_new;
-  A.splits = chunk_splits(pl, n_new);
+  A.slots = chunk_slots(pl);
+  A.room = chunk_may_cut(pl, n_new, !new_lens) ? (int)(chunk_pieces(pl, n_new) / A.Hkv) : 0;
   A.sink = std::min(sink, pl.p.n_max);
   A.window = std::min(window, pl.p.n_max);
   A.log2_scale = (float)((double)pl.sm_scale * 1.4426950408889634);
   A.part = static_cast<float*>(ws);
-  A.part_ml = reinterpret_cast<float2*>(A.part + (size_t)A.batch * n_new * A.Hq * A.splits * pl.p.head_dim);
+  A.part_ml = reinterpret_cast<float2*>(A.part + (size_t)chunk_pieces(pl, n_new) * kTileRows * pl.p.head_dim);
   return pl.p.head_dim == 128 ? launch_chunk_d<128>(pl, A, bf16, st) : launch_chunk_d<64>(pl, A, bf16, st);
 }
 

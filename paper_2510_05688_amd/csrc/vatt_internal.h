@@ -268,6 +268,11 @@ size_t chunk_workspace_bytes(const Plan& pl, int n_new);
 hipError_t launch_chunk(const Plan& pl, const void* q, int64_t q_stride, int n_new, const int32_t* first, const int32_t* new_lens, const void* k,
                         const void* v, const int32_t* block_table, int sink, int window, void* ws, bool bf16, void* out_o, float* out_lse,
                         hipStream_t st);
+// (its form for few query vectors per KV head: the kernel of the decode steps)
+size_t few_workspace_bytes(const Plan& pl, int n_new);
+hipError_t launch_few(const Plan& pl, const void* q, int64_t q_stride, int n_new, const int32_t* first, const int32_t* new_lens, const void* k,
+                      const void* v, const int32_t* block_table, int sink, int window, void* ws, bool bf16, void* out_o, float* out_lse,
+                      hipStream_t st);
 hipError_t launch_window(const Plan& pl, const void* q, const void* k, const void* v, const int32_t* block_table, const int32_t* seq_lens,
                          int sink, int window, void* ws, float* out_o, float* out_lse, hipStream_t st);
 hipError_t set_kernel_attributes(const Plan& pl);        // every selection kernel: dynamic LDS limit

@@ -30,35 +30,70 @@ hipError_t launch_window_p(const Plan& pl, const AttendArgs& A, hipStream_t st) 
 
 }  // namespace
 
-hipError_t launch_window(const Plan& pl, const void* q, const void* k, const void* v, const int32_t* block_table, const int32_t* seq_lens,
-                         int sink, int window, void* ws, float* out_o, float* out_lse, hipStream_t st) {
-  AttendArgs A = {};
+namespace {
+
+// Workgroups that share out the tokens of a sequence: four per CU in all, none with less than a unit of keys per wave.
+int window_splits(const Plan& pl, int q_len, int64_t longest) {
+  const int vectors = pl.group * q_len, rounds = vectors <= 16 ? 1 : (vectors + 31) / 32;
+  const int64_t jobs = (int64_t)pl.p.batch * pl.p.n_kv_heads * rounds;
+  return (int)std::min<int64_t>({(4 * pl.num_cus + jobs - 1) / jobs, (longest + kUnit * kAttendWaves - 1) / (kUnit * kAttendWaves), kSplitsMax});
+}
+
+hipError_t launch_rows(const Plan& pl, AttendArgs& A, const void* q, const void* k, const void* v, const int32_t* block_table, int sink,
+                       int window, int splits, void* ws, hipStream_t st) {
   A.q = static_cast<const uint16_t*>(q);
   A.k = static_cast<const unsigned char*>(k);
   A.v = static_cast<const unsigned char*>(v);
   A.scale_off = (int64_t)kv_scale_offset(pl);
-  A.seq_lens = seq_lens;
-  A.out_o = out_o;
-  A.out_lse = out_lse;
   A.M = row_map(pl, block_table);
   A.Hq = pl.p.n_q_heads;
   A.Hkv = pl.p.n_kv_heads;
-  A.q_len = pl.q_len;
-  A.q_stride = (int64_t)A.Hq * pl.p.head_dim;
   A.log2_scale = (float)((double)pl.sm_scale * 1.4426950408889634);
   A.sink = std::min(sink, pl.p.n_max);
   A.window = std::min(window, pl.p.n_max);
-  const int vectors = pl.group * pl.q_len;
+  const int vectors = pl.group * A.q_len;
   A.rounds = vectors <= 16 ? 1 : (vectors + 31) / 32;
-  // Four workgroups per CU in all, none with less than a unit of keys per wave; the partial sums fit the workspace.
-  const int64_t rows = (int64_t)pl.vbatch * A.Hq, jobs = (int64_t)pl.p.batch * A.Hkv * A.rounds;
-  const int64_t longest = std::min<int64_t>(pl.p.n_max, (int64_t)A.sink + A.window + pl.q_len + 14);  // (whole groups of 8 at both ends)
-  int64_t splits = std::min<int64_t>((4 * pl.num_cus + jobs - 1) / jobs, (longest + kUnit * kAttendWaves - 1) / (kUnit * kAttendWaves));
-  splits = std::min<int64_t>({splits, kSplitsMax, (int64_t)(pl.ws_bytes / (rows * (pl.p.head_dim + 2) * sizeof(float)))});
-  A.splits = (int)std::max<int64_t>(splits, 1);
+  A.splits = splits;
   A.part = static_cast<float*>(ws);
-  A.part_ml = reinterpret_cast<float2*>(A.part + rows * A.splits * pl.p.head_dim);
+  A.part_ml = reinterpret_cast<float2*>(A.part + (int64_t)pl.p.batch * A.q_len * A.Hq * A.splits * pl.p.head_dim);
   return pl.p.head_dim == 128 ? launch_window_p<128>(pl, A, st) : launch_window_p<64>(pl, A, st);
+}
+
+}  // namespace
+
+hipError_t launch_window(const Plan& pl, const void* q, const void* k, const void* v, const int32_t* block_table, const int32_t* seq_lens,
+                         int sink, int window, void* ws, float* out_o, float* out_lse, hipStream_t st) {
+  AttendArgs A = {};
+  A.seq_lens = seq_lens;
+  A.q_len = pl.q_len;
+  A.q_stride = (int64_t)pl.p.n_q_heads * pl.p.head_dim;
+  A.out_o = out_o;
+  A.out_lse = out_lse;
+  // (whole groups of 8 at both ends of the window; the partial sums fit the workspace)
+  const int64_t longest = std::min<int64_t>(pl.p.n_max, (int64_t)std::min(sink, pl.p.n_max) + std::min(window, pl.p.n_max) + pl.q_len + 14);
+  const int64_t fit = pl.ws_bytes / ((int64_t)pl.vbatch * pl.p.n_q_heads * (pl.p.head_dim + 2) * sizeof(float));
+  const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(window_splits(pl, pl.q_len, longest), fit));
+  return launch_rows(pl, A, q, k, v, block_table, sink, window, splits, ws, st);
+}
+
+size_t few_workspace_bytes(const Plan& pl, int n_new) {
+  return (size_t)pl.p.batch * n_new * pl.p.n_q_heads * window_splits(pl, n_new, pl.p.n_max) * (pl.p.head_dim + 2) * sizeof(float);
+}
+
+hipError_t launch_few(const Plan& pl, const void* q, int64_t q_stride, int n_new, const int32_t* first, const int32_t* new_lens, const void* k,
+                      const void* v, const int32_t* block_table, int sink, int window, void* ws, bool bf16, void* out_o, float* out_lse,
+                      hipStream_t st) {
+  AttendArgs A = {};
+  A.first = first;
+  A.new_lens = new_lens;
+  A.q_len = n_new;
+  A.q_stride = q_stride;
+  A.out_o = static_cast<float*>(out_o);
+  A.out_lse = out_lse;
+  A.out_bf16 = bf16;
+  const int64_t seen = window > 0 ? (int64_t)std::min(sink, pl.p.n_max) + std::min(window, pl.p.n_max) + n_new + 14 : pl.p.n_max;
+  const int splits = window_splits(pl, n_new, std::min<int64_t>(pl.p.n_max, seen));
+  return launch_rows(pl, A, q, k, v, block_table, window > 0 ? sink : 0, window > 0 ? window : pl.p.n_max, splits, ws, st);
 }
 
 }  // namespace vatt
