@@ -16,7 +16,6 @@ __device__ __forceinline__ uint32_t lower_halves(uint32_t a, uint32_t b) { retur
 
 constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / kWave;
 constexpr int kUnit = 32;          // keys that a wave takes at a time
-constexpr int kChunk = 16;         // groups of 8 tokens that a workgroup takes at a time: a unit for each wave
 constexpr int kSlots = 1024;       // groups of 8 tokens that a workgroup looks up at a time
 constexpr int kSplitsMax = 128;
 constexpr int kNowhere = 0x7fffff00;  // token of a group that does not exist: beyond every sequence
@@ -122,6 +121,81 @@ __device__ __forceinline__ uint32_t row_scales(const unsigned char* p) {
   else return *reinterpret_cast<const uint16_t*>(p);
 }
 
+// The tokens of one list again for one head, by the whole workgroup: dot products, every row only where it is seen.
+template <int D, int FMT, bool PAGED, int KIND, int WAVES>
+__device__ __forceinline__ void attend_again(const AttendArgs& A, const uint16_t* q, int seq, int kvh, const TokenList& L, float (&s_acc)[WAVES][D],
+                                             float (&s_m)[WAVES], float (&s_l)[WAVES]) {
+  constexpr int LPR = D / 8, RPW = kWave / LPR;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane % LPR, rsub = lane / LPR;
+  const uint4 qv = *reinterpret_cast<const uint4*>(q + sub * 8);
+  const uint32_t qw[4] = {qv.x, qv.y, qv.z, qv.w};
+  float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int64_t i = wave * RPW + rsub; i < (int64_t)L.count * 8; i += WAVES * RPW) {
+    const int group = (int)(i >> 3), tok = token_of<KIND>(L, group, entry_of<KIND>(L, group)) + (int)(i & 7);
+    if (tok >= L.n || (KIND == kFirstAndWindow && !L.seen(tok))) continue;
+    const RowAt at = row_at<PAGED>(A.M, seq, kvh, tok, row_block<PAGED>(A.M, seq, tok));
+    uint4 x[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const unsigned char* buf = y ? A.v : A.k;
+      uint32_t byte = 0;
+      if constexpr (FMT != VATT_KV_BF16) byte = buf[A.scale_off + at.scales * (D / 32) + sub / 4];
+      x[y] = chunk_bf16<FMT>(load_chunk<FMT>(buf + at.row * kRowBytes<FMT, D> + sub * (kRowBytes<FMT, D> / LPR)), byte);
+    }
+    const uint32_t kw[4] = {x[0].x, x[0].y, x[0].z, x[0].w}, vw[4] = {x[1].x, x[1].y, x[1].z, x[1].w};
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s += bf16_lo(kw[j]) * bf16_lo(qw[j]) + bf16_hi(kw[j]) * bf16_hi(qw[j]);
+    s = group_sum<LPR>(s) * A.log2_scale;
+    const float mnew = fmaxf(m, s), shift = mnew == -INFINITY ? -3.0e38f : mnew;
+    const float alpha = m == -INFINITY ? 0.f : m == shift ? 1.f : __builtin_amdgcn_exp2f(m - shift);
+    const float p = __builtin_amdgcn_exp2f(s - shift);
+    m = shift;
+    l = l * alpha + p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      acc[2 * j] = acc[2 * j] * alpha + p * bf16_lo(vw[j]);
+      acc[2 * j + 1] = acc[2 * j + 1] * alpha + p * bf16_hi(vw[j]);
+    }
+  }
+  float all = m;
+#pragma unroll
+  for (int o = LPR; o < kWave; o <<= 1) all = fmaxf(all, __shfl_xor(all, o));
+  const float f = m == -INFINITY ? 0.f : m == all ? 1.f : __builtin_amdgcn_exp2f(m - all);
+  l *= f;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) acc[c] *= f;
+#pragma unroll
+  for (int o = LPR; o < kWave; o <<= 1) {
+    l += __shfl_xor(l, o);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[c] += __shfl_xor(acc[c], o);
+  }
+  __syncthreads();
+  if (rsub == 0) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) s_acc[wave][sub * 8 + c] = acc[c];
+  }
+  if (lane == 0) {
+    s_m[wave] = all;
+    s_l[wave] = l;
+  }
+  __syncthreads();
+}
+
+// N consecutive values of the output, from value `at` on, in the call's type.
+template <int N>
+__device__ __forceinline__ void store_row(const AttendArgs& A, int64_t at, const float (&x)[N]) {
+  if (A.out_bf16) {
+    uint16_t* out = reinterpret_cast<uint16_t*>(A.out_o) + at;
+    if constexpr (N == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+    else out[0] = (uint16_t)pack_bf16(x[0], x[0]);
+  } else {
+    if constexpr (N == 4) *reinterpret_cast<float4*>(A.out_o + at) = make_float4(x[0], x[1], x[2], x[3]);
+    else A.out_o[at] = x[0];
+  }
+}
+
 // Attention with the query vectors of a KV head on the matrix cores, 32 keys of a wave at a time:
 //   S [keys x vectors] = K Q^T   and   O^T [d x vectors] += V^T P^T,   P = exp(S - m),
 // both v_mfma_f32_16x16x32_bf16 (operand lane l: row or column l % 16, eight inner elements; result lane l: column l % 16, rows
@@ -138,8 +212,13 @@ __device__ __forceinline__ uint32_t row_scales(const unsigned char* p) {
 // same loads without the products and exponentials take 164; lists of 12 x 4K - 64K tokens with two queries each (98 MB in pieces of 2 KB, with scales of 64
 // bytes apart from them) 28 us, loads alone 22.  Half or twice as many workgroups, three of them on a CU instead of two, and a least
 // number of chunks for each made no difference or were slower.
-template <int D, int FMT, bool PAGED, int KIND, int NQT, int PACK>
-__global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A) {
+// WHOLE (kFirstAndWindow): one workgroup, of WAVES waves, has all tokens of a sequence and KV head, and writes the results.
+template <int D, int FMT, bool PAGED, int KIND, int NQT, int PACK, int WAVES = kAttendWaves, bool WHOLE = false>
+__global__ __launch_bounds__(WAVES * kWave, 2) void attend_kernel(AttendArgs A) {
+  constexpr int kThreads = WAVES * kWave;
+  constexpr int kChunk = 4 * WAVES;  // groups of 8 tokens that a workgroup takes at a time: a unit for each wave
+  static_assert(WAVES == 4 || WAVES == 8, "see the end");
+  static_assert(!WHOLE || KIND == kFirstAndWindow, "the others have a merge");
   constexpr bool LIST = KIND == kListedBlocks, RANGE = KIND == kFirstAndWindow;
   constexpr int S = D / 32;  // steps over a row of K
   constexpr int E = D / 16;  // values of a V row per lane = tiles over the head dimension
@@ -168,8 +247,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
 
   __shared__ __align__(16) int s_tok[kSlots];
   __shared__ __align__(16) int s_at[kSlots];
-  __shared__ float4 s_o[kAttendWaves][4][E / 4][kWave];
-  __shared__ float s_m[kAttendWaves][16], s_l[kAttendWaves][16];
+  __shared__ float4 s_o[4][4][E / 4][kWave];
+  __shared__ float s_m[4][16], s_l[4][16];
   // (with two tiles of vectors the queries stay in LDS: there are no registers for them)
   constexpr bool kQueriesInLds = NQT > 1;
   __shared__ uint4 s_q[kQueriesInLds ? NQT * S : 1][kWave];
@@ -296,7 +375,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
   for (int c0 = 0; c0 < mine; c0 += kSlots / kChunk) {
     const int c_n = min(kSlots / kChunk, mine - c0);
     if (c0 > 0) __syncthreads();
-    for (int i = tid; i < c_n * kChunk; i += kAttendThreads) {
+    for (int i = tid; i < c_n * kChunk; i += kThreads) {
       const int group = group_of(c0 * kChunk + i);
       const int tok = token_of<KIND>(L, group, c0 == 0 && i == tid ? entry0 : entry_of<KIND>(L, group)), safe = tok == kNowhere ? 0 : tok;
       s_tok[i] = tok;
@@ -456,7 +535,9 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
     }
   }
 
-  // The waves' sums together, one 16-vector tile at a time, in the result layout: wave w finishes rows 4 g + w.
+  // The waves' sums together, one 16-vector tile at a time, in the result layout (of eight waves the upper four's go to the lower four first):
+  // wave w finishes rows 4 g + w.
+  uint32_t odd = 0;  // WHOLE: vectors of the tile with an Inf or a NaN
 #pragma unroll
   for (int nt = 0; nt < NQT; ++nt) {
     float l = lrun[nt];
@@ -466,37 +547,64 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
     saw |= __shfl_xor(saw, 16);
     saw |= __shfl_xor(saw, 32);
     // (a piece all of whose scores are -Inf is no piece without a token)
-    const float m_own = saw && mrun[nt] == -INFINITY ? -3.0e38f : mrun[nt];
+    float m_own = saw && mrun[nt] == -INFINITY ? -3.0e38f : mrun[nt];
+    auto factor = [](float of, float m) { return of == -INFINITY ? 0.f : of == m ? 1.f : __builtin_amdgcn_exp2f(of - m); };
     __syncthreads();
+    auto put = [&](int w) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+      for (int r = 0; r < 4; ++r) {
 #pragma unroll
-      for (int e = 0; e < E; e += 4)
-        s_o[wave][r][e / 4][lane] = make_float4(acc[nt][e][r], acc[nt][e + 1][r], acc[nt][e + 2][r], acc[nt][e + 3][r]);
+        for (int e = 0; e < E; e += 4)
+          s_o[w][r][e / 4][lane] = make_float4(acc[nt][e][r], acc[nt][e + 1][r], acc[nt][e + 2][r], acc[nt][e + 3][r]);
+      }
+      if (g4 == 0) {
+        s_m[w][i16] = m_own;
+        s_l[w][i16] = l;
+      }
+    };
+    if constexpr (WAVES == 8) {
+      if (wave >= 4) put(wave - 4);
+      __syncthreads();
+      if (wave < 4) {
+        const float m_other = s_m[wave][i16], m = fmaxf(m_own, m_other), f0 = factor(m_own, m), f1 = factor(m_other, m);
+        l = l * f0 + s_l[wave][i16] * f1;
+        m_own = m;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+#pragma unroll
+          for (int e = 0; e < E; e += 4) {
+            const float4 y = s_o[wave][r][e / 4][lane];
+            acc[nt][e][r] = acc[nt][e][r] * f0 + y.x * f1;
+            acc[nt][e + 1][r] = acc[nt][e + 1][r] * f0 + y.y * f1;
+            acc[nt][e + 2][r] = acc[nt][e + 2][r] * f0 + y.z * f1;
+            acc[nt][e + 3][r] = acc[nt][e + 3][r] * f0 + y.w * f1;
+          }
+        }
+      }
+      __syncthreads();
     }
-    if (g4 == 0) {
-      s_m[wave][i16] = m_own;
-      s_l[wave][i16] = l;
-    }
+    if (WAVES == 4 || wave < 4) put(wave);
     __syncthreads();
-    float m = -INFINITY, fac[kAttendWaves];
+    float m = -INFINITY, fac[4];
     l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kAttendWaves; ++w) m = fmaxf(m, s_m[w][i16]);
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, s_m[w][i16]);
 #pragma unroll
-    for (int w = 0; w < kAttendWaves; ++w) {
-      fac[w] = s_m[w][i16] == -INFINITY ? 0.f : s_m[w][i16] == m ? 1.f : __builtin_amdgcn_exp2f(s_m[w][i16] - m);
+    for (int w = 0; w < 4; ++w) {
+      fac[w] = factor(s_m[w][i16], m);
       l += s_l[w][i16] * fac[w];
     }
     const int c = c_base + nt * 16 + i16;
-    if (c < vectors) {
+    bool bad = false;
+    if (c < vectors && (WAVES == 4 || wave < 4)) {
       const int t = t0 + c / G, g = c % G;
-      const int64_t place = (((int64_t)seq * Q + t) * A.Hq + (int64_t)kvh * G + g) * A.splits + split;
+      const int64_t row = ((int64_t)seq * Q + t) * A.Hq + (int64_t)kvh * G + g;
+      const int64_t place = row * A.splits + split;
 #pragma unroll
       for (int e = 0; e < E; e += 4) {
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) {
+        for (int w = 0; w < 4; ++w) {
 #pragma unroll
           for (int x = 0; x < PACK; ++x) {  // (the columns of a vector's terms)
             const float4 y = s_o[w][wave][e / 4][lane + x * vectors];
@@ -506,73 +614,54 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
             o.w += y.w * fac[w];
           }
         }
-        *reinterpret_cast<float4*>(A.part + place * D + E * (4 * g4 + wave) + e) = o;
+        if constexpr (WHOLE) {
+          bad |= !(fabsf(o.x) + fabsf(o.y) + fabsf(o.z) + fabsf(o.w) < INFINITY);
+          store_row<4>(A, row * D + E * (4 * g4 + wave) + e, {o.x / l, o.y / l, o.z / l, o.w / l});
+        } else {
+          *reinterpret_cast<float4*>(A.part + place * D + E * (4 * g4 + wave) + e) = o;
+        }
       }
-      if (wave == 0 && g4 == 0) A.part_ml[place] = make_float2(m, l);
+      if (wave == 0 && g4 == 0) {
+        if constexpr (!WHOLE) A.part_ml[place] = make_float2(m, l);
+        else if (A.out_lse) A.out_lse[row] = m * 0.69314718055994530942f + logf(l);
+      }
+      bad |= !(l < INFINITY);
+    }
+    if constexpr (WHOLE) {
+      const uint64_t there = __ballot(bad);
+      odd |= (uint32_t)((there | there >> 16 | there >> 32 | there >> 48) & 0xffff) << (16 * nt);
     }
   }
-}
-
-// The tokens of one list again for one head, by the whole workgroup: dot products, every row only where it is seen.
-template <int D, int FMT, bool PAGED, int KIND>
-__device__ __forceinline__ void attend_again(const AttendArgs& A, const uint16_t* q, int seq, int kvh, const TokenList& L, float (&s_acc)[kAttendWaves][D],
-                                             float (&s_m)[kAttendWaves], float (&s_l)[kAttendWaves]) {
-  constexpr int LPR = D / 8, RPW = kWave / LPR;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane % LPR, rsub = lane / LPR;
-  const uint4 qv = *reinterpret_cast<const uint4*>(q + sub * 8);
-  const uint32_t qw[4] = {qv.x, qv.y, qv.z, qv.w};
-  float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int64_t i = wave * RPW + rsub; i < (int64_t)L.count * 8; i += kAttendWaves * RPW) {
-    const int group = (int)(i >> 3), tok = token_of<KIND>(L, group, entry_of<KIND>(L, group)) + (int)(i & 7);
-    if (tok >= L.n || (KIND == kFirstAndWindow && !L.seen(tok))) continue;
-    const RowAt at = row_at<PAGED>(A.M, seq, kvh, tok, row_block<PAGED>(A.M, seq, tok));
-    uint4 x[2];
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      const unsigned char* buf = y ? A.v : A.k;
-      uint32_t byte = 0;
-      if constexpr (FMT != VATT_KV_BF16) byte = buf[A.scale_off + at.scales * (D / 32) + sub / 4];
-      x[y] = chunk_bf16<FMT>(load_chunk<FMT>(buf + at.row * kRowBytes<FMT, D> + sub * (kRowBytes<FMT, D> / LPR)), byte);
-    }
-    const uint32_t kw[4] = {x[0].x, x[0].y, x[0].z, x[0].w}, vw[4] = {x[1].x, x[1].y, x[1].z, x[1].w};
-    float s = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) s += bf16_lo(kw[j]) * bf16_lo(qw[j]) + bf16_hi(kw[j]) * bf16_hi(qw[j]);
-    s = group_sum<LPR>(s) * A.log2_scale;
-    const float mnew = fmaxf(m, s), shift = mnew == -INFINITY ? -3.0e38f : mnew;
-    const float alpha = m == -INFINITY ? 0.f : m == shift ? 1.f : __builtin_amdgcn_exp2f(m - shift);
-    const float p = __builtin_amdgcn_exp2f(s - shift);
-    m = shift;
-    l = l * alpha + p;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      acc[2 * j] = acc[2 * j] * alpha + p * bf16_lo(vw[j]);
-      acc[2 * j + 1] = acc[2 * j + 1] * alpha + p * bf16_hi(vw[j]);
+  if constexpr (WHOLE) {
+    // (see attend_merge_kernel)
+    __syncthreads();
+    if (lane == 0) s_tok[wave] = (int)odd;
+    __syncthreads();
+    odd = (uint32_t)(s_tok[0] | s_tok[1] | s_tok[2] | s_tok[3]);
+    __syncthreads();
+    float(&s_acc)[WAVES][D] = *reinterpret_cast<float(*)[WAVES][D]>(&s_o[0][0][0][0]);
+    float(&s_m2)[WAVES] = *reinterpret_cast<float(*)[WAVES]>(&s_m[0][0]);
+    float(&s_l2)[WAVES] = *reinterpret_cast<float(*)[WAVES]>(&s_l[0][0]);
+    while (odd) {
+      const int c = c_base + __builtin_ctz(odd), t = c / G, h = kvh * G + c % G;
+      odd &= odd - 1;
+      const int n_t = max(T.first + t + 1, 1);
+      attend_again<D, FMT, PAGED, KIND, WAVES>(A, A.q + ((int64_t)seq * Q + t) * A.q_stride + (int64_t)h * D, seq, kvh,
+                                               token_list<KIND>(A, 0, kvh, n_t, max(n_t - A.window, 0)), s_acc, s_m2, s_l2);
+      float m = s_m2[0], l = 0.f, a = 0.f;
+      for (int w = 1; w < WAVES; ++w) m = fmaxf(m, s_m2[w]);
+      for (int w = 0; w < WAVES; ++w) {
+        if (s_m2[w] == -INFINITY) continue;
+        const float f = s_m2[w] == m ? 1.f : __builtin_amdgcn_exp2f(s_m2[w] - m);
+        l += s_l2[w] * f;
+        if (tid < D) a += s_acc[w][tid] * f;
+      }
+      const int64_t row = ((int64_t)seq * Q + t) * A.Hq + h;
+      if (tid < D) store_row<1>(A, row * D + tid, {a / l});
+      if (tid == 0 && A.out_lse) A.out_lse[row] = m * 0.69314718055994530942f + logf(l);
+      __syncthreads();
     }
   }
-  float all = m;
-#pragma unroll
-  for (int o = LPR; o < kWave; o <<= 1) all = fmaxf(all, __shfl_xor(all, o));
-  const float f = m == -INFINITY ? 0.f : m == all ? 1.f : __builtin_amdgcn_exp2f(m - all);
-  l *= f;
-#pragma unroll
-  for (int c = 0; c < 8; ++c) acc[c] *= f;
-#pragma unroll
-  for (int o = LPR; o < kWave; o <<= 1) {
-    l += __shfl_xor(l, o);
-#pragma unroll
-    for (int c = 0; c < 8; ++c) acc[c] += __shfl_xor(acc[c], o);
-  }
-  __syncthreads();
-  if (rsub == 0) {
-#pragma unroll
-    for (int c = 0; c < 8; ++c) s_acc[wave][sub * 8 + c] = acc[c];
-  }
-  if (lane == 0) {
-    s_m[wave] = all;
-    s_l[wave] = l;
-  }
-  __syncthreads();
 }
 
 // Merge of a head's partial sums: bound by two dependent loads.  Every wave looks at all (max, sum) pairs, one or two per lane; the threads of
@@ -641,7 +730,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_merge_kernel(AttendArgs
     } else {
       n = max(min(max(A.seq_lens[seq], 1), A.M.n_max) - (A.q_len - 1 - t), 1);
     }
-    attend_again<D, FMT, PAGED, KIND>(A, q, seq, kvh, token_list<KIND>(A, (int)vb, kvh, n, lo), s_acc, s_m, s_l);
+    attend_again<D, FMT, PAGED, KIND, kAttendWaves>(A, q, seq, kvh, token_list<KIND>(A, (int)vb, kvh, n, lo), s_acc, s_m, s_l);
     m = s_m[0];
     for (int w = 1; w < kAttendWaves; ++w) m = fmaxf(m, s_m[w]);
     l = a = 0.f;
@@ -654,7 +743,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_merge_kernel(AttendArgs
   }
   if (tid < D) {
     const float o = m == -INFINITY ? 0.f : a / l;
-    if (KIND == kFirstAndWindow && A.out_bf16) reinterpret_cast<uint16_t*>(A.out_o)[head * D + c] = (uint16_t)pack_bf16(o, o);
+    if constexpr (KIND == kFirstAndWindow) store_row<1>(A, head * D + c, {o});
     else A.out_o[head * D + c] = o;
     if (tid == 0 && A.out_lse) A.out_lse[head] = m == -INFINITY ? -INFINITY : m * 0.69314718055994530942f + logf(l);
   }

@@ -13,7 +13,8 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kChunkThreads = 256, kChunkWaves = kChunkThreads / kWave;
 constexpr int kWaveRows = 32;                         // rows (query vectors) of a wave
-constexpr int kTileRows = kWaveRows * kChunkWaves;    // ... of a workgroup
+constexpr int kTileShift = 7, kTileRows = 1 << kTileShift;  // ... of a workgroup
+static_assert(kTileRows == kWaveRows * kChunkWaves, "32 rows of every wave");
 constexpr int kTileKeys = 64;
 constexpr int kPiecesMax = 64;      // pieces that a tile's keys are cut into at most
 constexpr int kPieceLeast = 4;      // key tiles of a piece at least
@@ -33,7 +34,7 @@ struct ChunkArgs {
   float* out_lse;
   RowMap M;
   int batch, Hq, Hkv, n_new, sink, window;
-  int slots;  // workgroups that run at a time
+  int slots;  // workgroups that run at a time, two to a compute unit
   int room;   // pieces of one KV head that the workspace holds
   float log2_scale;  // softmax scale / ln 2
 };
@@ -66,6 +67,8 @@ __device__ __forceinline__ KeyTiles key_tiles(const ChunkArgs& A, int p_lo, int 
 }
 
 __device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane((int)wave_inclusive_scan_u32((uint32_t)v), kWave - 1); }
+
+__device__ __forceinline__ uint64_t ones(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }  // the lowest n bits
 
 // What a workgroup does: a tile of rows of one sequence and KV head, over one of `pieces` parts of its keys.
 struct Work {
@@ -123,7 +126,7 @@ struct Batch {
         const NewTokens n = new_tokens(A, b);
         const SeqTiles t(A, g_shift, n);
         tiles[i] = t.tiles;
-        level[i] = n.first / (kTileRows >> g_shift);
+        level[i] = n.first >> (kTileShift - g_shift);
         last[i] = t.last;
         total += 0.5f * (float)(t.tiles * (t.first + t.last));
         most += (float)(t.tiles * t.last);
@@ -219,14 +222,12 @@ __device__ __forceinline__ int k_place(int row, int c) { return row * (2 * D) + 
 template <int D>
 __device__ __forceinline__ int v_place(int row, int c) { return row * (2 * D) + (v_chunk<D>(row, c) << 4); }
 
-// 16 bytes per lane from global memory into LDS, the lanes' one behind the other from a uniform place on.
-__device__ __forceinline__ void load_lds_16(const unsigned char* src, unsigned char* dst) {
-  typedef const __attribute__((address_space(1))) uint32_t* Global;
-  typedef __attribute__((address_space(3))) uint32_t* Lds;
-  __builtin_amdgcn_global_load_lds((Global)src, (Lds)dst, 16, 0, 0);
+__device__ __forceinline__ void load_lds_16(const unsigned char* base, uint32_t off, unsigned char* dst) {
+  typedef __attribute__((address_space(3))) unsigned char* Lds;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"((uint32_t)(uintptr_t)(Lds)dst), "v"(off), "s"(base) : "memory");
 }
 // Until this wave's loads into LDS are there (a barrier waits for the other waves').
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }  // vmcnt(0)
 
 template <bool BF16>
 __device__ __forceinline__ void store_4(void* out, int64_t at, float a, float b, float c, float d) {
@@ -341,8 +342,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   constexpr float kLazy = 8.0f;
   constexpr bool BF16 = TERMS == 1;
   constexpr int CARRY = BF16 ? 1 : 2;
-  // (objects of their own: what is on its way into one need not be awaited before another is read)
-  __shared__ __align__(256) unsigned char s_k0[TILE], s_k1[TILE], s_v0[TILE], s_v1[TILE];
+  __shared__ __align__(256) unsigned char s_kv[4 * TILE];  // K, K, V, V
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
   const int g_shift = 31 - __builtin_clz(A.Hq / A.Hkv), G = 1 << g_shift;
@@ -396,14 +396,8 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   };
   constexpr std::integral_constant<int, 0> K = {};
   constexpr std::integral_constant<int, 1> V = {};
-  auto buffer = [&](auto kv, auto parity) __attribute__((always_inline)) {
-    constexpr int I = 2 * decltype(kv)::value + decltype(parity)::value;
-    if constexpr (I == 0) return &s_k0[0];
-    else if constexpr (I == 1) return &s_k1[0];
-    else if constexpr (I == 2) return &s_v0[0];
-    else return &s_v1[0];
-  };
-  auto load = [&](auto which, const Rows& R, auto parity) __attribute__((always_inline)) {
+  auto buffer = [&](auto kv, int parity) __attribute__((always_inline)) { return &s_kv[(2 * decltype(kv)::value + parity) * TILE]; };
+  auto load = [&](auto which, const Rows& R, int parity) __attribute__((always_inline)) {
     constexpr int KV = decltype(which)::value;
     const unsigned char* src = KV ? A.v : A.k;
     if constexpr (!QUANT) {
@@ -415,7 +409,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
           const int r = x * RPI + lane / LPR, row = 8 * g + r, pos = lane % LPR;
           const int c = KV ? v_chunk<D>(row, pos) : k_chunk<D>(row, pos);
           const uint32_t off = (uint32_t)(min(r, R.left[g]) * ROW + c * 16);
-          load_lds_16(base + off, buffer(which, parity) + (16 * wave + 8 * g + x * RPI) * 2 * D);
+          load_lds_16(base, off, buffer(which, parity) + (16 * wave + 8 * g + x * RPI) * 2 * D);
         }
       }
     } else {
@@ -435,7 +429,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
       }
     }
   };
-  auto store = [&](auto which, auto parity) __attribute__((always_inline)) {
+  auto store = [&](auto which, int parity) __attribute__((always_inline)) {
     constexpr int KV = decltype(which)::value;
     if constexpr (QUANT) {
 #pragma unroll
@@ -461,7 +455,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   float mrun = -INFINITY, lrun = 0.f;
   bool any = false;
 
-  auto first_product = [&](auto parity) __attribute__((always_inline)) {
+  auto first_product = [&](int parity) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < S; ++s) {
 #pragma unroll
@@ -479,15 +473,18 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   auto maximum = [&](int k0, float& alpha) __attribute__((always_inline)) {
     const bool edge = k0 + kTileKeys - 1 > wp_lo || (A.window > 0 && k0 <= wp_hi - A.window && k0 + kTileKeys > A.sink);
     if (edge) {
+      // the tile's keys that the lane's row sees, a bit each; the lane's keys of a 32-bit half are 4 half + constants
+      const uint64_t seen = ones(p - k0 + 1) & ~(ones(low - k0 + 1) & ~ones(A.sink - k0));
+      any |= seen != 0;
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
+      for (int y = 0; y < 2; ++y) {
+        const uint32_t bits = (uint32_t)(seen >> (32 * y)) >> (4 * half);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const int tok = k0 + y * 32 + 8 * (j / 4) + 4 * half + j % 4;
-          const bool ok = tok <= p && (tok > low || tok < A.sink);
-          sc[y][j] = ok ? sc[y][j] : -INFINITY;
-          any |= ok;
+          const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 8 * (j / 4) + j % 4, 1);
+          sc[y][j] = __uint_as_float((__float_as_uint(sc[y][j]) & keep) | (0xff800000u & ~keep));  // (-Inf)
         }
+      }
     } else {
       any = true;
     }
@@ -521,7 +518,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
         pb[u][h] = make_uint4(__float_as_uint(y[4 * h]), __float_as_uint(y[4 * h + 1]), __float_as_uint(y[4 * h + 2]), __float_as_uint(y[4 * h + 3]));
     }
   };
-  auto second_product = [&](int u, auto parity) __attribute__((always_inline)) {
+  auto second_product = [&](int u, int parity) __attribute__((always_inline)) {
     typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
     const int l16 = lane & 15, c_half = (lane >> 4) & 1;
     uint4 term[TERMS];
@@ -558,15 +555,18 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   if (i0 < i1) {
     int blk[2] = {block_of(i0, 0), block_of(i0, 1)};
     Rows now = rows_of(i0, blk);
-    load(K, now, K);
+    load(K, now, 0);
     blk[0] = block_of(i0 + 1, 0);
     blk[1] = block_of(i0 + 1, 1);
-    store(K, K);
+    store(K, 0);
     wait_loads();
+#pragma unroll
+    for (int s = 0; s < S; ++s) asm volatile("" : "+v"(bq[s].x), "+v"(bq[s].y), "+v"(bq[s].z), "+v"(bq[s].w));
     __syncthreads();
-    auto step = [&](int i, auto parity, auto begin) __attribute__((always_inline)) {
-      constexpr std::integral_constant<int, decltype(parity)::value ^ 1> other = {};
+    int parity = 0;
+    auto step = [&](int i, auto begin) __attribute__((always_inline)) {
       constexpr bool FIRST = decltype(begin)::value == 1;
+      const int other = parity ^ 1;
       load(V, now, parity);
       if (i + 1 < i1) {
         now = rows_of(i + 1, blk);
@@ -576,6 +576,13 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
       blk[1] = block_of(i + 2, 1);
       if (active) {
         first_product(parity);
+        // (six reads of K ahead of the products)
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int x = 0; x < S; ++x) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
         float alpha;
         const bool moved = maximum(T.at(i) * kTileKeys, alpha);
         const float m = mrun == -INFINITY ? 0.f : mrun;  // (so far every score is -Inf: weights 0)
@@ -598,18 +605,13 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
       if (i + 1 < i1) store(K, other);
       wait_loads();
       __syncthreads();
+      parity = other;
     };
-    step(i0, K, V);
-    for (int i = i0 + 1; i < i1; i += 2) {
-      step(i, V, K);
-      if (i + 1 < i1) step(i + 1, K, K);
-    }
+    step(i0, V);
+    for (int i = i0 + 1; i < i1; ++i) step(i, K);
     if (active) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if ((i1 - i0) & 1) second_product(u, K);
-        else second_product(u, V);
-      }
+      for (int u = 0; u < 4; ++u) second_product(u, parity ^ 1);
     }
   }
   if (!active) return;
@@ -732,15 +734,18 @@ int64_t chunk_tiles(const Plan& pl, int n_new) {
   return (int64_t)pl.p.batch * pl.p.n_kv_heads * (((int64_t)n_new * pl.group + kTileRows - 1) / kTileRows);
 }
 int chunk_slots(const Plan& pl) { return 2 * pl.num_cus; }
-// Whether pieces can be wanted at all: one sequence whose new tokens all count is as long as the capacity at most.
-bool chunk_may_cut(const Plan& pl, int n_new, bool all_count) {
-  const int64_t longest = (pl.p.n_max + kTileKeys - 1) / kTileKeys;
-  if (pl.p.batch > 1 || !all_count) return longest > 12;
-  return longest > 12 && chunk_tiles(pl, n_new) < chunk_slots(pl);
+// Whether pieces can be wanted at all (the rule of Cut).  Of a batch, or where fewer new tokens may count, the host knows too little.
+bool chunk_may_cut(const Plan& pl, int n_new) {
+  const double longest = (pl.p.n_max + kTileKeys - 1) / kTileKeys, own = (double)n_new / kTileKeys;
+  if (pl.p.batch > kSeqsMax || longest <= 12) return false;
+  if (pl.p.batch > 1) return true;
+  // one sequence: its new tokens at the end of the capacity, or at its beginning (the rule is linear in between)
+  const double tiles = (double)chunk_tiles(pl, n_new) / chunk_slots(pl);
+  return longest > 1.25 * tiles * (longest - own / 2) + 12 || own > 1.25 * tiles * own / 2 + 12;
 }
 int64_t chunk_pieces(const Plan& pl, int n_new) {
+  if (!chunk_may_cut(pl, n_new)) return 0;
   const int64_t longest = (pl.p.n_max + kTileKeys - 1) / kTileKeys, each = std::min<int64_t>((longest + kPieceLeast - 1) / kPieceLeast, kPiecesMax);
-  if (pl.p.batch > kSeqsMax || longest <= 12) return 0;
   return std::min<int64_t>(2 * chunk_slots(pl), chunk_tiles(pl, n_new) * each);
 }
 
@@ -804,7 +809,7 @@ hipError_t launch_chunk(const Plan& pl, const void* q, int64_t q_stride, int n_n
   A.Hkv = pl.p.n_kv_heads;
   A.n_new = n_new;
   A.slots = chunk_slots(pl);
-  A.room = chunk_may_cut(pl, n_new, !new_lens) ? (int)(chunk_pieces(pl, n_new) / A.Hkv) : 0;
+  A.room = (int)(chunk_pieces(pl, n_new) / A.Hkv);
   A.sink = std::min(sink, pl.p.n_max);
   A.window = std::min(window, pl.p.n_max);
   A.log2_scale = (float)((double)pl.sm_scale * 1.4426950408889634);

@@ -8,6 +8,14 @@ template <int D, int FMT, bool PAGED>
 hipError_t launch_window_f(const AttendArgs& A, int batch, hipStream_t st) {
   const dim3 grid(A.Hkv, A.splits * A.rounds, batch), threads(kAttendThreads);
   const int vectors = A.Hq / A.Hkv * A.q_len;
+  if (A.splits == 1) {
+    const dim3 eight(8 * kWave);
+    if (vectors <= 5) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 3, 8, true>), grid, eight, 0, st, A);
+    else if (vectors <= 8) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 2, 8, true>), grid, eight, 0, st, A);
+    else if (vectors <= 16) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 1, 8, true>), grid, eight, 0, st, A);
+    else hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 2, 1, 8, true>), grid, eight, 0, st, A);
+    return hipGetLastError();
+  }
   if (vectors <= 5) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 3>), grid, threads, 0, st, A);
   else if (vectors <= 8) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 2>), grid, threads, 0, st, A);
   else if (vectors <= 16) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 1>), grid, threads, 0, st, A);
@@ -32,11 +40,15 @@ hipError_t launch_window_p(const Plan& pl, const AttendArgs& A, hipStream_t st) 
 
 namespace {
 
-// Workgroups that share out the tokens of a sequence: four per CU in all, none with less than a unit of keys per wave.
+// Workgroups that share out the tokens of a sequence.  One of eight waves, which writes the results, for up to 640 tokens (4 and 256, us: 1 x 8K
+// 16.2 -> 11.6, 16 in e4m3 26.8 -> 13.2; 4 and 512 15.6 -> 14.7, 768 15.3 -> 16.3) and where there are jobs for all slots (64 sequences in e4m3, 4 and
+// 2048 72 -> 62).  Else four of four waves, or what two slots per CU take, none with less than a unit of keys per wave (4 and 4096 with 2 / 4 / 8 / 16:
+// 48 sequences in e4m3 89 / 93 / 102 / 116, 24 50 / 44 / 48 / 53, 16 in bf16 51 / 50 / 53 / 55).
 int window_splits(const Plan& pl, int q_len, int64_t longest) {
   const int vectors = pl.group * q_len, rounds = vectors <= 16 ? 1 : (vectors + 31) / 32;
-  const int64_t jobs = (int64_t)pl.p.batch * pl.p.n_kv_heads * rounds;
-  return (int)std::min<int64_t>({(4 * pl.num_cus + jobs - 1) / jobs, (longest + kUnit * kAttendWaves - 1) / (kUnit * kAttendWaves), kSplitsMax});
+  const int64_t jobs = (int64_t)pl.p.batch * pl.p.n_kv_heads * rounds, slots = 2 * pl.num_cus;
+  if (longest <= 640 || (jobs >= slots && longest <= 4608)) return 1;
+  return (int)std::min<int64_t>({std::max<int64_t>(4, (slots + jobs - 1) / jobs), (longest + kUnit * kAttendWaves - 1) / (kUnit * kAttendWaves), kSplitsMax});
 }
 
 hipError_t launch_rows(const Plan& pl, AttendArgs& A, const void* q, const void* k, const void* v, const int32_t* block_table, int sink,
@@ -77,7 +89,8 @@ hipError_t launch_window(const Plan& pl, const void* q, const void* k, const voi
 }
 
 size_t few_workspace_bytes(const Plan& pl, int n_new) {
-  return (size_t)pl.p.batch * n_new * pl.p.n_q_heads * window_splits(pl, n_new, pl.p.n_max) * (pl.p.head_dim + 2) * sizeof(float);
+  const int splits = window_splits(pl, n_new, pl.p.n_max);  // (a window leaves no more)
+  return splits == 1 ? 0 : (size_t)pl.p.batch * n_new * pl.p.n_q_heads * splits * (pl.p.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_few(const Plan& pl, const void* q, int64_t q_stride, int n_new, const int32_t* first, const int32_t* new_lens, const void* k,

@@ -220,6 +220,48 @@ def test_first_scores_all_minus_infinity():
         _check_rows(s, q, _places(s, [60], None, 140), 0, 0, o, lse, bf16, finite=False)
 
 
+# (batch, hq, hkv, d, n_max, page, fmt, n_new, first, new_lens, sink, window)
+SHARED = [
+    # tiles that are cut into pieces: one long sequence, the same among short ones, in a window, with a last piece of one tile
+    (1, 4, 1, 128, 4000, 16, 0, 33, [3967], None, 0, 0),
+    (3, 4, 2, 64, 6000, 0, 1, 40, [5960, 100, 3], [40, 40, 0], 0, 0),
+    (2, 8, 1, 128, 3500, 64, 2, 70, [3430, 900], [70, 3], 300, 2500),
+    (1, 2, 1, 64, 5001, 0, 0, 200, [4801], [131], 0, 0),
+    # the same sizes with few new tokens: the kernel of the decode steps, in several workgroups
+    (1, 4, 1, 128, 4000, 16, 0, 8, [3991], None, 0, 0), (3, 4, 2, 64, 6000, 0, 1, 3, [5960, 100, 3], [2, 3, 0], 0, 0),
+    (2, 8, 1, 128, 3500, 64, 2, 4, [3430, 900], [4, 3], 300, 2500), (2, 1, 1, 64, 5001, 0, 0, 17, [4984, 17], None, 0, 0),
+    # more sequences than a wave has lanes, and than it looks through
+    (130, 2, 2, 64, 96, 16, 0, 33, [(i * 37) % 90 for i in range(130)], [(i * 5) % 34 for i in range(130)], 0, 0),
+    (300, 4, 1, 64, 64, 0, 1, 20, [(i * 37) % 60 - 1 for i in range(300)], [(i * 7) % 21 for i in range(300)], 2, 9),
+]
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("case", SHARED, ids=lambda c: "-".join(str(x) for x in c[:8]) + f"-{c[10]}-{c[11]}")
+def test_chunk_of_shared_work(case, bf16):
+    batch, hq, hkv, d, n_max, page, fmt, n_new, first, new, sink, window = case
+    s = Setup(batch, hq, hkv, d, n_max, page, fmt, None, seed=n_max + n_new)
+    q = _bf16(s.rng.normal(size=(batch, n_new, hq, d)))
+    o, lse = _chunk(s, q, first, new, sink, window, bf16)
+    _check_rows(s, q, _places(s, first, new, n_new), sink, window, o, lse, bf16)
+
+
+@pytest.mark.parametrize("n_new", [3, 40])
+def test_infinity_and_nan_in_pieces(n_new):
+    """As above, where several workgroups have the keys: pieces that a NaN lies in, and pieces that it does not reach."""
+    s = Setup(1, 4, 1, 128, 3000, 0, 0, None, seed=14)
+    for tok, value in ((2999, [INF, 1.0, NAN]), (2998, [INF, -INF, 1.0]), (1500, [1.0, NAN, 1.0]), (70, [-INF, 1.0, 1.0])):
+        row = s.rng.normal(size=128)
+        row[3:6] = value
+        s.set_row(s.v, 0, 0, tok, values=row)
+    s.set_row(s.k, 0, 0, 1000, values=np.full(128, NAN))
+    q = _bf16(s.rng.normal(size=(1, n_new, 4, 128)))
+    for sink, window in ((0, 0), (60, 1400), (71, 1450), (0, 1900)):
+        for bf16 in (False, True):
+            o, lse = _chunk(s, q, [3000 - n_new], None, sink, window, bf16)
+            _check_rows(s, q, _places(s, [3000 - n_new], None, n_new), sink, window, o, lse, bf16, finite=False)
+
+
 # ---- decode steps over a window --------------------------------------------------------------------------------------------------
 
 WINDOWS = [
@@ -230,6 +272,10 @@ WINDOWS = [
     (1, 8, 1, 128, 900, 0, 2, 12, [899], 70, 500), (1, 2, 1, 128, 1000, 256, 0, 40, [998], 1, 300), (2, 2, 2, 64, 150, 0, 1, 3, [150, 2], 200, 4),
     (1, 4, 1, 128, 9000, 0, 0, 1, [8999], 4, 4096), (1, 4, 1, 64, 170752, 64, 1, 1, [170752], 128, 128), (2, 2, 1, 64, 300, 0, 0, 2, [300, 299], 0, 1 << 30),
     (40, 2, 1, 64, 64, 16, 1, 1, [1 + (i * 37) % 64 for i in range(40)], 2, 7), (1, 4, 4, 128, 64, 0, 0, 1, [64], 1 << 30, 1),
+    # several workgroups for a sequence's tokens
+    (2, 4, 1, 128, 3000, 16, 1, 1, [3000, 700], 128, 1000), (2, 8, 1, 64, 3000, 0, 2, 1, [2999, 5], 0, 2000), (1, 8, 2, 128, 2500, 64, 0, 2, [2500], 300, 900),
+    (2, 4, 2, 64, 2000, 0, 0, 11, [2000, 1300], 37, 700), (1, 2, 2, 128, 2000, 8, 2, 3, [1999], 5, 1500), (2, 4, 4, 64, 1500, 0, 1, 7, [1500, 3], 0, 1 << 30),
+    (70, 8, 8, 64, 700, 0, 0, 1, [1 + (i * 137) % 700 for i in range(70)], 9, 690),
 ]
 
 
@@ -273,6 +319,26 @@ def test_window_decode_infinity_and_nan(page, q_len):
     for sink, window in ((4, 30), (11, 25), (0, 1), (0, 29)):
         o, lse = _window(s, q, lens, sink, window)
         _check_rows(s, q, _decode_places(s, lens), sink, window, o, lse, False, finite=False)
+
+
+@pytest.mark.parametrize("q_len", [1, 2, 6])
+def test_window_decode_infinity_and_nan_in_pieces(q_len):
+    s = Setup(1, 4, 1, 128, 3000, 0, 0, None, q_len, seed=15)
+    for tok, value in ((2999, [INF, 1.0, NAN]), (2000, [1.0, NAN, 1.0]), (5, [-INF, 1.0, 1.0])):
+        row = s.rng.normal(size=128)
+        row[3:6] = value
+        s.set_row(s.v, 0, 0, tok, values=row)
+    s.set_row(s.k, 0, 0, 1200, values=np.full(128, NAN))
+    low = s.rng.normal(size=128)
+    low[0] = -INF
+    s.set_row(s.k, 0, 0, 2500, values=low)
+    q = s.rng.normal(size=(1, q_len, 4, 128))
+    q[..., 0] = np.abs(q[..., 0]) + 0.1
+    q = _bf16(q)
+    for lens in ([2999], [3000]):
+        for sink, window in ((4, 900), (6, 1700), (0, 998), (0, 1802)):
+            o, lse = _window(s, q, lens, sink, window)
+            _check_rows(s, q, _decode_places(s, lens), sink, window, o, lse, False, finite=False)
 
 
 def test_windows_as_wide_as_the_sequence_are_dense_attention():
