@@ -628,16 +628,39 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   const uint64_t odd = __ballot(!(sum < INFINITY) || !(l < INFINITY));
   uint32_t again = (uint32_t)odd | (uint32_t)(odd >> 32);
   const int64_t out_row = ((int64_t)b * A.n_new + t) * A.Hq + head;
-  const float m_own = saw && mrun == -INFINITY ? -3.0e38f : mrun;
+  const float m_own = saw && mrun == -INFINITY ? -3.0e38f : mrun, inv = 1.f / l;
+  // bf16: a row's two lanes change columns 8 x + 4 half .. + 3 of two groups for all 8 of one
+  uint4 out16[BF16 ? E : 1][2];
+  if constexpr (BF16) {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        uint32_t w[2][2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) w[y][z] = pack_bf16(acc[e][8 * x + 4 * y + 2 * z] * inv, acc[e][8 * x + 4 * y + 2 * z + 1] * inv);
+        const auto a = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false), b = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+        out16[e][x] = make_uint4(a[0], b[0], a[1], b[1]);
+      }
+  }
   if (row < rows && !(again >> col & 1)) {
     if (pieces == 1) {
-      const float inv = 1.f / l;
+      if constexpr (BF16) {
 #pragma unroll
-      for (int e = 0; e < E; ++e)
+        for (int e = 0; e < E; ++e)
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          store_4<BF16>(A.out_o, out_row * D + 32 * e + 8 * x + 4 * half, acc[e][4 * x] * inv, acc[e][4 * x + 1] * inv, acc[e][4 * x + 2] * inv,
-                        acc[e][4 * x + 3] * inv);
+          for (int x = 0; x < 2; ++x)
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(A.out_o) + (out_row * D + 32 * e + 16 * x + 8 * half)) = out16[e][x];
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            store_4<false>(A.out_o, out_row * D + 32 * e + 8 * x + 4 * half, acc[e][4 * x] * inv, acc[e][4 * x + 1] * inv, acc[e][4 * x + 2] * inv,
+                           acc[e][4 * x + 3] * inv);
+      }
       if (A.out_lse && half == 0) A.out_lse[out_row] = m_own * 0.69314718055994530942f + logf(l);
     } else {
       const int64_t place = (int64_t)W.slot * kTileRows + wave * kWaveRows + col;
@@ -678,6 +701,7 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_merge_kernel(ChunkArgs A)
   constexpr int C = D / kWave, kAhead = 8;
   static_assert(kPiecesMax <= kWave, "a pair per lane");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kvh = blockIdx.x % A.Hkv;
+  const int part = blockIdx.y * kChunkWaves + wave, parts = gridDim.y * kChunkWaves;
   const int g_shift = 31 - __builtin_clz(A.Hq / A.Hkv);
   Batch all;
   all.read(A, g_shift);
@@ -685,9 +709,9 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_merge_kernel(ChunkArgs A)
     Work w;
     if (!all.find(A, y, w)) return;
     const NewTokens New = new_tokens(A, w.b);
-    // (every piece of a tile takes its share of the tile's rows)
+    // (the workgroups of all pieces share out the tile's rows)
     const int n = min((New.count << g_shift) - w.tile * kTileRows, kTileRows);
-    for (int r = w.piece * kChunkWaves + wave; r < n; r += w.pieces * kChunkWaves) {
+    for (int r = w.piece * parts + part; r < n; r += w.pieces * parts) {
       const int row = w.tile * kTileRows + r;
       const int64_t out_row = ((int64_t)w.b * A.n_new + (row >> g_shift)) * A.Hq + ((int64_t)kvh << g_shift) + (row & ((1 << g_shift) - 1));
       const int slot0 = (y - w.piece) * A.Hkv + kvh;
@@ -755,8 +779,11 @@ hipError_t launch_chunk_t(const Plan& pl, const ChunkArgs& A, hipStream_t st) {
   hipLaunchKernelGGL((chunk_kernel<D, FMT, PAGED, TERMS>), dim3((uint32_t)(tiles + pieces)), dim3(kChunkThreads), 0, st, A);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || A.room == 0) return e;
-  const int64_t wgs = std::min<int64_t>(A.room, (4 * pl.num_cus + A.Hkv - 1) / A.Hkv);
-  hipLaunchKernelGGL((chunk_merge_kernel<D, TERMS == 1>), dim3((uint32_t)(wgs * A.Hkv)), dim3(kChunkThreads), 0, st, A);
+  // About a row per wave where a tile has few pieces (4 x 1K tokens, 32 new ones each, whole call 28.5 us with one workgroup per piece, 21.8 with
+  // eight); one workgroup per piece where cuts are unlikely (with eight windowed prompts that are not cut take 147 us instead of 141).
+  const int64_t rows = std::min<int64_t>(kTileRows, (int64_t)A.n_new * pl.group), wgs = std::min<int64_t>(A.room, (4 * pl.num_cus + A.Hkv - 1) / A.Hkv);
+  const int64_t parts = 2 * tiles >= pieces ? 1 : std::max<int64_t>(1, std::min<int64_t>(8, rows / kChunkWaves * tiles / pieces));
+  hipLaunchKernelGGL((chunk_merge_kernel<D, TERMS == 1>), dim3((uint32_t)(wgs * A.Hkv), (uint32_t)parts), dim3(kChunkThreads), 0, st, A);
   return hipGetLastError();
 }
 template <int D, int FMT>
