@@ -222,12 +222,15 @@ __device__ __forceinline__ int k_place(int row, int c) { return row * (2 * D) + 
 template <int D>
 __device__ __forceinline__ int v_place(int row, int c) { return row * (2 * D) + (v_chunk<D>(row, c) << 4); }
 
+// 16 bytes per lane from global memory (a uniform address and a lane's offset) into LDS, the lanes' one behind the other from a uniform place on.
+// In assembly, since the compiler lets every transposed read of LDS wait for all such loads; what it does not see has to be awaited by
+// wait_loads.  (The result goes to LDS: there is no register that it could overwrite.  M0 is reserved, and nothing else here uses it.)
 __device__ __forceinline__ void load_lds_16(const unsigned char* base, uint32_t off, unsigned char* dst) {
   typedef __attribute__((address_space(3))) unsigned char* Lds;
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"((uint32_t)(uintptr_t)(Lds)dst), "v"(off), "s"(base) : "memory");
 }
 // Until this wave's loads into LDS are there (a barrier waits for the other waves').
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }  // vmcnt(0)
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 template <bool BF16>
 __device__ __forceinline__ void store_4(void* out, int64_t at, float a, float b, float c, float d) {

@@ -141,6 +141,31 @@ def test_queries_of_a_fused_projection_and_no_lse(bf16):
     _check_rows(s, q, _places(s, [0, 130], None, 130), 0, 0, o, None, bf16)
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+def test_few_queries_of_a_fused_projection(bf16):
+    s = Setup(2, 4, 2, 64, 700, 16, 1, None, seed=17)
+    x = _bf16(s.rng.normal(size=(2, 5, (4 + 2 + 2) * 64)))
+    q = x[..., 2 * 64:6 * 64].unflatten(-1, (4, 64))
+    o, lse = _chunk(s, q, [690, 17], [5, 2], 0, 0, bf16)
+    _check_rows(s, q, _places(s, [690, 17], [5, 2], 5), 0, 0, o, lse, bf16)
+
+
+@pytest.mark.parametrize("page", [0, 16])
+def test_a_cache_in_host_memory(page):
+    """K and V in pinned host memory: the same results, bit for bit."""
+    s = Setup(2, 4, 2, 128, 400, page, 0, None, seed=18)
+    q = _bf16(s.rng.normal(size=(2, 150, 4, 128)))
+    one = q[:, 0].contiguous()
+    res = []
+    for host in (False, True):
+        if host:
+            kept = [torch.empty(x.shape, dtype=x.dtype, pin_memory=True).copy_(x) for x in (s.k, s.v)]
+            s.k, s.v = (s.vb.vatt_host_kv_device_pointer(x) for x in kept)
+        res.append([*_chunk(s, q, [250, 0], [150, 90], 0, 0, True), *_chunk(s, q, [250, 0], [150, 90], 3, 70, False),
+                    *_chunk(s, q[:, :3].contiguous(), [397, 5], None, 0, 0, False), *_window(s, one, [400, 77], 5, 60)])
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
 @pytest.mark.parametrize("scale", [0.01, 3.0])
 @pytest.mark.parametrize("fmt", [0, 2])
 def test_chunk_with_another_scale(scale, fmt):
