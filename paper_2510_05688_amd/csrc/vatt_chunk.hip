@@ -18,6 +18,7 @@ static_assert(kTileRows == kWaveRows * kChunkWaves, "32 rows of every wave");
 constexpr int kTileKeys = 64;
 constexpr int kPiecesMax = 64;      // pieces that a tile's keys are cut into at most
 constexpr int kPieceLeast = 4;      // key tiles of a piece at least
+constexpr float kOnePerUnit = 5000.f;  // key tiles in all below which there is one piece per compute unit, not two
 constexpr int kSeqsPerLane = 4, kSeqsMax = kSeqsPerLane * kWave;  // sequences that a wave looks through for its work
 
 struct ChunkArgs {
@@ -77,15 +78,19 @@ struct Work {
 
 // Pieces that the tiles of sequences are cut into.  total: key tiles of all tiles of one KV head, most: if each had as many as its sequence's last one.
 // Tiles that are long beside what all work comes to per workgroup slot are cut into pieces of about that length, all tiles of a sequence into
-// equally many; their sums are joined by the merge.  (32-bit values, rounded the same way wherever this is worked out.)
+// equally many; their sums are joined by the merge.  Where there is little to do one piece per compute unit is better than two, whose sums are twice
+// the bytes: us with two / one, 16 new tokens on 1 x 16K 32.5 / 28.2, 64 45.9 / 40.7, but 64 on 3 x 5K - 16K 63.7 / 83.2, 33 with groups of 8 47.2 / 58.1.
+// They are a little longer than an equal share, so that rounding leaves none over for which nobody is free (33 with groups of 8 55.0 -> 47.2).
+// (32-bit values, rounded the same way wherever this is worked out.)
 struct Cut {
   float piece;  // key tiles; 0: nothing is cut
   __device__ __forceinline__ Cut(const ChunkArgs& A, float total, float most, int longest) {
 #pragma clang fp contract(off)
     const float share = total * A.Hkv / A.slots;
-    piece = A.room > 0 && longest > 1.25f * share + 12.f ? fmaxf(most * A.Hkv / A.slots, (float)kPieceLeast) : 0.f;
+    const float at_once = 0.97f * (most * A.Hkv < kOnePerUnit ? A.slots / 2 : A.slots);
+    piece = A.room > 0 && longest > 1.25f * share + 12.f ? fmaxf(most * A.Hkv / at_once, (float)kPieceLeast) : 0.f;
   }
-  __device__ __forceinline__ int pieces(int last) const { return piece == 0.f || last == 0 ? 1 : min((int)ceilf(last / piece), kPiecesMax); }
+  __device__ __forceinline__ int pieces(int last) const { return piece == 0.f ? 1 : max(min((int)(last / piece + 0.5f), kPiecesMax), 1); }
 };
 
 // A sequence's tiles: how many, and the key tiles of the first and the last one.
@@ -755,8 +760,7 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_merge_kernel(ChunkArgs A)
   }
 }
 
-// Tiles of all sequences if every new token counts, and pieces of tiles at most: a sequence's tiles are cut where they are longer than the piece,
-// of which all tiles at their longest have no more than there are slots, so that the rounding up at most doubles that.
+// Tiles of all sequences if every new token counts.
 int64_t chunk_tiles(const Plan& pl, int n_new) {
   return (int64_t)pl.p.batch * pl.p.n_kv_heads * (((int64_t)n_new * pl.group + kTileRows - 1) / kTileRows);
 }
@@ -770,6 +774,8 @@ bool chunk_may_cut(const Plan& pl, int n_new) {
   const double tiles = (double)chunk_tiles(pl, n_new) / chunk_slots(pl);
   return longest > 1.25 * tiles * (longest - own / 2) + 12 || own > 1.25 * tiles * own / 2 + 12;
 }
+// Pieces at most: a sequence's tiles are cut into two or more where they are one and a half pieces long, and all tiles at their longest have no more
+// than a piece for every slot, so that the rounding adds a third.
 int64_t chunk_pieces(const Plan& pl, int n_new) {
   if (!chunk_may_cut(pl, n_new)) return 0;
   const int64_t longest = (pl.p.n_max + kTileKeys - 1) / kTileKeys, each = std::min<int64_t>((longest + kPieceLeast - 1) / kPieceLeast, kPiecesMax);
