@@ -31,15 +31,17 @@ struct AttendArgs {
   const int32_t* seq_lens;
   const int32_t* blocks;
   const int32_t* block_count;
-  float* part;     // [B * q_len * Hq][splits][d]: sums of the weighted V rows
-  float2* part_ml;  // [B * q_len * Hq][splits]: (max in units of log 2, sum of the weights); max -Inf: no token seen
+  float* part;     // [B * q_len * Hq][splits][d] or, dealt out, [slot_rows][slots][d]: sums of the weighted V rows
+  float2* part_ml;  // the same without d: (max in units of log 2, sum of the weights); max -Inf: no token seen
   float* out_o;
   float* out_lse;
   RowMap M;
   int Hq, Hkv, q_len, splits, rounds, capacity, block_shift;
   float log2_scale;  // softmax scale / ln 2
   // kFirstAndWindow:
-  int sink, window, out_bf16;
+  int sink, window, out_bf16, batch;
+  int2* jobs;                 // [rounds][Hkv][B]: the first of a job's places for sums, and how many it has
+  int workgroups, slots, slot_rows;  // dealt out: workgroups at most, places for sums, vectors of each
   int64_t q_stride;         // elements between query tokens
   const int32_t* first;     // the first query token's position; nullptr: the q_len newest tokens of seq_lens
   const int32_t* new_lens;  // how many query tokens count; nullptr: all
@@ -212,13 +214,19 @@ __device__ __forceinline__ void store_row(const AttendArgs& A, int64_t at, const
 // same loads without the products and exponentials take 164; lists of 12 x 4K - 64K tokens with two queries each (98 MB in pieces of 2 KB, with scales of 64
 // bytes apart from them) 28 us, loads alone 22.  Half or twice as many workgroups, three of them on a CU instead of two, and a least
 // number of chunks for each made no difference or were slower.
-// WHOLE (kFirstAndWindow): one workgroup, of WAVES waves, has all tokens of a sequence and KV head, and writes the results.
-template <int D, int FMT, bool PAGED, int KIND, int NQT, int PACK, int WAVES = kAttendWaves, bool WHOLE = false>
-__global__ __launch_bounds__(WAVES * kWave, 2) void attend_kernel(AttendArgs A) {
+// A workgroup's part of the work: chunks first, first + step, .. of a token list, at most `count` of them.
+struct AttendPart {
+  int z, kvh, round;  // sequence (kListedBlocks: sequence and query token), KV head, which vectors
+  int first, step, count;
+  int slot;    // where the sums go
+  bool whole;  // kFirstAndWindow: these are all tokens, and the results are written
+  QueryTokens queries;  // kFirstAndWindow
+};
+template <int D, int FMT, bool PAGED, int KIND, int NQT, int PACK, int WAVES>
+__device__ __forceinline__ void attend_part(const AttendArgs& A, const AttendPart& part) {
   constexpr int kThreads = WAVES * kWave;
   constexpr int kChunk = 4 * WAVES;  // groups of 8 tokens that a workgroup takes at a time: a unit for each wave
   static_assert(WAVES == 4 || WAVES == 8, "see the end");
-  static_assert(!WHOLE || KIND == kFirstAndWindow, "the others have a merge");
   constexpr bool LIST = KIND == kListedBlocks, RANGE = KIND == kFirstAndWindow;
   constexpr int S = D / 32;  // steps over a row of K
   constexpr int E = D / 16;  // values of a V row per lane = tiles over the head dimension
@@ -232,18 +240,18 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_kernel(AttendArgs A) 
   static_assert(PACK == 1 || NQT == 1, "packed terms are of one tile");
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g4 = lane >> 4;
-  const int kvh = blockIdx.x, split = (int)blockIdx.y / A.rounds, round = (int)blockIdx.y - split * A.rounds;
+  const int kvh = part.kvh, round = part.round;
   const int G = A.Hq / A.Hkv, Q = A.q_len;
-  const int seq = LIST ? seq_of_pair(blockIdx.z, Q) : blockIdx.z;
+  const int seq = LIST ? seq_of_pair(part.z, Q) : part.z;
   QueryTokens T = {0, Q};
-  if constexpr (RANGE) T = query_tokens(A, seq);
+  if constexpr (RANGE) T = part.queries;
   const int n_seq = RANGE ? max(T.first + T.count, 1) : min(max(A.seq_lens[seq], 1), A.M.n_max);
   // LIST: the vectors are the heads of one query token; else those of all query tokens
-  const int t0 = LIST ? (int)blockIdx.z - seq * Q : 0, vectors = LIST ? G : T.count * G;
+  const int t0 = LIST ? part.z - seq * Q : 0, vectors = LIST ? G : T.count * G;
   const int n = LIST ? max(n_seq - (Q - 1 - t0), 1) : n_seq;
   const int c_base = round * 16 * NQT;
   if (RANGE && c_base >= vectors) return;
-  const TokenList L = token_list<KIND>(A, blockIdx.z, kvh, n, RANGE ? max(max(T.first + 1, 1) - A.window, 0) : 0);
+  const TokenList L = token_list<KIND>(A, part.z, kvh, n, RANGE ? max(max(T.first + 1, 1) - A.window, 0) : 0);
 
   __shared__ __align__(16) int s_tok[kSlots];
   __shared__ __align__(16) int s_at[kSlots];
@@ -368,10 +376,10 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_kernel(AttendArgs A) 
     }
   };
 
-  // The chunks of the list go round the workgroups, so that which entries a workgroup looks up first does not depend on the length.
-  auto group_of = [&](int i) { return (split + (i / kChunk) * A.splits) * kChunk + i % kChunk; };
+  auto group_of = [&](int i) { return (part.first + (i / kChunk) * part.step) * kChunk + i % kChunk; };
   const int entry0 = entry_of<KIND>(L, group_of(tid));
-  const int chunks = (L.count + kChunk - 1) / kChunk, mine = split < chunks ? (chunks - split + A.splits - 1) / A.splits : 0;
+  const int chunks = (L.count + kChunk - 1) / kChunk, left = part.first < chunks ? (chunks - part.first + part.step - 1) / part.step : 0;
+  const int mine = RANGE ? min(left, part.count) : left;
   for (int c0 = 0; c0 < mine; c0 += kSlots / kChunk) {
     const int c_n = min(kSlots / kChunk, mine - c0);
     if (c0 > 0) __syncthreads();
@@ -537,7 +545,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_kernel(AttendArgs A) 
 
   // The waves' sums together, one 16-vector tile at a time, in the result layout (of eight waves the upper four's go to the lower four first):
   // wave w finishes rows 4 g + w.
-  uint32_t odd = 0;  // WHOLE: vectors of the tile with an Inf or a NaN
+  uint32_t odd = 0;  // vectors with an Inf or a NaN with an Inf or a NaN
 #pragma unroll
   for (int nt = 0; nt < NQT; ++nt) {
     float l = lrun[nt];
@@ -599,7 +607,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_kernel(AttendArgs A) 
     if (c < vectors && (WAVES == 4 || wave < 4)) {
       const int t = t0 + c / G, g = c % G;
       const int64_t row = ((int64_t)seq * Q + t) * A.Hq + (int64_t)kvh * G + g;
-      const int64_t place = row * A.splits + split;
+      const int64_t place = RANGE ? (int64_t)(nt * 16 + i16) * A.slots + part.slot : row * A.splits + part.slot;
 #pragma unroll
       for (int e = 0; e < E; e += 4) {
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -614,7 +622,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_kernel(AttendArgs A) 
             o.w += y.w * fac[w];
           }
         }
-        if constexpr (WHOLE) {
+        if (RANGE && part.whole) {
           bad |= !(fabsf(o.x) + fabsf(o.y) + fabsf(o.z) + fabsf(o.w) < INFINITY);
           store_row<4>(A, row * D + E * (4 * g4 + wave) + e, {o.x / l, o.y / l, o.z / l, o.w / l});
         } else {
@@ -622,22 +630,23 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_kernel(AttendArgs A) 
         }
       }
       if (wave == 0 && g4 == 0) {
-        if constexpr (!WHOLE) A.part_ml[place] = make_float2(m, l);
+        if (!RANGE || !part.whole) A.part_ml[place] = make_float2(m, l);
         else if (A.out_lse) A.out_lse[row] = m * 0.69314718055994530942f + logf(l);
       }
       bad |= !(l < INFINITY);
     }
-    if constexpr (WHOLE) {
+    if (RANGE && part.whole) {
       const uint64_t there = __ballot(bad);
       odd |= (uint32_t)((there | there >> 16 | there >> 32 | there >> 48) & 0xffff) << (16 * nt);
     }
   }
-  if constexpr (WHOLE) {
+  if (RANGE && part.whole) {
     // (see attend_merge_kernel)
     __syncthreads();
     if (lane == 0) s_tok[wave] = (int)odd;
     __syncthreads();
-    odd = (uint32_t)(s_tok[0] | s_tok[1] | s_tok[2] | s_tok[3]);
+    odd = (uint32_t)__builtin_amdgcn_readfirstlane(s_tok[0] | s_tok[1] | s_tok[2] | s_tok[3]);
+    if (__builtin_expect(odd == 0, 1)) return;
     __syncthreads();
     float(&s_acc)[WAVES][D] = *reinterpret_cast<float(*)[WAVES][D]>(&s_o[0][0][0][0]);
     float(&s_m2)[WAVES] = *reinterpret_cast<float(*)[WAVES]>(&s_m[0][0]);
@@ -664,6 +673,121 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attend_kernel(AttendArgs A) 
   }
 }
 
+// All tokens and listed blocks: the chunks of a list go round the `splits` workgroups, so that which entries a workgroup looks up first does not
+// depend on the length.
+template <int D, int FMT, bool PAGED, int KIND, int NQT, int PACK>
+__global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A) {
+  const int split = (int)blockIdx.y / A.rounds;
+  attend_part<D, FMT, PAGED, KIND, NQT, PACK, kAttendWaves>(
+      A, {(int)blockIdx.z, (int)blockIdx.x, (int)blockIdx.y - split * A.rounds, split, A.splits, INT32_MAX, split, false, {0, 0}});
+}
+
+// The first tokens and a window, one workgroup of eight waves for a sequence, KV head and 32 vectors.
+template <int D, int FMT, bool PAGED, int NQT, int PACK>
+__global__ __launch_bounds__(8 * kWave, 2) void window_kernel(AttendArgs A) {
+  attend_part<D, FMT, PAGED, kFirstAndWindow, NQT, PACK, 8>(A, {(int)blockIdx.z, (int)blockIdx.x, (int)blockIdx.y, 0, 1, INT32_MAX, 0, true, query_tokens(A, blockIdx.z)});
+}
+
+// The same dealt out: the chunks of all sequences, one behind the other, KV head by KV head, in equal shares to the workgroups.  A job (sequence,
+// KV head, vectors) that one workgroup has alone it finishes; the sums of the others are joined by the merge.  Lane l of a wave looks at
+// sequences l, l + 64, ..
+constexpr int kDealtMost = kAttendThreads;  // sequences, one per thread
+struct DealtSeq {
+  int upto, own;  // chunks of the sequences of its wave up to and with this one, and its own
+  QueryTokens queries;
+};
+struct Deal {
+  const DealtSeq* seqs;
+  int of_wave[kAttendWaves], total;  // chunks of a wave's sequences, and of all, of one KV head and set of vectors
+  int share, more;                   // the first `more` workgroups have share + 1
+  QueryTokens only;                  // of a batch of one, which needs no list
+  __device__ __forceinline__ static int chunks_of(const AttendArgs& A, const QueryTokens& T) {
+    constexpr int kChunk = 4 * kAttendWaves;
+    if (T.count == 0) return 0;
+    return (token_list<kFirstAndWindow>(A, 0, 0, max(T.first + T.count, 1), max(max(T.first + 1, 1) - A.window, 0)).count + kChunk - 1) / kChunk;
+  }
+  // By the whole workgroup.
+  __device__ __forceinline__ Deal(const AttendArgs& A, DealtSeq (&s_seqs)[kDealtMost]) : seqs(s_seqs) {
+    const int tid = threadIdx.x;
+    total = 0;
+    only = {0, 0};
+#pragma unroll
+    for (int w = 0; w < kAttendWaves; ++w) of_wave[w] = 0;
+    if (A.batch == 1) {
+      only = query_tokens(A, 0);
+      of_wave[0] = total = chunks_of(A, only);
+    } else {
+      if (A.batch > (tid & ~(kWave - 1))) {
+        DealtSeq s = {0, 0, {0, 0}};
+        if (tid < A.batch) {
+          s.queries = query_tokens(A, tid);
+          s.own = chunks_of(A, s.queries);
+        }
+        s.upto = (int)wave_inclusive_scan_u32((uint32_t)s.own);
+        s_seqs[tid] = s;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kAttendWaves; ++w) {
+        if (A.batch > w * kWave) of_wave[w] = __builtin_amdgcn_readfirstlane(s_seqs[w * kWave + kWave - 1].upto);
+        total += of_wave[w];
+      }
+    }
+    const int all = total * A.Hkv * A.rounds, workgroups = max(min(A.workgroups, all), 1);
+    share = all / workgroups;
+    more = all - share * workgroups;
+  }
+  __device__ __forceinline__ int begin(int w) const { return w * share + min(w, more); }
+  __device__ __forceinline__ int owner(int x) const {
+    const int longer = more * (share + 1);
+    return x < longer ? x / (share + 1) : more + (x - longer) / max(share, 1);
+  }
+  struct Seq {
+    int b, from, n;  // its first chunk, and how many
+    QueryTokens queries;
+  };
+  __device__ __forceinline__ Seq seq(int b) const {
+    if (only.count > 0) return {0, 0, total, only};
+    const DealtSeq s = seqs[b];
+    const int n = __builtin_amdgcn_readfirstlane(s.own);
+    int from = __builtin_amdgcn_readfirstlane(s.upto) - n;
+#pragma unroll
+    for (int w = 0; w + 1 < kAttendWaves; ++w) from += b >= (w + 1) * kWave ? of_wave[w] : 0;
+    return {b, from, n, {__builtin_amdgcn_readfirstlane(s.queries.first), __builtin_amdgcn_readfirstlane(s.queries.count)}};
+  }
+  // The sequence that has chunk x.
+  __device__ __forceinline__ Seq find(int x) const {
+    if (only.count > 0) return seq(0);
+    int from = 0, w64 = 0, upto = 0;
+#pragma unroll
+    for (int w = 0; w + 1 < kAttendWaves; ++w) {
+      upto += of_wave[w];
+      if (x >= upto && upto < total) {
+        from = upto;
+        w64 = (w + 1) * kWave;
+      }
+    }
+    return seq(w64 + __builtin_ctzll(__ballot(x < from + seqs[w64 + (threadIdx.x & 63)].upto)));
+  }
+};
+template <int D, int FMT, bool PAGED, int NQT, int PACK>
+__global__ __launch_bounds__(kAttendThreads, 2) void dealt_kernel(AttendArgs A) {
+  __shared__ DealtSeq s_seqs[kDealtMost];
+  const Deal deal(A, s_seqs);
+  const int w = blockIdx.x, end = min(deal.begin(w + 1), deal.total * A.Hkv * A.rounds);
+  for (int x = deal.begin(w); x < end;) {
+    const int pair = x / deal.total;
+    const Deal::Seq s = deal.find(x - pair * deal.total);
+    const int job = pair * A.batch + s.b, job0 = pair * deal.total + s.from;
+    if (x == job0 && threadIdx.x == 0) A.jobs[job] = make_int2(w + job, deal.owner(job0 + s.n - 1) - w + 1);
+    const int first = x - pair * deal.total - s.from, count = min(s.n - first, end - x), round = pair / A.Hkv;
+    attend_part<D, FMT, PAGED, kFirstAndWindow, NQT, PACK, kAttendWaves>(
+        A, {s.b, pair - round * A.Hkv, round, first, 1, count, w + job, count == s.n, s.queries});
+    x += count;
+    if (x < end) __syncthreads();
+  }
+}
+
 // Merge of a head's partial sums: bound by two dependent loads.  Every wave looks at all (max, sum) pairs, one or two per lane; the threads of
 // a column take every PARTS-th partial sum each, the first ones asked for before it is known which count.
 // A result with an Inf or a NaN is worked out again: the second product of attend_kernel gives every column every V row of a step, with
@@ -676,19 +800,25 @@ __global__ __launch_bounds__(kAttendThreads) void attend_merge_kernel(AttendArgs
   __shared__ float s_acc[kAttendWaves][D], s_m[kAttendWaves], s_l[kAttendWaves];
   const int h = blockIdx.x, tid = threadIdx.x, c = tid % D, part = tid / D, lane = tid & 63;
   const int64_t vb = blockIdx.y, head = vb * A.Hq + h;
+  int splits = A.splits;
+  int64_t place = head * A.splits;  // its partial sums
   const int seq = seq_of_pair((int)vb, A.q_len), t = (int)vb - seq * A.q_len;
   QueryTokens T = {0, A.q_len};
   if constexpr (KIND == kFirstAndWindow) {
     T = query_tokens(A, seq);
-    if (t >= T.count) return;
+    const int G = A.Hq / A.Hkv, vector = t * G + h % G, round = vector / A.slot_rows;
+    const int2 job = A.jobs[(round * A.Hkv + h / G) * A.batch + seq];
+    if (t >= T.count || job.y == 1) return;  // (nothing to do, or done)
+    splits = min(job.y, kSplitsMax);
+    place = (int64_t)(vector - round * A.slot_rows) * A.slots + job.x;
   }
-  const float2* ml = A.part_ml + head * A.splits;
-  const float* p = A.part + head * A.splits * D + c;
+  const float2* ml = A.part_ml + place;
+  const float* p = A.part + place * D + c;
   const float2 none = make_float2(-INFINITY, 0.f);
-  const float2 x0 = lane < A.splits ? ml[lane] : none, x1 = kWave + lane < A.splits ? ml[kWave + lane] : none;
+  const float2 x0 = lane < splits ? ml[lane] : none, x1 = kWave + lane < splits ? ml[kWave + lane] : none;
   float first[kAhead];
 #pragma unroll
-  for (int u = 0; u < kAhead; ++u) first[u] = p[min(part + u * PARTS, A.splits - 1) * D];
+  for (int u = 0; u < kAhead; ++u) first[u] = p[min(part + u * PARTS, splits - 1) * D];
   float m = wave_max(fmaxf(x0.x, x1.x));
   // (pieces without a token, whose sums nobody wrote, do not count; one whose weight is 0 does, for the sake of an Inf or a NaN in it)
   auto counts = [](float2 x) { return x.x > -INFINITY; };
@@ -697,17 +827,17 @@ __global__ __launch_bounds__(kAttendThreads) void attend_merge_kernel(AttendArgs
   const uint64_t there0 = __ballot(counts(x0)), there1 = __ballot(counts(x1));
   float l = wave_sum_f32((counts(x0) ? x0.y * w0 : 0.f) + (counts(x1) ? x1.y * w1 : 0.f)), a = 0.f;
   auto weight = [&](int s) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s < kWave ? w0 : w1), s & (kWave - 1))); };
-  auto there = [&](int s) { return s < A.splits && ((s < kWave ? there0 : there1) >> (s & (kWave - 1)) & 1u); };
+  auto there = [&](int s) { return s < splits && ((s < kWave ? there0 : there1) >> (s & (kWave - 1)) & 1u); };
   const int wave_part = __builtin_amdgcn_readfirstlane(part);
 #pragma unroll
   for (int u = 0; u < kAhead; ++u) {
     const int s = wave_part + u * PARTS;
     if (there(s)) a += first[u] * weight(s);
   }
-  for (int s0 = wave_part + kAhead * PARTS; s0 < A.splits; s0 += kAhead * PARTS) {
+  for (int s0 = wave_part + kAhead * PARTS; s0 < splits; s0 += kAhead * PARTS) {
     float more[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) more[u] = p[min(s0 + u * PARTS, A.splits - 1) * D];
+    for (int u = 0; u < kAhead; ++u) more[u] = p[min(s0 + u * PARTS, splits - 1) * D];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int s = s0 + u * PARTS;

@@ -5,29 +5,29 @@ namespace vatt {
 namespace {
 
 template <int D, int FMT, bool PAGED>
-hipError_t launch_window_f(const AttendArgs& A, int batch, hipStream_t st) {
-  const dim3 grid(A.Hkv, A.splits * A.rounds, batch), threads(kAttendThreads);
+hipError_t launch_window_f(const AttendArgs& A, hipStream_t st) {
   const int vectors = A.Hq / A.Hkv * A.q_len;
-  if (A.splits == 1) {
-    const dim3 eight(8 * kWave);
-    if (vectors <= 5) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 3, 8, true>), grid, eight, 0, st, A);
-    else if (vectors <= 8) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 2, 8, true>), grid, eight, 0, st, A);
-    else if (vectors <= 16) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 1, 8, true>), grid, eight, 0, st, A);
-    else hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 2, 1, 8, true>), grid, eight, 0, st, A);
+  if (A.workgroups == 0) {
+    const dim3 grid(A.Hkv, A.rounds, A.batch), eight(8 * kWave);
+    if (vectors <= 5) hipLaunchKernelGGL((window_kernel<D, FMT, PAGED, 1, 3>), grid, eight, 0, st, A);
+    else if (vectors <= 8) hipLaunchKernelGGL((window_kernel<D, FMT, PAGED, 1, 2>), grid, eight, 0, st, A);
+    else if (vectors <= 16) hipLaunchKernelGGL((window_kernel<D, FMT, PAGED, 1, 1>), grid, eight, 0, st, A);
+    else hipLaunchKernelGGL((window_kernel<D, FMT, PAGED, 2, 1>), grid, eight, 0, st, A);
     return hipGetLastError();
   }
-  if (vectors <= 5) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 3>), grid, threads, 0, st, A);
-  else if (vectors <= 8) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 2>), grid, threads, 0, st, A);
-  else if (vectors <= 16) hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 1, 1>), grid, threads, 0, st, A);
-  else hipLaunchKernelGGL((attend_kernel<D, FMT, PAGED, kFirstAndWindow, 2, 1>), grid, threads, 0, st, A);
+  const dim3 grid(A.workgroups), threads(kAttendThreads);
+  if (vectors <= 5) hipLaunchKernelGGL((dealt_kernel<D, FMT, PAGED, 1, 3>), grid, threads, 0, st, A);
+  else if (vectors <= 8) hipLaunchKernelGGL((dealt_kernel<D, FMT, PAGED, 1, 2>), grid, threads, 0, st, A);
+  else if (vectors <= 16) hipLaunchKernelGGL((dealt_kernel<D, FMT, PAGED, 1, 1>), grid, threads, 0, st, A);
+  else hipLaunchKernelGGL((dealt_kernel<D, FMT, PAGED, 2, 1>), grid, threads, 0, st, A);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attend_merge_kernel<D, FMT, PAGED, kFirstAndWindow>), dim3(A.Hq, batch * A.q_len), threads, 0, st, A);
+  hipLaunchKernelGGL((attend_merge_kernel<D, FMT, PAGED, kFirstAndWindow>), dim3(A.Hq, A.batch * A.q_len), threads, 0, st, A);
   return hipGetLastError();
 }
 template <int D, int FMT>
 hipError_t launch_window_d(const Plan& pl, const AttendArgs& A, hipStream_t st) {
-  return pl.p.kv_layout == VATT_LAYOUT_PAGED ? launch_window_f<D, FMT, true>(A, pl.p.batch, st) : launch_window_f<D, FMT, false>(A, pl.p.batch, st);
+  return pl.p.kv_layout == VATT_LAYOUT_PAGED ? launch_window_f<D, FMT, true>(A, st) : launch_window_f<D, FMT, false>(A, st);
 }
 template <int D>
 hipError_t launch_window_p(const Plan& pl, const AttendArgs& A, hipStream_t st) {
@@ -40,19 +40,25 @@ hipError_t launch_window_p(const Plan& pl, const AttendArgs& A, hipStream_t st) 
 
 namespace {
 
-// Workgroups that share out the tokens of a sequence.  One of eight waves, which writes the results, for up to 640 tokens (4 and 256, us: 1 x 8K
-// 16.2 -> 11.6, 16 in e4m3 26.8 -> 13.2; 4 and 512 15.6 -> 14.7, 768 15.3 -> 16.3) and where there are jobs for all slots (64 sequences in e4m3, 4 and
-// 2048 72 -> 62).  Else four of four waves, or what two slots per CU take, none with less than a unit of keys per wave (4 and 4096 with 2 / 4 / 8 / 16:
-// 48 sequences in e4m3 89 / 93 / 102 / 116, 24 50 / 44 / 48 / 53, 16 in bf16 51 / 50 / 53 / 55).
-int window_splits(const Plan& pl, int q_len, int64_t longest) {
-  const int vectors = pl.group * q_len, rounds = vectors <= 16 ? 1 : (vectors + 31) / 32;
-  const int64_t jobs = (int64_t)pl.p.batch * pl.p.n_kv_heads * rounds, slots = 2 * pl.num_cus;
-  if (longest <= 640 || (jobs >= slots && longest <= 4608)) return 1;
-  return (int)std::min<int64_t>({std::max<int64_t>(4, (slots + jobs - 1) / jobs), (longest + kUnit * kAttendWaves - 1) / (kUnit * kAttendWaves), kSplitsMax});
+int window_rounds(const Plan& pl, int q_len) { return pl.group * q_len <= 16 ? 1 : (pl.group * q_len + 31) / 32; }
+int64_t window_jobs(const Plan& pl, int q_len) { return (int64_t)pl.p.batch * pl.p.n_kv_heads * window_rounds(pl, q_len); }
+int window_slot_rows(const Plan& pl, int q_len) { return pl.group * q_len <= 16 ? 16 : 32; }
+// Workgroups that the tokens are dealt out to, two to a compute unit, and no more than the merge takes for one job; 0: every job has one of eight
+// waves.  So it is for up to 640 tokens (4 and 256, us, shared by four / alone: 1 x 8K 16.2 / 11.6, 16 in e4m3 26.8 / 13.2; 4 and 512 15.6 / 14.7, 768
+// 15.3 / 16.3), where there are jobs for all slots (64 sequences in e4m3, 4 and 2048 72 / 62), and with more sequences than a wave looks through.
+int window_workgroups(const Plan& pl, int q_len, int64_t longest) {
+  const int64_t slots = 2 * pl.num_cus;
+  if (longest <= 640 || (window_jobs(pl, q_len) >= slots && longest <= 4608) || pl.p.batch > kDealtMost) return 0;
+  return (int)std::min<int64_t>(slots, (int64_t)(kSplitsMax - 2) * pl.p.n_kv_heads * window_rounds(pl, q_len));
+}
+// Bytes of the partial sums (a workgroup's share ends inside a job, or a job ends inside a share) and of the jobs' list.
+size_t window_part_bytes(const Plan& pl, int q_len, int workgroups) {
+  const int64_t jobs = window_jobs(pl, q_len);
+  return (size_t)(workgroups + jobs) * window_slot_rows(pl, q_len) * (pl.p.head_dim + 2) * sizeof(float) + jobs * sizeof(int2);
 }
 
 hipError_t launch_rows(const Plan& pl, AttendArgs& A, const void* q, const void* k, const void* v, const int32_t* block_table, int sink,
-                       int window, int splits, void* ws, hipStream_t st) {
+                       int window, int workgroups, void* ws, hipStream_t st) {
   A.q = static_cast<const uint16_t*>(q);
   A.k = static_cast<const unsigned char*>(k);
   A.v = static_cast<const unsigned char*>(v);
@@ -63,11 +69,14 @@ hipError_t launch_rows(const Plan& pl, AttendArgs& A, const void* q, const void*
   A.log2_scale = (float)((double)pl.sm_scale * 1.4426950408889634);
   A.sink = std::min(sink, pl.p.n_max);
   A.window = std::min(window, pl.p.n_max);
-  const int vectors = pl.group * A.q_len;
-  A.rounds = vectors <= 16 ? 1 : (vectors + 31) / 32;
-  A.splits = splits;
+  A.batch = pl.p.batch;
+  A.rounds = window_rounds(pl, A.q_len);
+  A.slot_rows = window_slot_rows(pl, A.q_len);
+  A.workgroups = workgroups;
   A.part = static_cast<float*>(ws);
-  A.part_ml = reinterpret_cast<float2*>(A.part + (int64_t)pl.p.batch * A.q_len * A.Hq * A.splits * pl.p.head_dim);
+  A.slots = (int)(workgroups + window_jobs(pl, A.q_len));
+  A.part_ml = reinterpret_cast<float2*>(A.part + (int64_t)A.slots * A.slot_rows * pl.p.head_dim);
+  A.jobs = reinterpret_cast<int2*>(A.part_ml + (int64_t)A.slots * A.slot_rows);
   return pl.p.head_dim == 128 ? launch_window_p<128>(pl, A, st) : launch_window_p<64>(pl, A, st);
 }
 
@@ -81,16 +90,19 @@ hipError_t launch_window(const Plan& pl, const void* q, const void* k, const voi
   A.q_stride = (int64_t)pl.p.n_q_heads * pl.p.head_dim;
   A.out_o = out_o;
   A.out_lse = out_lse;
-  // (whole groups of 8 at both ends of the window; the partial sums fit the workspace)
+  // (whole groups of 8 at both ends of the window)
   const int64_t longest = std::min<int64_t>(pl.p.n_max, (int64_t)std::min(sink, pl.p.n_max) + std::min(window, pl.p.n_max) + pl.q_len + 14);
-  const int64_t fit = pl.ws_bytes / ((int64_t)pl.vbatch * pl.p.n_q_heads * (pl.p.head_dim + 2) * sizeof(float));
-  const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(window_splits(pl, pl.q_len, longest), fit));
-  return launch_rows(pl, A, q, k, v, block_table, sink, window, splits, ws, st);
+  int workgroups = window_workgroups(pl, pl.q_len, longest);
+  if (window_part_bytes(pl, pl.q_len, workgroups) > pl.ws_bytes) {  // as many as there is room for
+    const int64_t least = (int64_t)window_part_bytes(pl, pl.q_len, 0), one = (int64_t)window_part_bytes(pl, pl.q_len, 1) - least;
+    workgroups = (int)std::max<int64_t>(((int64_t)pl.ws_bytes - least) / one, 0);
+  }
+  return launch_rows(pl, A, q, k, v, block_table, sink, window, workgroups, ws, st);
 }
 
 size_t few_workspace_bytes(const Plan& pl, int n_new) {
-  const int splits = window_splits(pl, n_new, pl.p.n_max);  // (a window leaves no more)
-  return splits == 1 ? 0 : (size_t)pl.p.batch * n_new * pl.p.n_q_heads * splits * (pl.p.head_dim + 2) * sizeof(float);
+  const int workgroups = window_workgroups(pl, n_new, pl.p.n_max);  // (a window leaves no more)
+  return workgroups == 0 ? 0 : window_part_bytes(pl, n_new, workgroups);
 }
 
 hipError_t launch_few(const Plan& pl, const void* q, int64_t q_stride, int n_new, const int32_t* first, const int32_t* new_lens, const void* k,
@@ -105,8 +117,8 @@ hipError_t launch_few(const Plan& pl, const void* q, int64_t q_stride, int n_new
   A.out_lse = out_lse;
   A.out_bf16 = bf16;
   const int64_t seen = window > 0 ? (int64_t)std::min(sink, pl.p.n_max) + std::min(window, pl.p.n_max) + n_new + 14 : pl.p.n_max;
-  const int splits = window_splits(pl, n_new, std::min<int64_t>(pl.p.n_max, seen));
-  return launch_rows(pl, A, q, k, v, block_table, window > 0 ? sink : 0, window > 0 ? window : pl.p.n_max, splits, ws, st);
+  const int workgroups = window_workgroups(pl, n_new, std::min<int64_t>(pl.p.n_max, seen));
+  return launch_rows(pl, A, q, k, v, block_table, window > 0 ? sink : 0, window > 0 ? window : pl.p.n_max, workgroups, ws, st);
 }
 
 }  // namespace vatt

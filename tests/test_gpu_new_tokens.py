@@ -255,6 +255,11 @@ SHARED = [
     # the same sizes with few new tokens: the kernel of the decode steps, in several workgroups
     (1, 4, 1, 128, 4000, 16, 0, 8, [3991], None, 0, 0), (3, 4, 2, 64, 6000, 0, 1, 3, [5960, 100, 3], [2, 3, 0], 0, 0),
     (2, 8, 1, 128, 3500, 64, 2, 4, [3430, 900], [4, 3], 300, 2500), (2, 1, 1, 64, 5001, 0, 0, 17, [4984, 17], None, 0, 0),
+    # ... of which some have none, dealt out over several waves' lanes, and more than there are threads
+    (70, 4, 2, 64, 900, 16, 1, 2, [(i * 137) % 930 - 10 for i in range(70)], [i % 3 for i in range(70)], 0, 0),
+    (200, 2, 1, 64, 700, 0, 0, 1, [(i * 37) % 700 for i in range(200)], None, 0, 0), (270, 2, 1, 64, 700, 0, 2, 1, [(i * 37) % 700 for i in range(270)], None, 5, 660),
+    (3, 4, 1, 128, 1000, 0, 0, 1, [-1, 1000, 999], None, 0, 0), (2, 4, 1, 128, 1000, 0, 0, 1, [500, 999], [0, 0], 0, 0),
+    (1, 4, 1, 128, 1000, 0, 0, 2, [500], [0], 0, 0),
     # more sequences than a wave has lanes, and than it looks through
     (130, 2, 2, 64, 96, 16, 0, 33, [(i * 37) % 90 for i in range(130)], [(i * 5) % 34 for i in range(130)], 0, 0),
     (300, 4, 1, 64, 64, 0, 1, 20, [(i * 37) % 60 - 1 for i in range(300)], [(i * 7) % 21 for i in range(300)], 2, 9),
@@ -301,6 +306,9 @@ WINDOWS = [
     (2, 4, 1, 128, 3000, 16, 1, 1, [3000, 700], 128, 1000), (2, 8, 1, 64, 3000, 0, 2, 1, [2999, 5], 0, 2000), (1, 8, 2, 128, 2500, 64, 0, 2, [2500], 300, 900),
     (2, 4, 2, 64, 2000, 0, 0, 11, [2000, 1300], 37, 700), (1, 2, 2, 128, 2000, 8, 2, 3, [1999], 5, 1500), (2, 4, 4, 64, 1500, 0, 1, 7, [1500, 3], 0, 1 << 30),
     (70, 8, 8, 64, 700, 0, 0, 1, [1 + (i * 137) % 700 for i in range(70)], 9, 690),
+    # ... dealt out over sequences of several waves' lanes, and more than there are threads
+    (40, 4, 4, 64, 700, 0, 1, 1, [1 + (i * 137) % 700 for i in range(40)], 9, 690), (200, 2, 1, 64, 800, 16, 0, 1, [1 + (i * 317) % 800 for i in range(200)], 0, 700),
+    (300, 2, 2, 64, 800, 0, 2, 1, [1 + (i * 317) % 800 for i in range(300)], 3, 650), (5, 4, 1, 128, 2000, 64, 0, 9, [1999, 9, 2000, 700, 1], 40, 1300),
 ]
 
 
