@@ -699,7 +699,7 @@ struct DealtSeq {
 struct Deal {
   const DealtSeq* seqs;
   int of_wave[kAttendWaves], total;  // chunks of a wave's sequences, and of all, of one KV head and set of vectors
-  int share, more;                   // the first `more` workgroups have share + 1
+  int share;                         // chunks of a workgroup; the last ones may have less, or nothing
   QueryTokens only;                  // of a batch of one, which needs no list
   __device__ __forceinline__ static int chunks_of(const AttendArgs& A, const QueryTokens& T) {
     constexpr int kChunk = 4 * kAttendWaves;
@@ -733,15 +733,12 @@ struct Deal {
         total += of_wave[w];
       }
     }
-    const int all = total * A.Hkv * A.rounds, workgroups = max(min(A.workgroups, all), 1);
-    share = all / workgroups;
-    more = all - share * workgroups;
+    // Rounded up: no share is smaller than all / workgroups, so that a job, `total` chunks at most, lies in at most workgroups / (Hkv * rounds) + 2
+    // of them, which the merge can take.
+    share = (total * A.Hkv * A.rounds + A.workgroups - 1) / A.workgroups;
   }
-  __device__ __forceinline__ int begin(int w) const { return w * share + min(w, more); }
-  __device__ __forceinline__ int owner(int x) const {
-    const int longer = more * (share + 1);
-    return x < longer ? x / (share + 1) : more + (x - longer) / max(share, 1);
-  }
+  __device__ __forceinline__ int begin(int w) const { return w * share; }
+  __device__ __forceinline__ int owner(int x) const { return x / share; }
   struct Seq {
     int b, from, n;  // its first chunk, and how many
     QueryTokens queries;

@@ -260,6 +260,8 @@ SHARED = [
     (200, 2, 1, 64, 700, 0, 0, 1, [(i * 37) % 700 for i in range(200)], None, 0, 0), (270, 2, 1, 64, 700, 0, 2, 1, [(i * 37) % 700 for i in range(270)], None, 5, 660),
     (3, 4, 1, 128, 1000, 0, 0, 1, [-1, 1000, 999], None, 0, 0), (2, 4, 1, 128, 1000, 0, 0, 1, [500, 999], [0, 0], 0, 0),
     (1, 4, 1, 128, 1000, 0, 0, 2, [500], [0], 0, 0),
+    # ... four KV heads with 202 and 239 pieces of 128 tokens each, for 504 workgroups: shares of two pieces, one head in 102 to 121 of them
+    (1, 4, 4, 64, 25856, 16, 1, 1, [25855], None, 0, 0), (1, 4, 4, 64, 30600, 0, 0, 1, [30591], None, 0, 0),
     # more sequences than a wave has lanes, and than it looks through
     (130, 2, 2, 64, 96, 16, 0, 33, [(i * 37) % 90 for i in range(130)], [(i * 5) % 34 for i in range(130)], 0, 0),
     (300, 4, 1, 64, 64, 0, 1, 20, [(i * 37) % 60 - 1 for i in range(300)], [(i * 7) % 21 for i in range(300)], 2, 9),
@@ -308,7 +310,7 @@ WINDOWS = [
     (70, 8, 8, 64, 700, 0, 0, 1, [1 + (i * 137) % 700 for i in range(70)], 9, 690),
     # ... dealt out over sequences of several waves' lanes, and more than there are threads
     (40, 4, 4, 64, 700, 0, 1, 1, [1 + (i * 137) % 700 for i in range(40)], 9, 690), (200, 2, 1, 64, 800, 16, 0, 1, [1 + (i * 317) % 800 for i in range(200)], 0, 700),
-    (300, 2, 2, 64, 800, 0, 2, 1, [1 + (i * 317) % 800 for i in range(300)], 3, 650), (5, 4, 1, 128, 2000, 64, 0, 9, [1999, 9, 2000, 700, 1], 40, 1300),
+    (300, 2, 2, 64, 800, 0, 2, 1, [1 + (i * 317) % 800 for i in range(300)], 3, 650), (1, 4, 4, 64, 30600, 16, 2, 1, [30600], 100, 25700), (5, 4, 1, 128, 2000, 64, 0, 9, [1999, 9, 2000, 700, 1], 40, 1300),
 ]
 
 
