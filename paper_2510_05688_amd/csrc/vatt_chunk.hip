@@ -333,14 +333,22 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& A, int g_shift, Work&
 }
 
 // Rows of a KV head: row r is query token r / G, head r % G of the group.  A workgroup takes 128 of them, a wave 32, over the key tiles
-// of its split; the tiles go through LDS in bf16, the next one on its way in registers.
+// of its piece; the tiles go through LDS in bf16, two of K and two of V: while one is worked on, bf16 rows of the next one come straight into the
+// other and codes into registers.
 //   S^T [keys x rows] = K Q^T   and   O^T [d x rows] += V^T P^T,   P = exp(S - m),
 // v_mfma_f32_32x32x16_bf16 (operand lane l: row or column l % 32, eight inner elements of half l / 32; result lane l: column l % 32,
 // rows 8 (i / 4) + 4 (l / 32) + i % 4).  A row's scores lie in two lanes, and are the operand of the second product as they come when
 // its inner elements j of half h are keys 4 h + j and 8 + 4 h + j - 4; V comes out of LDS transposed.
 // TERMS 1 (output in bf16): P rounded to bf16, as the output is.  TERMS 3 (output in 32 bits): P as three bf16 terms that add up to the
 // fp32 value.  The sums of P are of the unrounded values.
-// The running maximum of a row moves only when a score passes it by more than kLazy.
+// The running maximum of a row moves only when a score passes it by more than kLazy (the sums are then at most 2^8 times larger, and fp32 has
+// 2^127), so that the results so far are seldom multiplied.
+// Bound by the matrix cores and the vector instructions beside them, at the clock that the power allows: 2048 tokens on 64K (group of 4, d 128,
+// bf16) 2.02 ms, 1070 TFLOP/s of the 1253 that a large product reaches; the matrix cores are busy for 67 % of the cycles, no LDS bank conflicts.
+// A tile of 64 keys takes a workgroup of a full compute unit 2 us (e4m3 2.2, output in 32 bits with d 64 2.5).
+// 128 rows, since each row of K and V read from LDS then serves 32 rows of a wave and each loaded one 128; two workgroups per unit, since one's
+// barriers are then the other's time (64 KB of LDS each).  The second product is made one tile late, so that the weights' exponentials have matrix
+// instructions to run beside (2.38 -> 2.02 ms with the loads straight to LDS).
 template <int D, int FMT, bool PAGED, int TERMS>
 __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   constexpr int S = D / 16;                        // steps of the first product
@@ -703,7 +711,8 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   }
 }
 
-// The pieces' partial sums together: a wave per row, and every fourth row of a tile that was cut.
+// The pieces' partial sums together, a row per wave at a time; the rows of a tile go round the workgroups of its pieces.  Bound by three dependent
+// reads (the lengths, a row's maxima, its sums), 4 us; 10 where 33 tokens on 5K - 16K are cut into 236 pieces (16 MB).
 template <int D, bool BF16>
 __global__ __launch_bounds__(kChunkThreads) void chunk_merge_kernel(ChunkArgs A) {
   constexpr int C = D / kWave, kAhead = 8;
@@ -765,19 +774,22 @@ int64_t chunk_tiles(const Plan& pl, int n_new) {
   return (int64_t)pl.p.batch * pl.p.n_kv_heads * (((int64_t)n_new * pl.group + kTileRows - 1) / kTileRows);
 }
 int chunk_slots(const Plan& pl) { return 2 * pl.num_cus; }
-// Whether pieces can be wanted at all (the rule of Cut).  Of a batch, or where fewer new tokens may count, the host knows too little.
-bool chunk_may_cut(const Plan& pl, int n_new) {
-  const double longest = (pl.p.n_max + kTileKeys - 1) / kTileKeys, own = (double)n_new / kTileKeys;
+// Whether pieces can be wanted at all (the rule of Cut) for queries that see up to `keys` tokens; the merge is launched only then.  Of a batch the
+// host knows too little.  fewer: fewer than n_new tokens may count.  Then every length can be wanted in pieces, and the launch for it, 2 to 15 us, is
+// worth it beyond 32 key tiles (64 of 2048 tokens count, us in whole tiles / in pieces: on 4K 72 / 24, on 64K 1033 / 99; where all 4096 of a prompt
+// count 165 / 167).
+bool chunk_may_cut(const Plan& pl, int n_new, bool fewer, int64_t keys) {
+  const double longest = (double)((keys + kTileKeys - 1) / kTileKeys), own = std::min((double)n_new / kTileKeys, longest);
   if (pl.p.batch > kSeqsMax || longest <= 12) return false;
-  if (pl.p.batch > 1) return true;
+  if (pl.p.batch > 1 || (fewer && longest > 32)) return true;
   // one sequence: its new tokens at the end of the capacity, or at its beginning (the rule is linear in between)
   const double tiles = (double)chunk_tiles(pl, n_new) / chunk_slots(pl);
   return longest > 1.25 * tiles * (longest - own / 2) + 12 || own > 1.25 * tiles * own / 2 + 12;
 }
 // Pieces at most: a sequence's tiles are cut into two or more where they are one and a half pieces long, and all tiles at their longest have no more
 // than a piece for every slot, so that the rounding adds a third.
-int64_t chunk_pieces(const Plan& pl, int n_new) {
-  if (!chunk_may_cut(pl, n_new)) return 0;
+int64_t chunk_pieces(const Plan& pl, int n_new, bool fewer, int64_t keys) {
+  if (!chunk_may_cut(pl, n_new, fewer, keys)) return 0;
   const int64_t longest = (pl.p.n_max + kTileKeys - 1) / kTileKeys, each = std::min<int64_t>((longest + kPieceLeast - 1) / kPieceLeast, kPiecesMax);
   return std::min<int64_t>(2 * chunk_slots(pl), chunk_tiles(pl, n_new) * each);
 }
@@ -821,7 +833,7 @@ bool chunk_fits(const Plan& pl, int n_new) {
 
 size_t chunk_workspace_bytes(const Plan& pl, int n_new) {
   if (chunk_is_few(pl, n_new)) return few_workspace_bytes(pl, n_new);
-  return (size_t)chunk_pieces(pl, n_new) * kTileRows * (pl.p.head_dim + 2) * sizeof(float);
+  return (size_t)chunk_pieces(pl, n_new, true, pl.p.n_max) * kTileRows * (pl.p.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_chunk(const Plan& pl, const void* q, int64_t q_stride, int n_new, const int32_t* first, const int32_t* new_lens, const void* k,
@@ -845,12 +857,15 @@ hipError_t launch_chunk(const Plan& pl, const void* q, int64_t q_stride, int n_n
   A.Hkv = pl.p.n_kv_heads;
   A.n_new = n_new;
   A.slots = chunk_slots(pl);
-  A.room = (int)(chunk_pieces(pl, n_new) / A.Hkv);
   A.sink = std::min(sink, pl.p.n_max);
   A.window = std::min(window, pl.p.n_max);
+  // (a window: its tiles and those of the first tokens, of which one more may be begun each, and those of a tile of rows)
+  const int64_t seen = (int64_t)A.sink + A.window + kTileRows / pl.group + 2 * kTileKeys;
+  const int64_t pieces = chunk_pieces(pl, n_new, new_lens != nullptr, A.window > 0 ? std::min<int64_t>(pl.p.n_max, seen) : pl.p.n_max);
+  A.room = (int)(pieces / A.Hkv);
   A.log2_scale = (float)((double)pl.sm_scale * 1.4426950408889634);
   A.part = static_cast<float*>(ws);
-  A.part_ml = reinterpret_cast<float2*>(A.part + (size_t)chunk_pieces(pl, n_new) * kTileRows * pl.p.head_dim);
+  A.part_ml = reinterpret_cast<float2*>(A.part + (size_t)pieces * kTileRows * pl.p.head_dim);
   return pl.p.head_dim == 128 ? launch_chunk_d<128>(pl, A, bf16, st) : launch_chunk_d<64>(pl, A, bf16, st);
 }
 

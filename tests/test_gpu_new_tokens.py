@@ -166,6 +166,57 @@ def test_a_cache_in_host_memory(page):
     assert all(torch.equal(a, b) for a, b in zip(*res))
 
 
+class Large(Setup):
+    """A cache of more than 4 GiB per buffer of which the last sequence (contiguous) or the last pages hold what small's first one does."""
+
+    def __init__(self, small, batch, n_max, blocks):
+        self.vb, self.rng, self.hq, self.hkv, self.d, self.fmt, self.page, self.q_len = small.vb, small.rng, small.hq, small.hkv, small.d, small.fmt, small.page, 1
+        self.batch, self.n_max = batch, n_max
+        self.params = dict(small.params, batch=batch, n_max=n_max, num_blocks=blocks)
+        self.plan = self.vb.vatt_plan_create_chunk(self.params, 1, 0)
+        self.vb.vatt_plan_set_option(self.plan, self.vb.VATT_OPT_KV_FORMAT, self.fmt)
+        self.ws = torch.empty(self.vb.vatt_plan_workspace_bytes(self.plan), dtype=torch.uint8, device="cuda")
+        self.table = small.table + (blocks - small.pages) if self.page else None
+        row, ends = {0: 2 * self.d, 1: self.d, 2: self.d // 2}[self.fmt], self.d // 32
+        for name in "kv":
+            big = torch.zeros(self.vb.vatt_kv_cache_bytes(self.plan), dtype=torch.uint8, device="cuda")
+            assert big.numel() > 1 << 32
+            for x, s in ((big, self), (getattr(small, name), small)):
+                off = self.vb.vatt_kv_scale_offset(s.plan)
+                n8 = (s.n_max + 7) // 8 * 8
+                shape = (s.pages if s is small else blocks, s.hkv, s.page) if s.page else (s.batch, s.hkv, s.n_max)
+                scales = shape if s.page else (s.batch, s.hkv, n8)
+                views = [x[:math.prod(shape) * row].view(*shape, row)]
+                if self.fmt:
+                    views.append(x[off:off + math.prod(scales) * ends].view(*scales, ends))
+                if s is self:
+                    into = views
+            for a, b in zip(into, views):
+                if self.page:
+                    a[-small.pages:] = b
+                else:
+                    a[-1, :, :b.shape[2]] = b[0]
+            setattr(self, name, big)
+
+
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("fmt", [0, 1, 2])
+def test_offsets_beyond_32_bits(fmt, page):
+    s = Setup(1, 4, 2, 128, 600, page, fmt, None, seed=21)
+    batch = 1 if page else (60, 104, 208)[fmt]
+    big = Large(s, batch, 600 if page else 170752, (600000, 1100000, 2200000)[fmt] if page else 0)
+    for n_new, bf16, sink, window in ((3, False, 0, 0), (70, True, 0, 0), (70, False, 5, 300)):
+        q = torch.zeros(batch, n_new, 4, 128, dtype=torch.bfloat16, device="cuda")
+        q[-1] = _bf16(s.rng.normal(size=(n_new, 4, 128)))
+        o, lse = _chunk(big, q, [-1] * (batch - 1) + [600 - n_new], None, sink, window, bf16)
+        _check_rows(s, q[-1:], [list(range(600 - n_new, 600))], sink, window, o[-1:], lse[-1:], bf16)
+    q = torch.zeros(batch, 1, 4, 128, dtype=torch.bfloat16, device="cuda")
+    q[-1] = _bf16(s.rng.normal(size=(1, 4, 128)))
+    for sink, window in ((3, 200), (0, 900)):
+        o, lse = _window(big, q, [1] * (batch - 1) + [600], sink, window)
+        _check_rows(s, q[-1:], [[599]], sink, window, o[-1:], lse[-1:], False)
+
+
 @pytest.mark.parametrize("scale", [0.01, 3.0])
 @pytest.mark.parametrize("fmt", [0, 2])
 def test_chunk_with_another_scale(scale, fmt):

@@ -43,15 +43,19 @@ def test_workspace_of_chunks():
     plan = _plan()
     assert [vb.vatt_chunk_workspace_bytes(plan, n) for n in (0, -1, 1001)] == [0, 0, 0]
     few = vb.vatt_chunk_workspace_bytes(plan, 1)
-    assert few > 0 and few % (2 * 8 * (128 + 2) * 4) == 0  # whole partial sums for every output row
+    # sums of 16 vectors for 126 workgroups per KV head and the 4 jobs (sequence, KV head), and the jobs' list
+    assert few == (126 * 2 + 4) * 16 * (128 + 2) * 4 + 4 * 8
     many = vb.vatt_chunk_workspace_bytes(plan, 500)
     assert many > 0 and many % (128 * (128 + 2) * 4) == 0  # of whole tiles of 128 rows
     vb.vatt_plan_destroy(plan)
     short = _plan(n_max=640)  # nothing to share out: one workgroup has all keys of its rows
     assert [vb.vatt_chunk_workspace_bytes(short, n) for n in (1, 8, 9, 640)] == [0, 0, 0, 0]
     vb.vatt_plan_destroy(short)
-    one = _plan(batch=1, n_kv_heads=8, n_max=65536, n_q_heads=32)  # tiles for all compute units, or for a few
+    one = _plan(batch=1, n_kv_heads=8, n_max=2048, n_q_heads=32)  # tiles for all compute units, or for a few
     assert vb.vatt_chunk_workspace_bytes(one, 2048) == 0 and vb.vatt_chunk_workspace_bytes(one, 64) > 0
+    vb.vatt_plan_destroy(one)
+    one = _plan(batch=1, n_kv_heads=8, n_max=65536, n_q_heads=32)  # of many new tokens a few may count
+    assert vb.vatt_chunk_workspace_bytes(one, 2048) > 0
     vb.vatt_plan_destroy(one)
 
 
