@@ -24,7 +24,7 @@ def _chunk(s, q, first, new, sink, window, bf16, stride=None, lse=True):
     o = torch.full((batch, n_new, s.hq, s.d), FILL, dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda")
     out_lse = torch.full((batch, n_new, s.hq), FILL, device="cuda") if lse else None
     need = s.vb.vatt_chunk_workspace_bytes(s.plan, n_new)
-    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda") if need else None  # (NaN, in whatever way it is read)
     s.vb.vatt_chunk_attend(s.plan, q, stride or s.vb.token_stride(q), n_new, s.ints(first), None if new is None else s.ints(new), s.k, s.v, s.table,
                            sink, window, ws, s.vb.VATT_OUT_BF16 if bf16 else s.vb.VATT_OUT_F32, o, out_lse, _stream())
     torch.cuda.synchronize()
@@ -368,6 +368,7 @@ WINDOWS = [
 def _window(s, q, lens, sink, window, lse=True):
     o = torch.full((s.batch, s.q_len, s.hq, s.d), FILL, device="cuda")
     out_lse = torch.full((s.batch, s.q_len, s.hq), FILL, device="cuda") if lse else None
+    s.ws.fill_(255)
     s.vb.vatt_window_decode(s.plan, q, s.k, s.v, s.table, s.ints(lens), sink, window, s.ws, o, out_lse, _stream())
     torch.cuda.synchronize()
     return o, out_lse
@@ -527,6 +528,60 @@ def test_another_stream():
             res.append([*_chunk(s, q, [400, 3], [70, 50], 0, 0, True), *_window(s, one, [470, 53], 4, 50)])
         stream.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
+def test_calls_at_once():
+    """Calls of one plan under way on two streams, each with its own workspace: what each gives alone."""
+    s = Setup(2, 8, 2, 128, 4000, 16, 1, None, seed=22)
+    q = [_bf16(s.rng.normal(size=(2, n, 8, 128))) for n in (40, 3)]
+    firsts = [s.ints([3900, 1200]), s.ints([3990, 2100])]
+    lens = s.ints([4000, 2500])
+
+    def calls(i, o, ws, st):
+        s.vb.vatt_chunk_attend(s.plan, q[i], 8 * 128, q[i].shape[1], firsts[i], None, s.k, s.v, s.table, 0, 0, ws[0], s.vb.VATT_OUT_F32, o[0], o[1], st)
+        s.vb.vatt_window_decode(s.plan, q[i], s.k, s.v, s.table, lens, 9, 900 + i, ws[1], o[2], o[3], st)
+
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[[torch.zeros(2, x.shape[1], 8, 128, device="cuda"), torch.zeros(2, x.shape[1], 8, device="cuda"), torch.zeros(2, 8, 128, device="cuda"),
+              torch.zeros(2, 8, device="cuda")] for x in q] for _ in range(2)]
+    ws = [[torch.empty(s.vb.vatt_chunk_workspace_bytes(s.plan, x.shape[1]), dtype=torch.uint8, device="cuda"), torch.empty_like(s.ws)] for x in q]
+    torch.cuda.synchronize()
+    for i in range(2):
+        calls(i, outs[0][i], ws[i], _stream())
+        torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            calls(i, outs[1][i], ws[i], sides[i].cuda_stream)
+    torch.cuda.synchronize()
+    for a, b in zip(outs[0], outs[1]):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("n_new", [2, 40])
+def test_as_many_sequences_as_a_plan_takes(n_new):
+    s = Setup(65535, 1, 1, 64, 48, 0, 0, None, seed=23)
+    q = torch.randn(65535, n_new, 1, 64, device="cuda", generator=torch.Generator("cuda").manual_seed(3)).to(torch.bfloat16)
+    first = torch.arange(65535, device="cuda", dtype=torch.int32) * 7 % (49 - n_new)
+    o, lse = torch.zeros(q.shape, device="cuda"), torch.zeros(q.shape[:3], device="cuda")
+    need = s.vb.vatt_chunk_workspace_bytes(s.plan, n_new)
+    assert need == 0
+    s.vb.vatt_chunk_attend(s.plan, q, 64, n_new, first, None, s.k, s.v, None, 3, 30, None, s.vb.VATT_OUT_F32, o, lse, _stream())
+    wo, wlse = torch.zeros(65535, 1, 64, device="cuda"), torch.zeros(65535, 1, device="cuda")
+    one, lens = q[:, 0].contiguous(), first + 1
+    s.vb.vatt_window_decode(s.plan, one, s.k, s.v, None, lens, 3, 30, s.ws, wo, wlse, _stream())
+    torch.cuda.synchronize()
+    for b0 in range(0, 65535, 8192):
+        b = slice(b0, b0 + 8192)
+        k, v = (x.view(torch.bfloat16).view(65535, 48, 64)[b].double().cpu() for x in (s.k, s.v))
+        p = (first[b, None] + torch.arange(n_new, device="cuda")).cpu()[..., None]
+        i = torch.arange(48)
+        x = torch.bmm(q[b, :, 0].double().cpu(), k.transpose(1, 2).contiguous()) / 8
+        x = x.masked_fill(~((i <= p) & ((i < 3) | (i > p - 30))), -INF)
+        want, ln = torch.bmm(x.softmax(-1), v), x.logsumexp(-1)
+        for got, exp in ((o[b, :, 0], want), (wo[b], want[:, :1])):
+            assert ((got.double().cpu() - exp).norm(dim=-1) <= 2e-5 * exp.norm(dim=-1)).all(), b0
+        for got, exp in ((lse[b, :, 0], ln), (wlse[b], ln[:, :1])):
+            assert ((got.double().cpu() - exp).abs() <= 2e-5 * exp.abs().clamp(min=1)).all(), b0
 
 
 @pytest.mark.parametrize("fmt", [0, 1])
