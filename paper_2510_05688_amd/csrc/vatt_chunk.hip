@@ -18,7 +18,9 @@ static_assert(kTileRows == kWaveRows * kChunkWaves, "32 rows of every wave");
 constexpr int kTileKeys = 64;
 constexpr int kPiecesMax = 64;      // pieces that a tile's keys are cut into at most
 constexpr int kPieceLeast = 4;      // key tiles of a piece at least
+constexpr int kRestLeast = 24;      // key tiles of a tile that is cut because it is over
 constexpr float kOnePerUnit = 5000.f;  // key tiles in all below which there is one piece per compute unit, not two
+constexpr int kSteps = 8;           // of a tile's level, for the order (a power of two)
 constexpr int kSeqsPerLane = 4, kSeqsMax = kSeqsPerLane * kWave;  // sequences that a wave looks through for its work
 
 struct ChunkArgs {
@@ -73,7 +75,7 @@ __device__ __forceinline__ uint64_t ones(int n) { return n >= 64 ? ~0ull : n <= 
 
 // What a workgroup does: a tile of rows of one sequence and KV head, over one of `pieces` parts of its keys.
 struct Work {
-  int b, kvh, tile, piece, pieces, slot;  // slot: the piece's place in the workspace
+  int b, kvh, tile, piece, pieces, slot;  // slot: the piece's place in the workspace, for one KV head
 };
 
 // Pieces that the tiles of sequences are cut into.  total: key tiles of all tiles of one KV head, most: if each had as many as its sequence's last one.
@@ -84,13 +86,44 @@ struct Work {
 // (32-bit values, rounded the same way wherever this is worked out.)
 struct Cut {
   float piece;  // key tiles; 0: nothing is cut
+  float up = 0.5f;
   __device__ __forceinline__ Cut(const ChunkArgs& A, float total, float most, int longest) {
 #pragma clang fp contract(off)
     const float share = total * A.Hkv / A.slots;
     const float at_once = 0.97f * (most * A.Hkv < kOnePerUnit ? A.slots / 2 : A.slots);
     piece = A.room > 0 && longest > 1.25f * share + 12.f ? fmaxf(most * A.Hkv / at_once, (float)kPieceLeast) : 0.f;
   }
-  __device__ __forceinline__ int pieces(int last) const { return piece == 0.f ? 1 : max(min((int)(last / piece + 0.5f), kPiecesMax), 1); }
+  __device__ __forceinline__ int pieces(int last) const { return piece == 0.f ? 1 : max(min((int)(last / piece + up), kPiecesMax), 1); }
+  // `cut` pieces of one KV head: where a few too many for the slots would wait for all others, twice as many of half the length, rounded down (700
+  // new tokens on 32K, 176 tiles: three pieces each 490 us, five 420).
+  __device__ __forceinline__ bool finer(const ChunkArgs& A, int cut) {
+    if (cut * A.Hkv <= A.slots) return false;
+    piece *= 0.5f;
+    up = 0.f;
+    return true;
+  }
+};
+
+// Where nothing is long beside everybody's share, but the tiles leave a rest when the slots have been filled as often as they can be: the tiles of the
+// rest, the last in the order, in equally many pieces each, which fill the slots once or twice.  shortest: key tiles of the shortest tile.
+struct Rest {
+  int whole, pieces;  // tiles of a KV head before the rest
+  __device__ __forceinline__ Rest(const ChunkArgs& A, int count, int shortest) : whole(count), pieces(1) {
+    const int all = count * A.Hkv;
+    if (A.room == 0 || shortest < kRestLeast || all <= A.slots) return;
+    const int before = all / A.slots * A.slots / A.Hkv, rest = (count - before) * A.Hkv;
+    if (rest == 0) return;
+    // in units of a key tile of a workgroup that shares its unit: one alone takes two thirds; a piece costs 3 more, the join 6 per filling
+    const int most = min(shortest / kPieceLeast, kPiecesMax), once = min(A.slots / rest, most), twice = min(2 * A.slots / rest, most);
+    float least = 2 * rest <= A.slots ? 0.65f * shortest : (float)shortest;
+    const float a = (float)shortest / (float)max(once, 1) + 11.f, b = 2.f * (float)shortest / (float)max(twice, 1) + 20.f;
+    if (once > 1 && a < least) {
+      least = a;
+      pieces = once;
+    }
+    if (twice > 1 && b < least) pieces = twice;
+    if (pieces > 1) whole = before;
+  }
 };
 
 // A sequence's tiles: how many, and the key tiles of the first and the last one.
@@ -115,13 +148,14 @@ __device__ __forceinline__ int order(const ChunkArgs& A, int y, int count) {
 // first: what a tile costs goes by its place in the sequence, counted in tiles (its level).
 struct Batch {
   int tiles[kSeqsPerLane], pieces[kSeqsPerLane], level[kSeqsPerLane];
-  int cut;  // pieces of one KV head in all
+  int cut;    // pieces of one KV head in all
+  int whole, rest;  // tiles that are not cut, and pieces of each of the others (1: there are none)
 
   __device__ __forceinline__ void read(const ChunkArgs& A, int g_shift) {
     const int lane = threadIdx.x & 63;
     int last[kSeqsPerLane];
-    float total = 0.f, most = 0.f;
-    int longest = 0;
+    float total = 0.f, most = 0.f, shortest = 1e9f;
+    int longest = 0, count = 0;
 #pragma unroll
     for (int i = 0; i < kSeqsPerLane; ++i) {
       const int b = lane + i * kWave;
@@ -136,19 +170,35 @@ struct Batch {
         total += 0.5f * (float)(t.tiles * (t.first + t.last));
         most += (float)(t.tiles * t.last);
         longest = max(longest, t.last);
+        count += t.tiles;
+        if (t.tiles > 0) shortest = fminf(shortest, (float)t.first);
       }
     }
     cut = 0;
+    whole = INT32_MAX;
+    rest = 1;
     if (A.room == 0) return;
-    const Cut c(A, wave_sum_f32(total), wave_sum_f32(most), (int)wave_max((float)longest));
-    if (c.piece == 0.f) return;
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < kSeqsPerLane; ++i) {
-      pieces[i] = c.pieces(last[i]);
-      if (pieces[i] > 1) n += tiles[i] * pieces[i];
+    Cut c(A, wave_sum_f32(total), wave_sum_f32(most), (int)wave_max((float)longest));
+    if (c.piece == 0.f) {
+      const Rest r(A, wave_total(count), (int)-wave_max(-shortest));
+      if (r.pieces > 1) {
+        whole = r.whole;
+        rest = r.pieces;
+        cut = (wave_total(count) - whole) * rest;
+      }
+      return;
     }
-    cut = wave_total(n);
+    auto cut_all = [&]() __attribute__((always_inline)) {
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < kSeqsPerLane; ++i) {
+        pieces[i] = c.pieces(last[i]);
+        if (pieces[i] > 1) n += tiles[i] * pieces[i];
+      }
+      cut = wave_total(n);
+    };
+    cut_all();
+    if (c.finer(A, cut)) cut_all();
     if (cut > A.room) {  // (not reached: see chunk_pieces)
       cut = 0;
 #pragma unroll
@@ -164,8 +214,18 @@ struct Batch {
   }
   // Item y of one KV head; false where there is none.
   __device__ __forceinline__ bool find(const ChunkArgs& A, int y, Work& w) const {
-    const int lane = threadIdx.x & 63;
-    if (y < cut) {
+    w.slot = y;
+    w.piece = 0;
+    w.pieces = 1;
+    if (rest > 1) {
+      if (y >= whole) {
+        w.slot = y - whole;
+        w.pieces = rest;
+        y = w.slot / rest;
+        w.piece = w.slot - y * rest;
+        y += whole;
+      }
+    } else if (y < cut) {
       int before = 0;
 #pragma unroll
       for (int i = 0; i < kSeqsPerLane; ++i) {
@@ -182,35 +242,37 @@ struct Batch {
         before = __builtin_amdgcn_readlane(upto, kWave - 1);
       }
       return false;
+    } else {
+      y -= cut;
     }
-    y -= cut;
     int top = 0;
 #pragma unroll
     for (int i = 0; i < kSeqsPerLane; ++i) top = max(top, level[i] + tiles[i]);
-    int lo = 0, hi = (int)wave_max((float)top);  // above(lo) > y >= above(hi)
+    const int step = ((int)wave_max((float)top) + kSteps - 1) / kSteps;
+    int lo = 0, hi = kSteps;  // above(lo * step) > y >= above(hi * step)
     const int count = above(0);
     if (count <= y) return false;
     y = order(A, y, count);
-    while (hi - lo > 1) {
+#pragma unroll
+    for (int x = 1; x < kSteps; x <<= 1) {
       const int mid = (lo + hi) / 2;
-      if (above(mid) > y) lo = mid; else hi = mid;
+      if (above(mid * step) > y) lo = mid; else hi = mid;
     }
-    y -= above(lo + 1);
-    w.piece = 0;
-    w.pieces = 1;
+    y -= above(hi * step);
     int before = 0;
 #pragma unroll
     for (int i = 0; i < kSeqsPerLane; ++i) {
-      const uint64_t there = __ballot(pieces[i] == 1 && level[i] <= lo && lo < level[i] + tiles[i]);
-      const int rank = before + __popcll(there & ((1ull << lane) - 1));
-      const uint64_t hit = __ballot((there >> lane & 1) && rank == y);
+      if (i * kWave >= A.batch) break;
+      const int end = min(level[i] + tiles[i], hi * step), mine = pieces[i] == 1 ? max(end - max(level[i], lo * step), 0) : 0;
+      const int upto = before + (int)wave_inclusive_scan_u32((uint32_t)mine);
+      const uint64_t hit = __ballot(y >= upto - mine && y < upto);
       if (hit) {
-        const int l = __builtin_ctzll(hit);
+        const int l = __builtin_ctzll(hit), last = __builtin_amdgcn_readlane(end - level[i], l) - 1;
         w.b = l + i * kWave;
-        w.tile = lo - __builtin_amdgcn_readlane(level[i], l);
+        w.tile = last - (y - __builtin_amdgcn_readlane(upto - mine, l));
         return true;
       }
-      before += __popcll(there);
+      before = __builtin_amdgcn_readlane(upto, kWave - 1);
     }
     return false;
   }
@@ -304,17 +366,37 @@ __device__ __forceinline__ void row_again(const ChunkArgs& A, int b, int kvh, in
 // This workgroup's work; false where there is none.  Neighbours have the same tile of all KV heads (workgroups go to the XCDs in turn: with a
 // multiple of 8 KV heads a KV head's rows stay in one L2).
 __device__ __forceinline__ bool find_work(const ChunkArgs& A, int g_shift, Work& w) {
-  const int x = blockIdx.x, y = x / A.Hkv;
+  const int x = blockIdx.x;
+  int y = x / A.Hkv;
   w.kvh = x - y * A.Hkv;
-  w.slot = x;
   if (A.batch == 1) {
     const NewTokens n = new_tokens(A, 0);
     const SeqTiles t(A, g_shift, n);
     w.b = 0;
-    w.pieces = Cut(A, 0.5f * (float)(t.tiles * (t.first + t.last)), (float)(t.tiles * t.last), t.last).pieces(t.last);
-    if (w.pieces * t.tiles > A.room) w.pieces = 1;
-    w.tile = w.pieces > 1 ? y / w.pieces : t.tiles - 1 - order(A, y, t.tiles);
-    w.piece = w.pieces > 1 ? y - w.tile * w.pieces : 0;
+    w.slot = y;
+    w.piece = 0;
+    Cut c(A, 0.5f * (float)(t.tiles * (t.first + t.last)), (float)(t.tiles * t.last), t.last);
+    w.pieces = c.pieces(t.last);
+    if (w.pieces > 1) {
+      if (c.finer(A, w.pieces * t.tiles)) w.pieces = c.pieces(t.last);
+      if (w.pieces * t.tiles > A.room) w.pieces = 1;
+    }
+    if (w.pieces > 1) {
+      w.tile = y / w.pieces;
+      w.piece = y - w.tile * w.pieces;
+      return w.tile < t.tiles;
+    }
+    if (c.piece == 0.f) {
+      const Rest r(A, t.tiles, t.first);
+      if (y >= r.whole) {
+        w.slot = y - r.whole;
+        w.pieces = r.pieces;
+        y = w.slot / r.pieces;
+        w.piece = w.slot - y * r.pieces;
+        y += r.whole;
+      }
+    }
+    w.tile = t.tiles - 1 - order(A, y, t.tiles);
     return w.tile >= 0 && w.tile < t.tiles;
   }
   if (A.batch <= kSeqsMax) {
@@ -325,6 +407,7 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& A, int g_shift, Work&
   // too many sequences to look through: tile by tile from the end, beginning with another sequence each time (short sequences leave workgroups
   // without work, and those with work should not all be on the same units)
   const int rank = y / A.batch;
+  w.slot = 0;
   w.b = (y - rank * A.batch + rank) % A.batch;
   w.tile = ((new_tokens(A, w.b).count << g_shift) + kTileRows - 1) / kTileRows - 1 - rank;
   w.piece = 0;
@@ -679,7 +762,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
       }
       if (A.out_lse && half == 0) A.out_lse[out_row] = m_own * 0.69314718055994530942f + logf(l);
     } else {
-      const int64_t place = (int64_t)W.slot * kTileRows + wave * kWaveRows + col;
+      const int64_t place = ((int64_t)W.slot * A.Hkv + kvh) * kTileRows + wave * kWaveRows + col;
 #pragma unroll
       for (int e = 0; e < E; ++e)
 #pragma unroll
@@ -703,7 +786,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
       store_4<BF16>(A.out_o, out_c * D + lane * 8 + 4, a[4] * inv, a[5] * inv, a[6] * inv, a[7] * inv);
       if (A.out_lse && lane == 0) A.out_lse[out_c] = m * 0.69314718055994530942f + logf(ls);
     } else {
-      const int64_t place = (int64_t)W.slot * kTileRows + wave * kWaveRows + c;
+      const int64_t place = ((int64_t)W.slot * A.Hkv + kvh) * kTileRows + wave * kWaveRows + c;
       store_4<false>(A.part, place * D + lane * 8, a[0], a[1], a[2], a[3]);
       store_4<false>(A.part, place * D + lane * 8 + 4, a[4], a[5], a[6], a[7]);
       if (lane == 0) A.part_ml[place] = make_float2(m, ls);
@@ -724,7 +807,7 @@ __global__ __launch_bounds__(kChunkThreads) void chunk_merge_kernel(ChunkArgs A)
   all.read(A, g_shift);
   for (int y = blockIdx.x / A.Hkv; y < all.cut; y += gridDim.x / A.Hkv) {
     Work w;
-    if (!all.find(A, y, w)) return;
+    if (!all.find(A, all.rest > 1 ? all.whole + y : y, w)) return;
     const NewTokens New = new_tokens(A, w.b);
     // (the workgroups of all pieces share out the tile's rows)
     const int n = min((New.count << g_shift) - w.tile * kTileRows, kTileRows);
@@ -782,8 +865,10 @@ bool chunk_may_cut(const Plan& pl, int n_new, bool fewer, int64_t keys) {
   const double longest = (double)((keys + kTileKeys - 1) / kTileKeys), own = std::min((double)n_new / kTileKeys, longest);
   if (pl.p.batch > kSeqsMax || longest <= 12) return false;
   if (pl.p.batch > 1 || (fewer && longest > 32)) return true;
-  // one sequence: its new tokens at the end of the capacity, or at its beginning (the rule is linear in between)
-  const double tiles = (double)chunk_tiles(pl, n_new) / chunk_slots(pl);
+  // one sequence: a rest of tiles behind full slots, of some length; or its new tokens at the end of the capacity, or at its beginning (the rule is linear in between)
+  const int64_t all = chunk_tiles(pl, n_new);
+  if (all > chunk_slots(pl) && all % chunk_slots(pl) != 0 && std::min<int64_t>(pl.p.n_max - n_new, keys) / kTileKeys + 1 >= kRestLeast) return true;
+  const double tiles = (double)all / chunk_slots(pl);
   return longest > 1.25 * tiles * (longest - own / 2) + 12 || own > 1.25 * tiles * own / 2 + 12;
 }
 // Pieces at most: a sequence's tiles are cut into two or more where they are one and a half pieces long, and all tiles at their longest have no more

@@ -313,6 +313,11 @@ SHARED = [
     (1, 4, 1, 128, 1000, 0, 0, 2, [500], [0], 0, 0),
     # ... four KV heads with 202 and 239 pieces of 128 tokens each, for 504 workgroups: shares of two pieces, one head in 102 to 121 of them
     (1, 4, 4, 64, 25856, 16, 1, 1, [25855], None, 0, 0), (1, 4, 4, 64, 30600, 0, 0, 1, [30591], None, 0, 0),
+    # more tiles than run at a time, and a rest that is cut: of one tile per KV head, of a few sequences, in a window
+    (1, 64, 8, 64, 2640, 0, 0, 1040, [1600], None, 0, 0), (5, 64, 8, 64, 1900, 16, 1, 230, [1600, 1670, 1590, 1600, 1655], [230, 230, 229, 230, 225], 0, 0),
+    (1, 64, 8, 64, 2700, 0, 2, 1090, [1600], [1087], 30, 1570),
+    # ... and tiles whose pieces, rounded to the nearest number, would be a few too many
+    (1, 16, 2, 64, 9000, 0, 0, 600, [8400], None, 0, 0), (3, 16, 4, 64, 2600, 0, 0, 230, [2370, 2000, 2200], None, 0, 0),
     # more sequences than a wave has lanes, and than it looks through
     (130, 2, 2, 64, 96, 16, 0, 33, [(i * 37) % 90 for i in range(130)], [(i * 5) % 34 for i in range(130)], 0, 0),
     (300, 4, 1, 64, 64, 0, 1, 20, [(i * 37) % 60 - 1 for i in range(300)], [(i * 7) % 21 for i in range(300)], 2, 9),
