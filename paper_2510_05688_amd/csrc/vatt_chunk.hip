@@ -95,7 +95,7 @@ struct Cut {
   }
   __device__ __forceinline__ int pieces(int last) const { return piece == 0.f ? 1 : max(min((int)(last / piece + up), kPiecesMax), 1); }
   // `cut` pieces of one KV head: where a few too many for the slots would wait for all others, twice as many of half the length, rounded down (700
-  // new tokens on 32K, 176 tiles: three pieces each 490 us, five 420).
+  // new tokens on 32K, 176 tiles: three pieces each 514 us, five 425).
   __device__ __forceinline__ bool finer(const ChunkArgs& A, int cut) {
     if (cut * A.Hkv <= A.slots) return false;
     piece *= 0.5f;
@@ -105,7 +105,8 @@ struct Cut {
 };
 
 // Where nothing is long beside everybody's share, but the tiles leave a rest when the slots have been filled as often as they can be: the tiles of the
-// rest, the last in the order, in equally many pieces each, which fill the slots once or twice.  shortest: key tiles of the shortest tile.
+// rest, the last in the order, in equally many pieces each, which fill the slots once or twice (us whole / cut: 2304 new tokens on 32K, 576 tiles for 512 slots, 1390 / 1110, 1280
+// 770 / 702, 256 on 9 x 8K 407 / 322).  shortest: key tiles of the shortest tile.
 struct Rest {
   int whole, pieces;  // tiles of a KV head before the rest
   __device__ __forceinline__ Rest(const ChunkArgs& A, int count, int shortest) : whole(count), pieces(1) {
@@ -145,7 +146,9 @@ __device__ __forceinline__ int order(const ChunkArgs& A, int y, int count) {
 }
 
 // The batch's work, as every wave sees it: lane l has sequences l, l + 64, ...  Pieces come first, then the tiles that are not cut, the longest
-// first: what a tile costs goes by its place in the sequence, counted in tiles (its level).
+// first: what a tile costs goes by its place in the sequence, counted in tiles (its level).  In steps of an eighth of the highest level, within which a
+// sequence's tiles are neighbours, so that they read its rows from L2 (level by level 32 x 512 new tokens on 4K 1474 us, so 994; 256 on 24 x 8K 1010
+// and 790; ragged prompts the same within 1 %).
 struct Batch {
   int tiles[kSeqsPerLane], pieces[kSeqsPerLane], level[kSeqsPerLane];
   int cut;    // pieces of one KV head in all
