@@ -407,11 +407,14 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& A, int g_shift, Work&
     all.read(A, g_shift);
     return all.find(A, y, w);
   }
-  // too many sequences to look through: tile by tile from the end, beginning with another sequence each time (short sequences leave workgroups
-  // without work, and those with work should not all be on the same units)
-  const int rank = y / A.batch;
+  // too many sequences to look through: sequence by sequence, whose tiles read the same rows, each beginning with another tile (short sequences leave
+  // workgroups without work, and those with work should not all be on the same XCDs).  us with the tiles of a rank together / so: 256 new tokens on
+  // 300 x 1K 1934 / 1301, 64 on 300 x 2K 984 / 759.
+  const int most = ((A.n_new << g_shift) + kTileRows - 1) / kTileRows;
   w.slot = 0;
-  w.b = (y - rank * A.batch + rank) % A.batch;
+  w.b = y / most;
+  const int rank = (y - w.b * most + w.b) % most;
+  if (w.b >= A.batch) return false;
   w.tile = ((new_tokens(A, w.b).count << g_shift) + kTileRows - 1) / kTileRows - 1 - rank;
   w.piece = 0;
   w.pieces = 1;

@@ -321,6 +321,7 @@ SHARED = [
     # more sequences than a wave has lanes, and than it looks through
     (130, 2, 2, 64, 96, 16, 0, 33, [(i * 37) % 90 for i in range(130)], [(i * 5) % 34 for i in range(130)], 0, 0),
     (300, 4, 1, 64, 64, 0, 1, 20, [(i * 37) % 60 - 1 for i in range(300)], [(i * 7) % 21 for i in range(300)], 2, 9),
+    (260, 8, 1, 64, 90, 0, 0, 50, [(i * 37) % 90 - 1 for i in range(260)], [(i * 7) % 51 for i in range(260)], 0, 0),
 ]
 
 
