@@ -105,8 +105,8 @@ struct Cut {
 };
 
 // Where nothing is long beside everybody's share, but the tiles leave a rest when the slots have been filled as often as they can be: the tiles of the
-// rest, the last in the order, in equally many pieces each, which fill the slots once or twice (us whole / cut: 2304 new tokens on 32K, 576 tiles for 512 slots, 1390 / 1110, 1280
-// 770 / 702, 256 on 9 x 8K 407 / 322).  shortest: key tiles of the shortest tile.
+// rest, the last in the order, in equally many pieces each, which fill the slots once or twice (us whole / cut: 2304 new tokens on 32K, 576 tiles for 512 slots, 1393 / 1097, 2560
+// 1382 / 1257, 256 on 9 x 8K 384 / 314, 32 on 72 x 4K 297 / 248; at 256 on 12 x 2K to 8K, 768 tiles, it would not pay, and is not done).  shortest: key tiles of the shortest tile.
 struct Rest {
   int whole, pieces;  // tiles of a KV head before the rest
   __device__ __forceinline__ Rest(const ChunkArgs& A, int count, int shortest) : whole(count), pieces(1) {
@@ -114,10 +114,10 @@ struct Rest {
     if (A.room == 0 || shortest < kRestLeast || all <= A.slots) return;
     const int before = all / A.slots * A.slots / A.Hkv, rest = (count - before) * A.Hkv;
     if (rest == 0) return;
-    // in units of a key tile of a workgroup that shares its unit: one alone takes two thirds; a piece costs 3 more, the join 6 per filling
+    // in units of a key tile of a workgroup that shares its unit: one alone takes 0.6; pieces cost 14 for every filling of the slots
     const int most = min(shortest / kPieceLeast, kPiecesMax), once = min(A.slots / rest, most), twice = min(2 * A.slots / rest, most);
-    float least = 2 * rest <= A.slots ? 0.65f * shortest : (float)shortest;
-    const float a = (float)shortest / (float)max(once, 1) + 11.f, b = 2.f * (float)shortest / (float)max(twice, 1) + 20.f;
+    float least = 2 * rest <= A.slots ? 0.6f * shortest : (float)shortest;
+    const float a = (float)shortest / (float)max(once, 1) + 14.f, b = 2.f * (float)shortest / (float)max(twice, 1) + 28.f;
     if (once > 1 && a < least) {
       least = a;
       pieces = once;
