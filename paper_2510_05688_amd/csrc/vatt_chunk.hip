@@ -893,7 +893,9 @@ hipError_t launch_chunk_t(const Plan& pl, const ChunkArgs& A, hipStream_t st) {
   if (e != hipSuccess || A.room == 0) return e;
   // About a row per wave where a tile has few pieces (4 x 1K tokens, 32 new ones each, whole call 28.5 us with one workgroup per piece, 21.8 with
   // eight); one workgroup per piece where cuts are unlikely (with eight windowed prompts that are not cut take 147 us instead of 141).
-  const int64_t rows = std::min<int64_t>(kTileRows, (int64_t)A.n_new * pl.group), wgs = std::min<int64_t>(A.room, (4 * pl.num_cus + A.Hkv - 1) / A.Hkv);
+  // No more than two times the compute units to a part (4 windowed chunks of 100 tokens, not cut, 25.7 us, with four times 28.2; 33 tokens on
+  // 3 x 5K - 16K 46, with one time 51).
+  const int64_t rows = std::min<int64_t>(kTileRows, (int64_t)A.n_new * pl.group), wgs = std::min<int64_t>(A.room, (2 * pl.num_cus + A.Hkv - 1) / A.Hkv);
   const int64_t parts = 2 * tiles >= pieces ? 1 : std::max<int64_t>(1, std::min<int64_t>(8, rows / kChunkWaves * tiles / pieces));
   hipLaunchKernelGGL((chunk_merge_kernel<D, TERMS == 1>), dim3((uint32_t)(wgs * A.Hkv), (uint32_t)parts), dim3(kChunkThreads), 0, st, A);
   return hipGetLastError();
