@@ -20,6 +20,11 @@ constexpr int kPiecesMax = 64;      // pieces that a tile's keys are cut into at
 constexpr int kPieceLeast = 4;      // key tiles of a piece at least
 constexpr int kRestLeast = 24;      // key tiles of a tile that is cut because it is over
 constexpr float kOnePerUnit = 5000.f;  // key tiles in all below which there is one piece per compute unit, not two
+// Key tiles whose weighted rows are added up in one sum where the output has 32 bits.  A matrix instruction cuts its sums off, 12 times a tile: rows
+// of equal weight came out 2e-4 too small on 64K tokens and 7e-4 on 170K, so 1e-5 (with 32 tiles 8e-6, with 64 1.3e-5).  2K on 64K 3453 us in
+// one sum, 3551 so (with 32 tiles 3655).  Output in bf16 has one term, 4 sums a tile, and half a step of 4e-3: one sum.
+constexpr int kSumTiles = 48;
+constexpr int kAgainTiles = 8;  // the same where a row is worked out again, whose sums are rounded
 constexpr int kSteps = 8;           // of a tile's level, for the order (a power of two)
 constexpr int kSeqsPerLane = 4, kSeqsMax = kSeqsPerLane * kWave;  // sequences that a wave looks through for its work
 
@@ -309,6 +314,7 @@ __device__ __forceinline__ void store_4(void* out, int64_t at, float a, float b,
 }
 
 // One row again by one wave: dot products, every key only where it is seen.  (max, sum) and the lane's 8 columns (lane % (D / 8)).
+// (Sums of kAgainTiles tiles are added up, not all rows one by one: see lrest.)
 template <int D, int FMT, bool PAGED>
 __device__ __forceinline__ void row_again(const ChunkArgs& A, int b, int kvh, int64_t q_at, int p, const KeyTiles& T, int i0, int i1, float& m,
                                           float& l, float (&acc)[8]) {
@@ -316,11 +322,22 @@ __device__ __forceinline__ void row_again(const ChunkArgs& A, int b, int kvh, in
   const int lane = threadIdx.x & 63, sub = lane % LPR, rsub = lane / LPR;
   const uint4 qv = *reinterpret_cast<const uint4*>(A.q + q_at + sub * 8);
   const uint32_t qw[4] = {qv.x, qv.y, qv.z, qv.w};
+  float l_now = 0.f, now[8];
   m = -INFINITY;
   l = 0.f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+  for (int j = 0; j < 8; ++j) acc[j] = now[j] = 0.f;
+  auto add_now = [&]() {
+    l += l_now;
+    l_now = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      acc[j] += now[j];
+      now[j] = 0.f;
+    }
+  };
   for (int i = i0; i < i1; ++i) {
+    if ((i - i0) % kAgainTiles == 0) add_now();
     for (int r = rsub; r < kTileKeys; r += RPW) {
       const int tok = T.at(i) * kTileKeys + r;
       if (tok > p || (A.window > 0 && tok <= p - A.window && tok >= A.sink)) continue;
@@ -342,14 +359,18 @@ __device__ __forceinline__ void row_again(const ChunkArgs& A, int b, int kvh, in
       const float alpha = m == -INFINITY ? 0.f : m == shift ? 1.f : __builtin_amdgcn_exp2f(m - shift);
       const float w = __builtin_amdgcn_exp2f(s - shift);
       m = shift;
-      l = l * alpha + w;
+      l *= alpha;
+      l_now = l_now * alpha + w;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        acc[2 * j] = acc[2 * j] * alpha + w * bf16_lo(vw[j]);
-        acc[2 * j + 1] = acc[2 * j + 1] * alpha + w * bf16_hi(vw[j]);
+        acc[2 * j] *= alpha;
+        acc[2 * j + 1] *= alpha;
+        now[2 * j] = now[2 * j] * alpha + w * bf16_lo(vw[j]);
+        now[2 * j + 1] = now[2 * j + 1] * alpha + w * bf16_hi(vw[j]);
       }
     }
   }
+  add_now();
   float all = m;
 #pragma unroll
   for (int o = LPR; o < kWave; o <<= 1) all = fmaxf(all, __shfl_xor(all, o));
@@ -557,7 +578,9 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
   for (int e = 0; e < E; ++e)
 #pragma unroll
     for (int j = 0; j < 16; ++j) acc[e][j] = 0.f;
-  float mrun = -INFINITY, lrun = 0.f;
+  // The sum of the weights so far is lrun + lrest: a tile's 32 weights of a lane are added up by themselves, and what their sum loses when it is added
+  // to lrun goes to lrest.  Added one by one, the weights of 64K keys of equal score lose up to 5e-4 of their sum.
+  float mrun = -INFINITY, lrun = 0.f, lrest = 0.f, ltile = 0.f;
   bool any = false;
 
   auto first_product = [&](int parity) __attribute__((always_inline)) {
@@ -606,6 +629,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
     alpha = mrun == mnew ? 1.f : __builtin_amdgcn_exp2f(mrun - mnew);
     mrun = mnew;
     lrun *= alpha;
+    lrest *= alpha;
     return true;
   };
   auto weights = [&](int u, float m) __attribute__((always_inline)) {  // of the keys of step u of the second product
@@ -613,7 +637,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       y[j] = __builtin_amdgcn_exp2f(fmaf(sc[u / 2][8 * (u % 2) + j], A.log2_scale, -m));
-      lrun += y[j];
+      ltile += y[j];
     }
     if constexpr (BF16) {
       pb[u][0] = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
@@ -656,6 +680,40 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
     }
   };
 
+  // 32 bits: after kSumTiles tiles the sums go, added to those that went before, to the place of the row's result, at which they are relative to
+  // maximum m_away; at the end they come back.
+  float m_away = -INFINITY;
+  bool away = false;  // (uniform)
+  const int64_t out_row = ((int64_t)b * A.n_new + t) * A.Hq + head, place = ((int64_t)W.slot * A.Hkv + kvh) * kTileRows + wave * kWaveRows + col;
+  auto add_away = [&](auto back) __attribute__((always_inline)) {
+    if (row >= rows) return;
+    float* at = (pieces == 1 ? static_cast<float*>(A.out_o) + out_row * D : A.part + place * D) + 4 * half;
+    const float f = m_away == mrun ? 1.f : __builtin_amdgcn_exp2f(m_away - mrun);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        float4* p = reinterpret_cast<float4*>(at + 32 * e + 8 * x);
+        if (away) {
+          const float4 y = *p;
+          acc[e][4 * x] += y.x * f;
+          acc[e][4 * x + 1] += y.y * f;
+          acc[e][4 * x + 2] += y.z * f;
+          acc[e][4 * x + 3] += y.w * f;
+        }
+        if constexpr (decltype(back)::value == 0) {
+          *p = make_float4(acc[e][4 * x], acc[e][4 * x + 1], acc[e][4 * x + 2], acc[e][4 * x + 3]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[e][4 * x + j] = 0.f;
+        }
+      }
+  };
+  auto put_away = [&]() __attribute__((always_inline)) {
+    add_away(K);
+    m_away = mrun;
+    away = true;
+  };
+
   // V is one tile behind K: the second product of tile i - 1 is made while the weights of tile i are, on the matrix cores and beside them.
   if (i0 < i1) {
     int blk[2] = {block_of(i0, 0), block_of(i0, 1)};
@@ -696,6 +754,10 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
           if constexpr (!FIRST) second_product(u, other);
           weights(u, m);
         }
+        const float sum = lrun + ltile, part = sum - lrun;
+        lrest += (lrun - (sum - part)) + (ltile - part);
+        lrun = sum;
+        ltile = 0.f;
         // (made here, beside the products, not after the branch)
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -713,16 +775,22 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
       parity = other;
     };
     step(i0, V);
-    for (int i = i0 + 1; i < i1; ++i) step(i, K);
+    for (int i = i0 + 1; i < i1;) {
+      const int stop = BF16 ? i1 : min(i + kSumTiles, i1);
+      for (; i < stop; ++i) step(i, K);
+      if (!BF16 && active && i < i1) put_away();
+    }
     if (active) {
 #pragma unroll
       for (int u = 0; u < 4; ++u) second_product(u, parity ^ 1);
+      if (!BF16 && away) add_away(V);
     }
   }
   if (!active) return;
 
   // A result with an Inf or a NaN is worked out again: the second product gives every row every V row of a tile, with weight 0 where
   // the row does not see the key (and in three terms of which some are 0), so that an Inf or a NaN has a say where it should have none.
+  lrun += lrest;
   float l = lrun + __shfl_xor(lrun, 32);
   const bool saw = any || __shfl_xor((int)any, 32);
   float sum = 0.f;
@@ -732,7 +800,6 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
     for (int j = 0; j < 16; ++j) sum += fabsf(acc[e][j]);
   const uint64_t odd = __ballot(!(sum < INFINITY) || !(l < INFINITY));
   uint32_t again = (uint32_t)odd | (uint32_t)(odd >> 32);
-  const int64_t out_row = ((int64_t)b * A.n_new + t) * A.Hq + head;
   const float m_own = saw && mrun == -INFINITY ? -3.0e38f : mrun, inv = 1.f / l;
   // bf16: a row's two lanes change columns 8 x + 4 half .. + 3 of two groups for all 8 of one
   uint4 out16[BF16 ? E : 1][2];
@@ -768,7 +835,6 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(ChunkArgs A) {
       }
       if (A.out_lse && half == 0) A.out_lse[out_row] = m_own * 0.69314718055994530942f + logf(l);
     } else {
-      const int64_t place = ((int64_t)W.slot * A.Hkv + kvh) * kTileRows + wave * kWaveRows + col;
 #pragma unroll
       for (int e = 0; e < E; ++e)
 #pragma unroll
