@@ -18,6 +18,7 @@ constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / kWave;
 constexpr int kUnit = 32;          // keys that a wave takes at a time
 constexpr int kSlots = 1024;       // groups of 8 tokens that a workgroup looks up at a time
 constexpr int kSplitsMax = 128;
+constexpr int kAgainRows = 128;     // rows that are added up in one sum where a result is worked out again
 constexpr int kNowhere = 0x7fffff00;  // token of a group that does not exist: beyond every sequence
 
 // Which tokens: all of them, those of listed blocks, or the first `sink` and the last `window` up to each query's own.
@@ -132,6 +133,19 @@ __device__ __forceinline__ void attend_again(const AttendArgs& A, const uint16_t
   const uint4 qv = *reinterpret_cast<const uint4*>(q + sub * 8);
   const uint32_t qw[4] = {qv.x, qv.y, qv.z, qv.w};
   float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  // (sums of up to kAgainRows rows are added up, not all rows one by one: see lrest)
+  float l_now = 0.f, now[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  int rows = 0;
+  auto add_now = [&]() {
+    l += l_now;
+    l_now = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      acc[j] += now[j];
+      now[j] = 0.f;
+    }
+    rows = 0;
+  };
   for (int64_t i = wave * RPW + rsub; i < (int64_t)L.count * 8; i += WAVES * RPW) {
     const int group = (int)(i >> 3), tok = token_of<KIND>(L, group, entry_of<KIND>(L, group)) + (int)(i & 7);
     if (tok >= L.n || (KIND == kFirstAndWindow && !L.seen(tok))) continue;
@@ -153,13 +167,18 @@ __device__ __forceinline__ void attend_again(const AttendArgs& A, const uint16_t
     const float alpha = m == -INFINITY ? 0.f : m == shift ? 1.f : __builtin_amdgcn_exp2f(m - shift);
     const float p = __builtin_amdgcn_exp2f(s - shift);
     m = shift;
-    l = l * alpha + p;
+    l *= alpha;
+    l_now = l_now * alpha + p;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      acc[2 * j] = acc[2 * j] * alpha + p * bf16_lo(vw[j]);
-      acc[2 * j + 1] = acc[2 * j + 1] * alpha + p * bf16_hi(vw[j]);
+      acc[2 * j] *= alpha;
+      acc[2 * j + 1] *= alpha;
+      now[2 * j] = now[2 * j] * alpha + p * bf16_lo(vw[j]);
+      now[2 * j + 1] = now[2 * j + 1] * alpha + p * bf16_hi(vw[j]);
     }
+    if (++rows == kAgainRows) add_now();
   }
+  add_now();
   float all = m;
 #pragma unroll
   for (int o = LPR; o < kWave; o <<= 1) all = fmaxf(all, __shfl_xor(all, o));
@@ -288,12 +307,14 @@ __device__ __forceinline__ void attend_part(const AttendArgs& A, const AttendPar
   const uint32_t last_term = PACK == 2 && term == 1 ? 0xffffffffu : 0u;
 
   f32x4_t acc[NQT][E];
-  float mrun[NQT], lrun[NQT];  // running maxima of the scores in units of log 2
+  // Running maxima of the scores in units of log 2, and sums of the weights, lrun + lrest: the 8 weights of a step are added up by themselves, and what
+  // their sum loses when it is added to lrun goes to lrest.  One by one the weights of 170K keys of equal score would lose 1e-4 of their sum.
+  float mrun[NQT], lrun[NQT], lrest[NQT];
   bool any[NQT];
 #pragma unroll
   for (int nt = 0; nt < NQT; ++nt) {
     mrun[nt] = -INFINITY;
-    lrun[nt] = 0.f;
+    lrun[nt] = lrest[nt] = 0.f;
     any[nt] = false;
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[nt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -467,15 +488,17 @@ __device__ __forceinline__ void attend_part(const AttendArgs& A, const AttendPar
           const float alpha = mrun[nt] == mnew ? 1.f : __builtin_amdgcn_exp2f(mrun[nt] - mnew);
           mrun[nt] = mnew;
           lrun[nt] *= alpha;
+          lrest[nt] *= alpha;
 #pragma unroll
           for (int e = 0; e < E; ++e) acc[nt][e] *= alpha;
         }
         const float m = mrun[nt] == -INFINITY ? 0.f : mrun[nt];  // (so far every score is -Inf: weights 0)
         uint32_t w[TERMS][8];
+        float step = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float p = __builtin_amdgcn_exp2f(fmaf(s[j], A.log2_scale, -m));
-          lrun[nt] += p;
+          step += p;
           if constexpr (PACK > 1) {
             float r = p - __uint_as_float(__float_as_uint(p) & first_term);
             if constexpr (PACK == 3) r -= __uint_as_float(__float_as_uint(r) & second_term);
@@ -489,6 +512,9 @@ __device__ __forceinline__ void attend_part(const AttendArgs& A, const AttendPar
             w[2][j] = __float_as_uint(r2);
           }
         }
+        const float sum = lrun[nt] + step, of_step = sum - lrun[nt];
+        lrest[nt] += (lrun[nt] - (sum - of_step)) + (step - of_step);
+        lrun[nt] = sum;
 #pragma unroll
         for (int x = 0; x < TERMS; ++x)
           pb[nt][x] = make_uint4(upper_halves(w[x][0], w[x][1]), upper_halves(w[x][2], w[x][3]), upper_halves(w[x][4], w[x][5]),
@@ -548,7 +574,7 @@ __device__ __forceinline__ void attend_part(const AttendArgs& A, const AttendPar
   uint32_t odd = 0;  // vectors with an Inf or a NaN with an Inf or a NaN
 #pragma unroll
   for (int nt = 0; nt < NQT; ++nt) {
-    float l = lrun[nt];
+    float l = lrun[nt] + lrest[nt];
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     int saw = any[nt];

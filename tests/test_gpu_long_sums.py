@@ -125,6 +125,14 @@ def test_rows_worked_out_again():
     assert max(decode_errors(257, 1, 65536, 0, q_len=2, odd=(65535,))) <= TOL
 
 
+# (sequences, KV heads, tokens, format, dense, queries): window decode, and dense decode of a quantised cache, by one workgroup per sequence and KV head
+@pytest.mark.parametrize("case", [(257, 1, 170752, 0, False, 1), (256, 4, 170752, 0, False, 1), (256, 4, 65536, 2, False, 17), (256, 4, 65536, 1, False, 6),
+                                  (256, 4, 170752, 1, True, 1)], ids=str)
+def test_decode_of_equal_weights(case):
+    batch, hkv, n, fmt, dense, q_len = case
+    assert max(decode_errors(batch, hkv, n, fmt, dense, q_len)) <= TOL
+
+
 @pytest.mark.parametrize("low", [False, True])
 @pytest.mark.parametrize("n,d,n_new,sink,window", [(12000, 64, 768, 0, 0), (12000, 128, 768, 0, 0), (12000, 64, 768, 100, 9000), (12000, 128, 40, 0, 0),
                                                    (12000, 64, 61, 700, 10000), (65536, 128, 64, 0, 0)])
