@@ -492,7 +492,8 @@ int vatt_chunk_attend(vatt_plan* plan, const void* q, int64_t q_stride, int n_ne
 /*
  * A decode step over the first `sink` (>= 0) and the last `window` (>= 1) tokens that each query sees, its own among them: the
  * deterministic set of Algorithm 1 without top-k and samples, for layers that attend to a window.  The sizes are the call's, not
- * those of the plan.  K and V in the plan's format; other arguments as in vatt_dense_decode.
+ * those of the plan.  K and V in the plan's format; out_o 16-byte aligned, no output over an input; other
+ * arguments as in vatt_dense_decode.
  */
 int vatt_window_decode(vatt_plan* plan, const void* q, const void* k, const void* v, const int32_t* block_table,
                        const int32_t* seq_lens, int sink, int window, void* workspace, size_t workspace_bytes, float* out_o,

@@ -857,7 +857,7 @@ int vatt_window_decode(vatt_plan* plan, const void* q, const void* k, const void
                        float* out_lse, void* stream) {
   if (!plan) return VATT_E_INVALID_ARG;
   if (!q || !k || !v || !seq_lens || !out_o || sink < 0 || window < 1) return VATT_E_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return VATT_E_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out_o)) return VATT_E_INVALID_ARG;
   const int rc = check_common(plan, workspace, workspace_bytes, block_table);
   if (rc != VATT_OK) return rc;
   VATT_LAUNCH(launch_window(plan->pl, q, k, v, block_table, seq_lens, sink, window, workspace, out_o, out_lse,
