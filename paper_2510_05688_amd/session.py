@@ -265,6 +265,8 @@ class DecodeSession:
         self.written = False
         if self.first is None:
             self.first = torch.empty_like(self.seq_lens)
+        if new_lens is not None and any(self._overlap(new_lens, x) for x in (self.seq_lens, self.first)):
+            new_lens = new_lens.clone()  # (both are written to)
         self.first.copy_(self.seq_lens)
         vb.vatt_write_kv(self.plan, q, k_new, v_new, *strides, k_new.shape[1], self.first, new_lens, self.k, self.v, self.block_table,
                          self.summary, out_q, self.seq_lens, self._stream())
@@ -302,6 +304,12 @@ class DecodeSession:
         """A decode step over the first `sink` and the last `window` tokens, into out_o and out_lse."""
         vb.vatt_window_decode(self.plan, self._query(q), self.k, self.v, self.block_table, self.seq_lens, sink, window, self.workspace,
                               self.out_o, self.out_lse, self._stream())
+
+    @staticmethod
+    def _overlap(x, y):
+        """Whether two tensors, each one value behind the other, share memory."""
+        a, b = x.data_ptr(), y.data_ptr()
+        return a < b + y.numel() * y.element_size() and b < a + x.numel() * x.element_size()
 
     def _check(self, name, x, dtype, *shape):
         """A kernel gets x as an address: x has to be a tensor of so many values, one behind the other, on this device (None is left to
