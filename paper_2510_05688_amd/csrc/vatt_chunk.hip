@@ -957,8 +957,13 @@ bool chunk_may_cut(const Plan& pl, int n_new, bool fewer, int64_t keys) {
   const double tiles = (double)all / chunk_slots(pl);
   return longest > 1.25 * tiles * (longest - own / 2) + 12 || own > 1.25 * tiles * own / 2 + 12;
 }
-// Pieces at most: a sequence's tiles are cut into two or more where they are one and a half pieces long, and all tiles at their longest have no more
-// than a piece for every slot, so that the rounding adds a third.
+// Pieces at most, so that what all tiles are cut into has room:
+//   * A piece has 1 / 0.97 of an equal share of all tiles at their longest, `most`, for a slot each (Cut), so that all are 0.97 slots pieces long.  Two or
+//     more to the nearest number are 4/3 of that at most: 1.3 slots.
+//   * Only where these are more than the slots they are halved (Cut::finer): rounded down, 2 * 0.97 = 1.94 slots.
+//   * Of a rest (Rest) there are two slots full.
+//   * A tile of n key tiles has ceil(n / kPieceLeast) pieces at most: a piece is no shorter, and a halved one is longer too, since below kOnePerUnit
+//     key tiles there is one piece for two slots, never more than the slots, and above it half a piece is 5000 / (2 * 0.97 slots) = 5.
 int64_t chunk_pieces(const Plan& pl, int n_new, bool fewer, int64_t keys) {
   if (!chunk_may_cut(pl, n_new, fewer, keys)) return 0;
   const int64_t longest = (pl.p.n_max + kTileKeys - 1) / kTileKeys, each = std::min<int64_t>((longest + kPieceLeast - 1) / kPieceLeast, kPiecesMax);
