@@ -42,7 +42,6 @@ namespace {
 
 int window_rounds(const Plan& pl, int q_len) { return pl.group * q_len <= 16 ? 1 : (pl.group * q_len + 31) / 32; }
 int64_t window_jobs(const Plan& pl, int q_len) { return (int64_t)pl.p.batch * pl.p.n_kv_heads * window_rounds(pl, q_len); }
-int window_slot_rows(const Plan& pl, int q_len) { return pl.group * q_len <= 16 ? 16 : 32; }
 // Workgroups that the tokens are dealt out to, two to a compute unit, and no more than the merge takes for one job; 0: every job has one of eight
 // waves.  So it is for up to 640 tokens (4 and 256, us, shared by four / alone: 1 x 8K 16.2 / 11.6, 16 in e4m3 26.8 / 13.2; 4 and 512 15.6 / 14.7, 768
 // 15.3 / 16.3), where there are jobs for all slots (64 sequences in e4m3, 4 and 2048 72 / 62), and with more sequences than a wave looks through.
@@ -51,14 +50,14 @@ int window_workgroups(const Plan& pl, int q_len, int64_t longest) {
   if (longest <= 640 || (window_jobs(pl, q_len) >= slots && longest <= 4608) || pl.p.batch > kDealtMost) return 0;
   return (int)std::min<int64_t>(slots, (int64_t)(kSplitsMax - 2) * pl.p.n_kv_heads * window_rounds(pl, q_len));
 }
-// Bytes of the partial sums (a workgroup's share ends inside a job, or a job ends inside a share) and of the jobs' list.
-size_t window_part_bytes(const Plan& pl, int q_len, int workgroups) {
+// Bytes of the partial sums (a workgroup's share ends inside a job, or a job ends inside a share) of `rows` vectors each, and of the jobs' list.
+size_t window_part_bytes(const Plan& pl, int q_len, int workgroups, int rows) {
   const int64_t jobs = window_jobs(pl, q_len);
-  return (size_t)(workgroups + jobs) * window_slot_rows(pl, q_len) * (pl.p.head_dim + 2) * sizeof(float) + jobs * sizeof(int2);
+  return (size_t)(workgroups + jobs) * rows * (pl.p.head_dim + 2) * sizeof(float) + jobs * sizeof(int2);
 }
 
 hipError_t launch_rows(const Plan& pl, AttendArgs& A, const void* q, const void* k, const void* v, const int32_t* block_table, int sink,
-                       int window, int workgroups, void* ws, hipStream_t st) {
+                       int window, int workgroups, int slot_rows, void* ws, hipStream_t st) {
   A.q = static_cast<const uint16_t*>(q);
   A.k = static_cast<const unsigned char*>(k);
   A.v = static_cast<const unsigned char*>(v);
@@ -71,7 +70,7 @@ hipError_t launch_rows(const Plan& pl, AttendArgs& A, const void* q, const void*
   A.window = std::min(window, pl.p.n_max);
   A.batch = pl.p.batch;
   A.rounds = window_rounds(pl, A.q_len);
-  A.slot_rows = window_slot_rows(pl, A.q_len);
+  A.slot_rows = slot_rows;
   A.workgroups = workgroups;
   A.part = static_cast<float*>(ws);
   A.slots = (int)(workgroups + window_jobs(pl, A.q_len));
@@ -92,17 +91,25 @@ hipError_t launch_window(const Plan& pl, const void* q, const void* k, const voi
   A.out_lse = out_lse;
   // (whole groups of 8 at both ends of the window)
   const int64_t longest = std::min<int64_t>(pl.p.n_max, (int64_t)std::min(sink, pl.p.n_max) + std::min(window, pl.p.n_max) + pl.q_len + 14);
+  // The workspace is the plan's, which other calls size: sums of as many vectors as there are, not of 16, for which it has room in a part of the
+  // workgroups only (us in so many / in all, one sequence in bf16, one query head per KV head: 8 KV heads and 4096 tokens, 118 of 512, 19.9 / 14.5, 8000,
+  // 152, 21.5 / 17.7; one and 9000, 20 of 126, 16.2 / 15.6; but four and 16000, 111 of 504, 21.0 / 22.0).
+  const int vectors = pl.group * pl.q_len, rows = vectors <= 16 ? vectors : 32;
   int workgroups = window_workgroups(pl, pl.q_len, longest);
-  if (window_part_bytes(pl, pl.q_len, workgroups) > pl.ws_bytes) {  // as many as there is room for
-    const int64_t least = (int64_t)window_part_bytes(pl, pl.q_len, 0), one = (int64_t)window_part_bytes(pl, pl.q_len, 1) - least;
+  if (window_part_bytes(pl, pl.q_len, workgroups, rows) > pl.ws_bytes) {  // as many as there is room for (17 vectors of one KV head on 700 tokens: 102 of 126)
+    const int64_t least = (int64_t)window_part_bytes(pl, pl.q_len, 0, rows), one = (int64_t)window_part_bytes(pl, pl.q_len, 1, rows) - least;
     workgroups = (int)std::max<int64_t>(((int64_t)pl.ws_bytes - least) / one, 0);
   }
-  return launch_rows(pl, A, q, k, v, block_table, sink, window, workgroups, ws, st);
+  return launch_rows(pl, A, q, k, v, block_table, sink, window, workgroups, rows, ws, st);
 }
+
+namespace {
+int few_slot_rows(const Plan& pl, int n_new) { return pl.group * n_new <= 16 ? 16 : 32; }
+}  // namespace
 
 size_t few_workspace_bytes(const Plan& pl, int n_new) {
   const int workgroups = window_workgroups(pl, n_new, pl.p.n_max);  // (a window leaves no more)
-  return workgroups == 0 ? 0 : window_part_bytes(pl, n_new, workgroups);
+  return workgroups == 0 ? 0 : window_part_bytes(pl, n_new, workgroups, few_slot_rows(pl, n_new));
 }
 
 hipError_t launch_few(const Plan& pl, const void* q, int64_t q_stride, int n_new, const int32_t* first, const int32_t* new_lens, const void* k,
@@ -118,7 +125,8 @@ hipError_t launch_few(const Plan& pl, const void* q, int64_t q_stride, int n_new
   A.out_bf16 = bf16;
   const int64_t seen = window > 0 ? (int64_t)std::min(sink, pl.p.n_max) + std::min(window, pl.p.n_max) + n_new + 14 : pl.p.n_max;
   const int workgroups = window_workgroups(pl, n_new, std::min<int64_t>(pl.p.n_max, seen));
-  return launch_rows(pl, A, q, k, v, block_table, window > 0 ? sink : 0, window > 0 ? window : pl.p.n_max, workgroups, ws, st);
+  return launch_rows(pl, A, q, k, v, block_table, window > 0 ? sink : 0, window > 0 ? window : pl.p.n_max, workgroups, few_slot_rows(pl, n_new), ws,
+                     st);
 }
 
 }  // namespace vatt

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from test_gpu_cache_ops import Setup, _bf16
-from test_gpu_new_tokens import SHARED, WINDOWS, _check_rows, _decode_places, _stream, _window
+from test_gpu_new_tokens import SHARED, WINDOWS, _check_rows, _chunk, _decode_places, _stream, _window
 
 pytestmark = pytest.mark.gpu
 
@@ -57,6 +57,17 @@ def test_window_decode(case):
     s.vb.vatt_window_decode(s.plan, q, s.k, s.v, s.table, s.ints(lens), sink, window, ws, o, lse, _stream())
     torch.cuda.synchronize()
     assert (buf[need:] == PATTERN).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d,n", [(8, 8, 128, 8192), (1, 1, 128, 9000), (4, 4, 128, 16384), (4, 2, 64, 3000), (32, 8, 128, 2000)])
+def test_window_decode_has_room_for_all_workgroups(hq, hkv, d, n):
+    """In the plan's workspace, which other calls size: the tokens are dealt out as vatt_chunk_attend does it in a workspace of its own, to the same bits."""
+    s = Setup(1, hq, hkv, d, n, 0, 1, None, seed=n, topk_frac=0.025, base_frac=0.025)
+    q = _bf16(s.rng.normal(size=(1, 1, hq, d)))
+    o, lse = _window(s, q, [n], 0, n)
+    _check_rows(s, q, [[n - 1]], 0, n, o, lse, False)
+    for a, b in zip((o, lse), _chunk(s, q, [n - 1], None, 0, 0, False)):
+        assert torch.equal(a, b)
 
 
 def test_window_decode_with_room_for_a_part_of_the_workgroups():
