@@ -571,7 +571,7 @@ __device__ __forceinline__ void attend_part(const AttendArgs& A, const AttendPar
 
   // The waves' sums together, one 16-vector tile at a time, in the result layout (of eight waves the upper four's go to the lower four first):
   // wave w finishes rows 4 g + w.
-  uint32_t odd = 0;  // vectors with an Inf or a NaN with an Inf or a NaN
+  uint32_t odd = 0;  // vectors with an Inf or a NaN
 #pragma unroll
   for (int nt = 0; nt < NQT; ++nt) {
     float l = lrun[nt] + lrest[nt];

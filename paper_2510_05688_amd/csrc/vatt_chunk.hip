@@ -86,8 +86,9 @@ struct Work {
 // Pieces that the tiles of sequences are cut into.  total: key tiles of all tiles of one KV head, most: if each had as many as its sequence's last one.
 // Tiles that are long beside what all work comes to per workgroup slot are cut into pieces of about that length, all tiles of a sequence into
 // equally many; their sums are joined by the merge.  Where there is little to do one piece per compute unit is better than two, whose sums are twice
-// the bytes: us with two / one, 16 new tokens on 1 x 16K 32.5 / 28.2, 64 45.9 / 40.7, but 64 on 3 x 5K - 16K 63.7 / 83.2, 33 with groups of 8 47.2 / 58.1.
-// They are a little longer than an equal share, so that rounding leaves none over for which nobody is free (33 with groups of 8 55.0 -> 47.2).
+// the bytes: us with two / one (three calls at a time, as here below), 16 new tokens on 1 x 16K 33.8 / 29.3, 64 46.0 / 40.6, but 64 on 3 x 5K - 16K
+// 66 / 85, 33 with groups of 8 49.0 / 60.4.  They are a little longer than an equal share, so that rounding leaves none over for which nobody is free (33
+// with groups of 8 62.6 -> 49.0).
 // (32-bit values, rounded the same way wherever this is worked out.)
 struct Cut {
   float piece;  // key tiles; 0: nothing is cut
@@ -100,7 +101,7 @@ struct Cut {
   }
   __device__ __forceinline__ int pieces(int last) const { return piece == 0.f ? 1 : max(min((int)(last / piece + up), kPiecesMax), 1); }
   // `cut` pieces of one KV head: where a few too many for the slots would wait for all others, twice as many of half the length, rounded down (700
-  // new tokens on 32K, 176 tiles: three pieces each 514 us, five 425).
+  // new tokens on 32K, 176 tiles: three pieces each 503 us, five 411).
   __device__ __forceinline__ bool finer(const ChunkArgs& A, int cut) {
     if (cut * A.Hkv <= A.slots) return false;
     piece *= 0.5f;
@@ -110,8 +111,10 @@ struct Cut {
 };
 
 // Where nothing is long beside everybody's share, but the tiles leave a rest when the slots have been filled as often as they can be: the tiles of the
-// rest, the last in the order, in equally many pieces each, which fill the slots once or twice (us whole / cut: 2304 new tokens on 32K, 576 tiles for 512 slots, 1393 / 1097, 2560
-// 1382 / 1257, 256 on 9 x 8K 384 / 314, 32 on 72 x 4K 297 / 248; at 256 on 12 x 2K to 8K, 768 tiles, it would not pay, and is not done).  shortest: key tiles of the shortest tile.
+// rest, the last in the order, in equally many pieces each, which fill the slots once or twice (us whole / cut: 2304 new tokens on 32K, 576 tiles for
+// 512 slots, 1384 / 1094, 2560 1412 / 1264, 256 on 9 x 8K 390 / 312, 32 on 72 x 4K 293 / 248; at 256 on 12 x 2K to 8K, 768 tiles, it would not pay, and
+// is not done).  shortest: key tiles of the batch's shortest tile, from which the pieces are worked out for all, so that this is for sequences of about one
+// length: with one of 300 tokens among them nothing is cut (9 x 8K and that one 378, 72 x 4K and that one 292).
 struct Rest {
   int whole, pieces;  // tiles of a KV head before the rest
   __device__ __forceinline__ Rest(const ChunkArgs& A, int count, int shortest) : whole(count), pieces(1) {
@@ -454,7 +457,7 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& A, int g_shift, Work&
 // The running maximum of a row moves only when a score passes it by more than kLazy (the sums are then at most 2^8 times larger, and fp32 has
 // 2^127), so that the results so far are seldom multiplied.
 // Bound by the matrix cores and the vector instructions beside them, at the clock that the power allows: 2048 tokens on 64K (group of 4, d 128,
-// bf16) 2.02 ms, 1070 TFLOP/s of the 1253 that a large product reaches; the matrix cores are busy for 67 % of the cycles, no LDS bank conflicts.
+// bf16) 2.01 ms, 1075 TFLOP/s of the 1232 that a large product reaches; the matrix cores are busy for 65 % of the cycles, no LDS bank conflicts.
 // A tile of 64 keys takes a workgroup of a full compute unit 2 us (e4m3 2.2, output in 32 bits with d 64 2.5).
 // 128 rows, since each row of K and V read from LDS then serves 32 rows of a wave and each loaded one 128; two workgroups per unit, since one's
 // barriers are then the other's time (64 KB of LDS each).  The second product is made one tile late, so that the weights' exponentials have matrix
@@ -978,8 +981,8 @@ hipError_t launch_chunk_t(const Plan& pl, const ChunkArgs& A, hipStream_t st) {
   if (e != hipSuccess || A.room == 0) return e;
   // About a row per wave where a tile has few pieces (4 x 1K tokens, 32 new ones each, whole call 28.5 us with one workgroup per piece, 21.8 with
   // eight); one workgroup per piece where cuts are unlikely (with eight windowed prompts that are not cut take 147 us instead of 141).
-  // No more than two times the compute units to a part (4 windowed chunks of 100 tokens, not cut, 25.7 us, with four times 28.2; 33 tokens on
-  // 3 x 5K - 16K 46, with one time 51).
+  // No more than two times the compute units to a part (4 windowed chunks of 100 tokens, not cut, 28.2 us, with four times 30.3; 33 tokens on
+  // 3 x 5K - 16K 49, with one time 54).
   const int64_t rows = std::min<int64_t>(kTileRows, (int64_t)A.n_new * pl.group), wgs = std::min<int64_t>(A.room, (2 * pl.num_cus + A.Hkv - 1) / A.Hkv);
   const int64_t parts = 2 * tiles >= pieces ? 1 : std::max<int64_t>(1, std::min<int64_t>(8, rows / kChunkWaves * tiles / pieces));
   hipLaunchKernelGGL((chunk_merge_kernel<D, TERMS == 1>), dim3((uint32_t)(wgs * A.Hkv), (uint32_t)parts), dim3(kChunkThreads), 0, st, A);
